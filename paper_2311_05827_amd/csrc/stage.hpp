@@ -1,0 +1,149 @@
+// Internal declarations of the stage operators: layer norm, blocks in 8-bit floating point, their product.
+#pragma once
+
+#include "accept_stage.h"
+#include "common.hpp"
+
+namespace accept {
+
+constexpr int kQBlock = 128;         // values along the contracted axis that share a scale
+constexpr int kMinExponent = -100;   // of a scale
+
+inline int64_t up_to(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+inline int64_t blocks_of(int64_t v, int64_t by) { return (v + by - 1) / by; }
+
+struct NormPlan {
+  int back_grid;  // workgroups of the backward pass = number of partial column sums
+  size_t bytes;   // workspace
+};
+NormPlan make_nplan(const accept_norm_desc& d);
+hipError_t launch_norm(const accept_norm_desc& d, const void* x, const void* weight, const void* bias, void* y,
+                       float* stats, hipStream_t s);
+hipError_t launch_norm_quantize(const accept_norm_desc& d, const void* x, const void* weight, const void* bias, void* codes,
+                                void* scales, float* stats, hipStream_t s);
+hipError_t launch_norm_backward(const accept_norm_desc& d, const NormPlan& p, const void* dy, const void* x,
+                                const void* weight, const float* stats, void* dx, void* dweight, void* dbias, void* ws,
+                                hipStream_t s);
+
+hipError_t launch_block_quantize(const accept_block_desc& d, const void* x, void* codes, void* scales, void* codes_t,
+                                 void* scales_t, hipStream_t s);
+
+struct MatmulPlan {
+  int tile;      // which kernel (see make_matmul_plan)
+  int splits;    // parts of the contracted axis, joined by a second kernel where there are several
+  size_t bytes;  // workspace
+};
+MatmulPlan make_matmul_plan(const accept_matmul_desc& d);
+hipError_t launch_matmul(const accept_matmul_desc& d, const MatmulPlan& p, const void* a, const void* a_scales, const void* b,
+                         const void* b_scales, void* y, void* ws, hipStream_t s);
+
+#if defined(__HIPCC__)
+
+// VEC consecutive elements from any element's alignment; the ones from `left` on are zeros and are not read.
+typedef uint32_t v4u_elem_t __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t v4u_word_t __attribute__((ext_vector_type(4), aligned(4)));
+template <typename T>
+__device__ __forceinline__ uint4 load_raw(const T* p, int64_t left) {
+  constexpr int VEC = Elem<T>::VEC;
+  uint4 r = make_uint4(0, 0, 0, 0);
+  if (left >= VEC) {
+    if constexpr (VEC == 4) {
+      const v4u_word_t v = *reinterpret_cast<const v4u_word_t*>(p);
+      r = make_uint4(v.x, v.y, v.z, v.w);
+    } else {
+      const v4u_elem_t v = *reinterpret_cast<const v4u_elem_t*>(p);
+      r = make_uint4(v.x, v.y, v.z, v.w);
+    }
+  } else if (left > 0) {
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < VEC - 1; ++j) {
+      if (j < left) {
+        if constexpr (VEC == 4) w[j] = f32_as_u32(p[j]);
+        else w[j / 2] |= uint32_t(p[j].bits) << (16 * (j & 1));
+      }
+    }
+    r = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  return r;
+}
+
+// N values as elements of T from any element's alignment on; those from `left` on are not written.
+template <typename T, int N>
+__device__ __forceinline__ void store_values(T* p, const float (&f)[N], int64_t left) {
+  static_assert(N == 4 || N == 8, "a vector");
+  if (left >= N) {
+    if constexpr (sizeof(T) == 4) {
+      typedef float v4_t __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+      for (int i = 0; i < N; i += 4) *reinterpret_cast<v4_t*>(p + i) = v4_t{f[i], f[i + 1], f[i + 2], f[i + 3]};
+    } else {
+      typedef uint32_t vec_t __attribute__((ext_vector_type(N / 2), aligned(2)));
+      vec_t v;
+#pragma unroll
+      for (int i = 0; i < N; i += 2) v[i / 2] = bf16_pair(f[i], f[i + 1]);
+      *reinterpret_cast<vec_t*>(p) = v;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N - 1; ++i)
+      if (i < left) {
+        if constexpr (sizeof(T) == 4) p[i] = f[i];
+        else p[i].bits = uint16_t(bf16_pair(f[i], 0.0f));
+      }
+  }
+}
+
+// Sum over the 64 lanes, in a fixed order; every lane receives it.
+__device__ __forceinline__ float wave_sum_f32(float v) {
+  v += u32_as_f32(dpp_u32<kDppQuadSwap1>(f32_as_u32(v)));
+  v += u32_as_f32(dpp_u32<kDppQuadSwap2>(f32_as_u32(v)));
+  v += u32_as_f32(dpp_u32<kDppRowHalfMirror>(f32_as_u32(v)));
+  v += u32_as_f32(dpp_u32<kDppRowMirror>(f32_as_u32(v)));
+  const float r0 = u32_as_f32(__builtin_amdgcn_readlane(f32_as_u32(v), 0));
+  const float r1 = u32_as_f32(__builtin_amdgcn_readlane(f32_as_u32(v), 16));
+  const float r2 = u32_as_f32(__builtin_amdgcn_readlane(f32_as_u32(v), 32));
+  const float r3 = u32_as_f32(__builtin_amdgcn_readlane(f32_as_u32(v), 48));
+  return (r0 + r1) + (r2 + r3);
+}
+
+// Maximum over 16 or 32 neighbouring lanes; every one of them receives it.
+template <int LANES>
+__device__ __forceinline__ float group_max(float v) {
+  static_assert(LANES == 16 || LANES == 32, "a row of lanes, or two");
+  v = fmaxf(v, u32_as_f32(dpp_u32<kDppQuadSwap1>(f32_as_u32(v))));
+  v = fmaxf(v, u32_as_f32(dpp_u32<kDppQuadSwap2>(f32_as_u32(v))));
+  v = fmaxf(v, u32_as_f32(dpp_u32<kDppRowHalfMirror>(f32_as_u32(v))));
+  v = fmaxf(v, u32_as_f32(dpp_u32<kDppRowMirror>(f32_as_u32(v))));
+  if constexpr (LANES == 32) v = fmaxf(v, __shfl_xor(v, 16, kWave));
+  return v;
+}
+
+// The exponent of a block's scale from its largest magnitude c: the smallest e >= kMinExponent with c <= 1.75 * 2^(top + e),
+// top = 8 (E4M3, whose largest value is 448) or 15 (E5M2, 57344).  c's exponent field less top, and one more where
+// its fraction is over .75: no rounding.  (A denormal c has the field 0 and ends at kMinExponent like all that small.)
+__device__ __forceinline__ int block_exponent(float c, int code) {
+  const uint32_t b = f32_as_u32(c);
+  const int e = int(b >> 23) - 127 - (code == ACCEPT_E5M2 ? 15 : 8) + ((b & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+  return e < kMinExponent ? kMinExponent : e;
+}
+// 2^-e
+__device__ __forceinline__ float inverse_scale(int e) { return u32_as_f32(uint32_t(127 - e) << 23); }
+
+// Four values to four codes, the first in the low byte: the conversion instructions round to nearest even, and nothing here is
+// beyond the largest code but infinities and NaN (E4M3: NaN; E5M2: themselves).
+__device__ __forceinline__ uint32_t four_codes(float a, float b, float c, float d, int code) {
+  int r = 0;
+  if (code == ACCEPT_E5M2) {
+    r = __builtin_amdgcn_cvt_pk_bf8_f32(a, b, r, false);
+    r = __builtin_amdgcn_cvt_pk_bf8_f32(c, d, r, true);
+  } else {
+    r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, r, false);
+    r = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
+  }
+  return uint32_t(r);
+}
+
+#endif  // __HIPCC__
+
+}  // namespace accept
