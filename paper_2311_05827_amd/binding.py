@@ -88,6 +88,7 @@ except ImportError as e:    # not built, or for another PyTorch: ctypes serves e
 
     class _native:
         compress = decompress = staticmethod(lambda *args: -1)
+        layer_norm = layer_norm_quantize = layer_norm_backward = block_quantize = block_matmul = compress
 
 
 def status_string(status):

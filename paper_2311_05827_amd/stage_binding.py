@@ -2,7 +2,8 @@
 
 Argument marshalling only, as in binding.py: tensors are checked on the host against the descriptor, outputs that are not
 given are allocated with ``torch.empty``, and the kernels run on the current stream of the current device, where the tensors
-have to be.  Codes are ``torch.float8_e4m3fn`` or ``torch.float8_e5m2``, scales ``torch.float8_e8m0fnu``.
+have to be.  csrc/native.cpp makes the same checks and calls without the interpreter; whatever it does not take comes to
+the code here, which says what is wrong.  Codes are ``torch.float8_e4m3fn`` or ``torch.float8_e5m2``, scales ``torch.float8_e8m0fnu``.
 """
 from __future__ import annotations
 
@@ -62,6 +63,7 @@ def _declare(lib):
 
 
 lib = _declare(B.lib)
+_native = B._native
 
 
 # ------------------------------------------------------------------------------- descriptors
@@ -142,6 +144,15 @@ def _check_flat(t, where, what, dtype, elems):
         _refuse(where, what, "is not contiguous")
 
 
+def _check_table(t, where, what, dtype, rows, cols):
+    """(rows, cols), contiguous: in another order they would be read as another's."""
+    _check_place(t, where, what, dtype)
+    if tuple(t.shape) != (rows, cols):
+        _refuse(where, what, "is %s, %s needed" % (tuple(t.shape), (rows, cols)))
+    if not t.is_contiguous():
+        _refuse(where, what, "is not contiguous")
+
+
 def _check_codes(t, where, what, dtype, rows, cols, stride):
     """(rows, cols) codes, rows `stride` bytes apart (one row: any) and readable up to a multiple of 16."""
     _check_place(t, where, what, dtype)
@@ -192,6 +203,12 @@ def accept_layer_norm(desc, x, weight=None, bias=None, y=None, stats=None):
     """Enqueue a layer norm of x's rows on the current stream; returns (y, stats).  y has x's shape, or is (rows, cols)
     where its rows are further apart; stats (2, rows) float32 are the means and reciprocal deviations that the backward
     pass takes."""
+    if type(desc) is NormDesc:
+        got = _native.layer_norm(desc, x, weight, bias, y, stats)
+        if type(got) is tuple:
+            return got
+        if got > 0:
+            raise B.AcceptError(got, "accept_layer_norm")
     where = "accept_layer_norm"
     _check_norm_inputs(where, desc, x, weight, bias)
     if y is None:
@@ -202,7 +219,7 @@ def accept_layer_norm(desc, x, weight=None, bias=None, y=None, stats=None):
     if stats is None:
         stats = _empty((2, desc.rows), torch.float32, x.device)
     _check_matrix(y, where, "y", B._DTYPES[desc.y_dtype], desc.rows, desc.cols, desc.y_stride)
-    _check_flat(stats, where, "stats", torch.float32, 2 * desc.rows)
+    _check_table(stats, where, "stats", torch.float32, 2, desc.rows)
     B._check(lib.accept_layer_norm(ctypes.byref(desc), B._ptr(x), B._ptr(weight), B._ptr(bias), B._ptr(y), B._ptr(stats),
                                    B._stream_handle()), where)
     return y, stats
@@ -211,6 +228,12 @@ def accept_layer_norm(desc, x, weight=None, bias=None, y=None, stats=None):
 def accept_layer_norm_quantize(desc, x, weight=None, bias=None, codes=None, scales=None, stats=None):
     """The same with y as codes (rows, cols) and scales (blocks of columns, rows), as accept_block_quantize makes them
     from the float32 y; returns (codes, scales, stats)."""
+    if type(desc) is NormDesc:
+        got = _native.layer_norm_quantize(desc, x, weight, bias, codes, scales, stats)
+        if type(got) is tuple:
+            return got
+        if got > 0:
+            raise B.AcceptError(got, "accept_layer_norm_quantize")
     where = "accept_layer_norm_quantize"
     _check_norm_inputs(where, desc, x, weight, bias)
     if codes is None:
@@ -220,8 +243,8 @@ def accept_layer_norm_quantize(desc, x, weight=None, bias=None, codes=None, scal
     if stats is None:
         stats = _empty((2, desc.rows), torch.float32, x.device)
     _check_out_codes(codes, where, "codes", _CODE_TYPES[desc.code], desc.rows, desc.cols)
-    _check_flat(scales, where, "scales", _SCALE_TYPE, _blocks(desc.cols) * desc.rows)
-    _check_flat(stats, where, "stats", torch.float32, 2 * desc.rows)
+    _check_table(scales, where, "scales", _SCALE_TYPE, _blocks(desc.cols), desc.rows)
+    _check_table(stats, where, "stats", torch.float32, 2, desc.rows)
     B._check(lib.accept_layer_norm_quantize(ctypes.byref(desc), B._ptr(x), B._ptr(weight), B._ptr(bias), B._ptr(codes),
                                             B._ptr(scales), B._ptr(stats), B._stream_handle()), where)
     return codes, scales, stats
@@ -230,10 +253,16 @@ def accept_layer_norm_quantize(desc, x, weight=None, bias=None, codes=None, scal
 def accept_layer_norm_backward(desc, dy, x, weight, stats, dx=None, dweight=None, dbias=None, need_weight=True, need_bias=True,
                                workspace=None):
     """Gradients of accept_layer_norm: (dx, dweight, dbias); None where need_weight or need_bias is false.  weight None: ones."""
+    if type(desc) is NormDesc:
+        got = _native.layer_norm_backward(desc, dy, x, weight, stats, dx, dweight, dbias, need_weight, need_bias, workspace)
+        if type(got) is tuple:
+            return got
+        if got > 0:
+            raise B.AcceptError(got, "accept_layer_norm_backward")
     where = "accept_layer_norm_backward"
     _check_norm_inputs(where, desc, x, weight, None)
     _check_matrix(dy, where, "dy", B._DTYPES[desc.y_dtype], desc.rows, desc.cols, desc.y_stride)
-    _check_flat(stats, where, "stats", torch.float32, 2 * desc.rows)
+    _check_table(stats, where, "stats", torch.float32, 2, desc.rows)
     if dx is None:
         if desc.dx_stride in (0, desc.cols):
             dx = _empty(x.shape, x.dtype, x.device)
@@ -270,6 +299,12 @@ def accept_block_quantize(desc, x, rowwise=True, colwise=False, codes=None, scal
     Returns (codes, scales, codes_t, scales_t), None for what is not wanted.  codes: (rows, cols), scales: (blocks of 128
     columns, rows, or blocks of 128 rows for group 128); codes_t: (cols, rows), scales_t: (blocks of rows, columns or blocks
     of columns)."""
+    if type(desc) is BlockDesc:
+        got = _native.block_quantize(desc, x, rowwise, colwise, codes, scales, codes_t, scales_t)
+        if type(got) is tuple:
+            return got
+        if got > 0:
+            raise B.AcceptError(got, "accept_block_quantize")
     where = "accept_block_quantize"
     _check_desc(desc, BlockDesc, where)
     if (desc.in_dtype not in (B.F32, B.BF16) or desc.code not in (E4M3, E5M2) or desc.group not in (1, BLOCK) or desc.rows < 0
@@ -284,14 +319,14 @@ def accept_block_quantize(desc, x, rowwise=True, colwise=False, codes=None, scal
         codes = _empty_codes(rows, cols, code, x.device) if codes is None else codes
         scales = _empty((_blocks(cols), -(-rows // group)), _SCALE_TYPE, x.device) if scales is None else scales
         _check_out_codes(codes, where, "codes", code, rows, cols)
-        _check_flat(scales, where, "scales", _SCALE_TYPE, _blocks(cols) * -(-rows // group))
+        _check_table(scales, where, "scales", _SCALE_TYPE, _blocks(cols), -(-rows // group))
     else:
         codes = scales = None
     if colwise:
         codes_t = _empty_codes(cols, rows, code, x.device) if codes_t is None else codes_t
         scales_t = _empty((_blocks(rows), -(-cols // group)), _SCALE_TYPE, x.device) if scales_t is None else scales_t
         _check_out_codes(codes_t, where, "codes_t", code, cols, rows)
-        _check_flat(scales_t, where, "scales_t", _SCALE_TYPE, _blocks(rows) * -(-cols // group))
+        _check_table(scales_t, where, "scales_t", _SCALE_TYPE, _blocks(rows), -(-cols // group))
     else:
         codes_t = scales_t = None
     B._check(lib.accept_block_quantize(ctypes.byref(desc), B._ptr(x), B._ptr(codes), B._ptr(scales), B._ptr(codes_t),
@@ -301,6 +336,12 @@ def accept_block_quantize(desc, x, rowwise=True, colwise=False, codes=None, scal
 
 def accept_block_matmul(desc, a, a_scales, b, b_scales, y=None, workspace=None):
     """y = a b^T of codes and scales (see accept_block_quantize), a (m, k), b (n, k); returns y (m, n)."""
+    if type(desc) is MatmulDesc:
+        got = _native.block_matmul(desc, a, a_scales, b, b_scales, y, workspace)
+        if type(got) is tuple:
+            return got[0]
+        if got > 0:
+            raise B.AcceptError(got, "accept_block_matmul")
     where = "accept_block_matmul"
     _check_desc(desc, MatmulDesc, where)
     nbytes = accept_matmul_workspace_size(desc)  # raises on a bad descriptor
@@ -308,8 +349,8 @@ def accept_block_matmul(desc, a, a_scales, b, b_scales, y=None, workspace=None):
     whole = accept_block_stride(k)
     _check_codes(a, where, "a", _CODE_TYPES[desc.a_code], m, k, desc.a_stride or whole)
     _check_codes(b, where, "b", _CODE_TYPES[desc.b_code], n, k, desc.b_stride or whole)
-    _check_flat(a_scales, where, "a_scales", _SCALE_TYPE, _blocks(k) * -(-m // desc.a_group))
-    _check_flat(b_scales, where, "b_scales", _SCALE_TYPE, _blocks(k) * -(-n // desc.b_group))
+    _check_table(a_scales, where, "a_scales", _SCALE_TYPE, _blocks(k), -(-m // desc.a_group))
+    _check_table(b_scales, where, "b_scales", _SCALE_TYPE, _blocks(k), -(-n // desc.b_group))
     out = B._DTYPES[desc.out_dtype]
     if y is None:
         y = _empty((m, n), out, a.device) if desc.y_stride in (0, n) else _empty((m, desc.y_stride), out, a.device)[:, :n]
