@@ -25,7 +25,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const BlockArgs a) {
   for (int64_t block = blockIdx.y; block < a.col_blocks; block += gridDim.y) {
     const int64_t col = block * kQBlock + threadIdx.x % LANES * VEC;
     float f[VEC], c = 0.0f;
-    widen(load_raw(static_cast<const T*>(a.x) + row * a.x_stride + col, a.cols - col), f);
+    load_short(static_cast<const T*>(a.x) + row * a.x_stride, col, a.cols, f);
 #pragma unroll
     for (int j = 0; j < VEC; ++j) c = fmaxf(c, fabsf(f[j]));
     const int e = block_exponent(group_max<LANES>(c), a.code);
@@ -52,20 +52,30 @@ __global__ __launch_bounds__(256) void quantize_square_kernel(const BlockArgs a)
   const int64_t rb = blockIdx.x / a.col_blocks, cb = blockIdx.x % a.col_blocks;
   const int64_t row0 = rb * kQBlock + 8 * ry, col0 = cb * kQBlock + 8 * cx;
   float f[8][8];
+  if (a.cols >= 8) {  // the same in all lanes
+    const int64_t at = col0 < a.cols - 8 ? col0 : a.cols - 8;
+    Raw<T, 8> raw[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const T* const p = static_cast<const T*>(a.x) + (row0 + i) * a.x_stride + col0;
-    const int64_t left = row0 + i < a.rows ? a.cols - col0 : 0;
-    if constexpr (Elem<T>::VEC == 8) {
-      widen(load_raw(p, left), f[i]);
-    } else {
-      float lo[4], hi[4];
-      widen(load_raw(p, left), lo);
-      widen(load_raw(p + 4, left - 4), hi);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) f[i][j] = lo[j], f[i][4 + j] = hi[j];
+    for (int i = 0; i < 8; ++i) {
+      const int64_t row = row0 + i < a.rows ? row0 + i : a.rows - 1;
+      raw[i] = load_values<T, 8>(static_cast<const T*>(a.x) + row * a.x_stride, at);
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      widened(raw[i], f[i]);
+      moved_up(f[i], col0 - at);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      load_short(static_cast<const T*>(a.x) + (row0 + i < a.rows ? row0 + i : a.rows - 1) * a.x_stride, col0, a.cols, f[i]);
   }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (row0 + i >= a.rows) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[i][j] = 0.0f;
+    }
   float inv_square = 0.0f;
   if constexpr (GROUP == kQBlock) {
     float c = 0.0f;

@@ -344,7 +344,7 @@ __global__ __launch_bounds__(256) void matmul_join_kernel(const float* parts, in
     float sum[4] = {0, 0, 0, 0};
     for (int s = 0; s < splits; ++s) {
       float f[4];
-      widen(load_raw(parts + s * total + at, total - at), f);
+      load_short(parts + s * total, at, total, f);
 #pragma unroll
       for (int j = 0; j < 4; ++j) sum[j] += f[j];
     }

@@ -30,54 +30,28 @@ struct NormBackArgs {
   int param_bf16;
 };
 
-template <typename T>
-__device__ __forceinline__ void widen_raw(const uint4 r, float (&f)[Elem<T>::VEC]) { widen(r, f); }
-
-// N values of any element alignment, widened; zeros from `left` on.
-template <typename T, int N>
-__device__ __forceinline__ void load_values(const T* p, int64_t left, float (&f)[N]) {
-  constexpr int VEC = Elem<T>::VEC;
-  if constexpr (N >= VEC) {
-#pragma unroll
-    for (int i = 0; i < N; i += VEC) {
-      float part[VEC];
-      widen(load_raw(p + i, left - i), part);
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) f[i + j] = part[j];
-    }
-  } else {  // half a vector of bfloat16
-    typedef uint32_t v2u_elem_t __attribute__((ext_vector_type(2), aligned(2)));
-    uint32_t w[2] = {0, 0};
-    if (left >= N) {
-      const v2u_elem_t v = *reinterpret_cast<const v2u_elem_t*>(p);
-      w[0] = v.x;
-      w[1] = v.y;
-    } else if (left > 0) {
-#pragma unroll
-      for (int j = 0; j < N - 1; ++j)
-        if (j < left) w[j / 2] |= uint32_t(p[j].bits) << (16 * (j & 1));
-    }
-    f[0] = u32_as_f32(w[0] << 16); f[1] = u32_as_f32(w[0] & 0xFFFF0000u);
-    f[2] = u32_as_f32(w[1] << 16); f[3] = u32_as_f32(w[1] & 0xFFFF0000u);
-  }
-}
-
-// VEC parameters from column `col` on; `none` where there are no parameters, 0 behind the last column.
-template <int VEC>
-__device__ __forceinline__ void load_param(const void* p, int bf16, int64_t col, int64_t cols, float none, float (&f)[VEC]) {
-#pragma unroll
-  for (int j = 0; j < VEC; ++j) f[j] = 0.0f;
+// N parameters from column `at` on; `none` where there are no parameters.
+template <int N, typename Col>
+__device__ __forceinline__ void load_param(const void* p, int bf16, Col at, float none, float (&f)[N]) {
   if (!p) {
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) f[j] = none;
+    for (int j = 0; j < N; ++j) f[j] = none;
   } else if (bf16) {
-#pragma unroll
-    for (int j = 0; j < VEC; ++j)
-      if (col + j < cols) f[j] = load_one(static_cast<const bf16_t*>(p) + col + j);
+    widened(load_values<bf16_t, N>(static_cast<const bf16_t*>(p), at), f);
   } else {
+    widened(load_values<float, N>(static_cast<const float*>(p), at), f);
+  }
+}
+// The same lane by lane, 0 behind the last column.
+template <int N>
+__device__ __forceinline__ void load_param_short(const void* p, int bf16, int64_t col, int64_t cols, float none, float (&f)[N]) {
+  if (!p) {
 #pragma unroll
-    for (int j = 0; j < VEC; ++j)
-      if (col + j < cols) f[j] = static_cast<const float*>(p)[col + j];
+    for (int j = 0; j < N; ++j) f[j] = none;
+  } else if (bf16) {
+    load_short(static_cast<const bf16_t*>(p), col, cols, f);
+  } else {
+    load_short(static_cast<const float*>(p), col, cols, f);
   }
 }
 
@@ -99,76 +73,91 @@ __device__ __forceinline__ float row_sum(float v, float* slots) {
   }
 }
 
-// y of one vector of a row, written as values or as codes.
-template <typename TY, int VEC>
-__device__ __forceinline__ void put(const NormArgs& a, int64_t row, int64_t col, const float (&y)[VEC]) {
-  if constexpr (__is_same(TY, Codes)) {
-    const int64_t stride = a.y_stride;  // whole blocks
-    float c = 0.0f;
+// y of the vector of a row at `col`, zeros behind the last column, as codes.
+template <int VEC, typename Col>
+__device__ __forceinline__ void put_codes(const NormArgs& a, int64_t row, Col col, const float (&y)[VEC]) {
+  float c = 0.0f;
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) c = fmaxf(c, fabsf(y[j]));
-    constexpr int LANES = kQBlock / VEC;
-    c = group_max<LANES>(c);
-    const int e = block_exponent(c, a.code);
-    const float inv = inverse_scale(e);
-    if (col < stride) {
-      uint8_t* const to = static_cast<uint8_t*>(a.y) + row * stride + col;
-      const uint32_t lo = four_codes(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv, a.code);
-      if constexpr (VEC == 8) {
-        const uint32_t hi = four_codes(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv, a.code);
-        *reinterpret_cast<uint2*>(to) = make_uint2(lo, hi);
-      } else {
-        *reinterpret_cast<uint32_t*>(to) = lo;
-      }
-      if (col % kQBlock == 0) a.scales[col / kQBlock * a.rows + row] = uint8_t(e + 127);
+  for (int j = 0; j < VEC; ++j) c = fmaxf(c, fabsf(y[j]));
+  constexpr int LANES = kQBlock / VEC;
+  c = group_max<LANES>(c);
+  const int e = block_exponent(c, a.code);
+  const float inv = inverse_scale(e);
+  if (col < a.y_stride) {  // whole blocks
+    uint8_t* const to = static_cast<uint8_t*>(a.y) + row * a.y_stride + col;
+    const uint32_t lo = four_codes(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv, a.code);
+    if constexpr (VEC == 8) {
+      const uint32_t hi = four_codes(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv, a.code);
+      *reinterpret_cast<uint2*>(to) = make_uint2(lo, hi);
+    } else {
+      *reinterpret_cast<uint32_t*>(to) = lo;
     }
-  } else {
-    store_values(static_cast<TY*>(a.y) + row * a.y_stride + col, y, a.cols - col);
+    if (col % kQBlock == 0) a.scales[col / kQBlock * a.rows + row] = uint8_t(e + 127);
   }
 }
 
-// One row at a time per WAVES wavefronts, C vectors of it in a lane's registers: x is read once, the variance is that of the
-// differences.  Bound by memory.
+// Where a lane's vector of a row begins: at `col`, or, where the row ends before, so that it ends with the row.  Its
+// first `over` columns are then the neighbour's too (all of them where the row ends before `col`): they count in no sum of the row, and
+// what both write there is the same.  So no lane reads or writes a vector in pieces.  (Lane by lane and value by value, 1531 rows of
+// 5003 bfloat16 took 15.3 us where they now take 9.2.)
+struct Place {
+  int at, over;
+};
+template <int VEC>
+__device__ __forceinline__ Place place_of(int col, int cols) {
+  const int at = col < cols - VEC ? col : cols - VEC;
+  return {at, col - at};
+}
+
+// One row at a time per WAVES wavefronts, C vectors of it in a lane's registers and the next row's on their way: x is read
+// once, the variance is that of the differences.  Bound by memory.
 template <typename TX, typename TY, int WAVES, int C>
 __global__ __launch_bounds__(WAVES == 8 ? 512 : 256) void norm_kernel(const NormArgs a) {
   constexpr int VEC = Elem<TX>::VEC;
   constexpr int kRows = WAVES == 1 ? 4 : 1;  // rows of a workgroup at a time
   __shared__ float slots[2][2][WAVES];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const int64_t first_col = int64_t((WAVES == 1 ? 0 : wave) * kWave + lane) * VEC;
-  constexpr int64_t kColStep = int64_t(WAVES) * kWave * VEC;
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int cols = int(a.cols), first_col = ((WAVES == 1 ? 0 : wave) * kWave + lane) * VEC;
+  constexpr int kColStep = WAVES * kWave * VEC;
+  const int64_t step = int64_t(gridDim.x) * kRows;
+  int64_t row = int64_t(blockIdx.x) * kRows + (WAVES == 1 ? wave : 0);
+  Place place[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) place[c] = place_of<VEC>(first_col + c * kColStep, cols);
+  Raw<TX, VEC> next[C];
+  auto fetch = [&](int64_t r) {
+    const TX* const x = static_cast<const TX*>(a.x) + r * a.x_stride;
+#pragma unroll
+    for (int c = 0; c < C; ++c) next[c] = load_values<TX, VEC>(x, place[c].at);
+  };
+  if (row < a.rows) fetch(row);
   float w[C][VEC], b[C][VEC];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    load_param(a.weight, a.param_bf16, first_col + c * kColStep, a.cols, 1.0f, w[c]);
-    load_param(a.bias, a.param_bf16, first_col + c * kColStep, a.cols, 0.0f, b[c]);
+    load_param(a.weight, a.param_bf16, place[c].at, 1.0f, w[c]);
+    load_param(a.bias, a.param_bf16, place[c].at, 0.0f, b[c]);
   }
   int parity = 0;
-  for (int64_t row = int64_t(blockIdx.x) * kRows + (WAVES == 1 ? wave : 0); row < a.rows; row += int64_t(gridDim.x) * kRows) {
-    const TX* const x = static_cast<const TX*>(a.x) + row * a.x_stride;
+  for (; row < a.rows; row += step) {
     float f[C][VEC];
     float sum = 0.0f;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int64_t col = first_col + c * kColStep;
-      widen_raw<TX>(load_raw(x + col, a.cols - col), f[c]);
-    }
+    for (int c = 0; c < C; ++c) widened(next[c], f[c]);
+    if (row + step < a.rows) fetch(row + step);
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) sum += f[c][j];
+      for (int j = 0; j < VEC; ++j) sum += j < place[c].over ? 0.0f : f[c][j];
     const float mean = row_sum<WAVES>(sum, slots[parity][0]) * a.inv_cols;
     float square = 0.0f;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int64_t col = first_col + c * kColStep;
+    for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        const float d = col + j < a.cols ? f[c][j] - mean : 0.0f;
-        f[c][j] = d;
+        f[c][j] -= mean;
+        const float d = j < place[c].over ? 0.0f : f[c][j];
         square = fmaf(d, d, square);
       }
-    }
     const float rstd = 1.0f / sqrtf(row_sum<WAVES>(square, slots[parity][1]) * a.inv_cols + a.eps);
     parity ^= 1;
     if (a.stats && lane == 0 && (WAVES == 1 || wave == 0)) {
@@ -177,42 +166,46 @@ __global__ __launch_bounds__(WAVES == 8 ? 512 : 256) void norm_kernel(const Norm
     }
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int64_t col = first_col + c * kColStep;
       float y[VEC];
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) y[j] = col + j < a.cols ? fmaf(f[c][j] * rstd, w[c][j], b[c][j]) : 0.0f;
-      put<TY>(a, row, col, y);
+      for (int j = 0; j < VEC; ++j) y[j] = fmaf(f[c][j] * rstd, w[c][j], b[c][j]);
+      if constexpr (__is_same(TY, Codes)) {
+        // a block's lanes hold its columns in order: back to where `col` is, zeros behind the last one
+        moved_up(y, place[c].over);
+        put_codes(a, row, first_col + c * kColStep, y);
+      } else {
+        store_some<TY, VEC>(static_cast<TY*>(a.y) + row * a.y_stride + place[c].at, y);
+      }
     }
   }
 }
 
-// Rows longer than a workgroup's registers hold: read three times, from the caches the second and third.
+// Rows longer than a workgroup's registers hold, or shorter than a vector: read three times, from the caches the second and third.
 template <typename TX, typename TY>
 __global__ __launch_bounds__(1024) void norm_long_kernel(const NormArgs a) {
   constexpr int VEC = Elem<TX>::VEC, WAVES = 16;
   __shared__ float slots[2][2][WAVES];
   int parity = 0;
-  const int64_t end = __is_same(TY, Codes) ? a.y_stride : a.cols;
+  const int64_t cols = a.cols, end = __is_same(TY, Codes) ? a.y_stride : a.cols;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const TX* const x = static_cast<const TX*>(a.x) + row * a.x_stride;
     constexpr int64_t kStep = 1024 * VEC;
     float f[VEC], sum = 0.0f, square = 0.0f;
-    for (int64_t col = int64_t(threadIdx.x) * VEC; col < a.cols; col += kStep) {
-      widen_raw<TX>(load_raw(x + col, a.cols - col), f);
+    for (int64_t col = int64_t(threadIdx.x) * VEC; col < cols; col += kStep) {
+      load_short(x, col, cols, f);
       float part = 0.0f;
 #pragma unroll
       for (int j = 0; j < VEC; ++j) part += f[j];
       sum += part;
     }
     const float mean = row_sum<WAVES>(sum, slots[parity][0]) * a.inv_cols;
-    for (int64_t col = int64_t(threadIdx.x) * VEC; col < a.cols; col += kStep) {
-      widen_raw<TX>(load_raw(x + col, a.cols - col), f);
+    for (int64_t col = int64_t(threadIdx.x) * VEC; col < cols; col += kStep) {
+      load_short(x, col, cols, f);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) f[j] -= mean;
       float part = 0.0f;
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        const float d = col + j < a.cols ? f[j] - mean : 0.0f;
-        part = fmaf(d, d, part);
-      }
+      for (int j = 0; j < VEC; ++j) part = col + j < cols ? fmaf(f[j], f[j], part) : part;
       square += part;
     }
     const float rstd = 1.0f / sqrtf(row_sum<WAVES>(square, slots[parity][1]) * a.inv_cols + a.eps);
@@ -225,62 +218,70 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const NormArgs a) {
     for (int64_t base = 0; base < end; base += kStep) {
       const int64_t col = base + int64_t(threadIdx.x) * VEC;
       float w[VEC], b[VEC], y[VEC];
-      widen_raw<TX>(load_raw(x + col, a.cols - col), f);
-      load_param(a.weight, a.param_bf16, col, a.cols, 1.0f, w);
-      load_param(a.bias, a.param_bf16, col, a.cols, 0.0f, b);
+      load_short(x, col, cols, f);
+      load_param_short(a.weight, a.param_bf16, col, cols, 1.0f, w);
+      load_param_short(a.bias, a.param_bf16, col, cols, 0.0f, b);
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) y[j] = col + j < a.cols ? fmaf((f[j] - mean) * rstd, w[j], b[j]) : 0.0f;
-      put<TY>(a, row, col, y);
+      for (int j = 0; j < VEC; ++j) y[j] = col + j < cols ? fmaf((f[j] - mean) * rstd, w[j], b[j]) : 0.0f;
+      if constexpr (__is_same(TY, Codes)) put_codes(a, row, col, y);
+      else store_values(static_cast<TY*>(a.y) + row * a.y_stride + col, y, cols - col);
     }
   }
 }
 
 // Backward: rows as in norm_kernel, with the two row sums that dx needs; every lane sums its columns' dy*h and dy over the rows
 // that it meets, and the workgroup leaves these sums for join_kernel.  One read of x and dy.
+// (Rows of a workgroup at a time: 16 wavefronts where their 128 registers do for one's vectors, so that there are few partial sums.)
+constexpr int back_rows(int vec, int waves, int c) { return waves != 1 ? 1 : vec == 4 && c == 4 ? 8 : 16; }
+constexpr int back_threads(int vec, int waves, int c) { return back_rows(vec, waves, c) * waves * kWave; }
 template <typename TX, typename TY, int WAVES, int C>
-__global__ __launch_bounds__(WAVES == 8 ? 512 : 256) void norm_back_kernel(const NormBackArgs a) {
+__global__ __launch_bounds__(back_threads(Elem<TX>::VEC, WAVES, C)) void norm_back_kernel(const NormBackArgs a) {
   constexpr int VEC = Elem<TX>::VEC;
-  constexpr int kRows = WAVES == 1 ? 4 : 1;
+  constexpr int kRows = back_rows(VEC, WAVES, C);
   __shared__ float slots[2][2][WAVES];
-  __shared__ float joined[WAVES == 1 ? 3 * kWave * VEC * C : 1];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const int64_t first_col = int64_t((WAVES == 1 ? 0 : wave) * kWave + lane) * VEC;
-  constexpr int64_t kColStep = int64_t(WAVES) * kWave * VEC;
+  __shared__ float joined[WAVES == 1 ? kRows : 1][2 * C * VEC][WAVES == 1 ? kWave : 1];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int cols = int(a.cols), first_col = ((WAVES == 1 ? 0 : wave) * kWave + lane) * VEC;
+  constexpr int kColStep = WAVES * kWave * VEC;
+  const int64_t step = int64_t(gridDim.x) * kRows;
+  int64_t row = int64_t(blockIdx.x) * kRows + (WAVES == 1 ? wave : 0);
+  Place place[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) place[c] = place_of<VEC>(first_col + c * kColStep, cols);
   float w[C][VEC], dw[C][VEC], db[C][VEC];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    load_param(a.weight, a.param_bf16, first_col + c * kColStep, a.cols, 1.0f, w[c]);
+    load_param(a.weight, a.param_bf16, place[c].at, 1.0f, w[c]);
 #pragma unroll
     for (int j = 0; j < VEC; ++j) dw[c][j] = db[c][j] = 0.0f;
   }
   int parity = 0;
-  for (int64_t row = int64_t(blockIdx.x) * kRows + (WAVES == 1 ? wave : 0); row < a.rows; row += int64_t(gridDim.x) * kRows) {
-    const TX* const x = static_cast<const TX*>(a.x) + row * a.x_stride;
-    const TY* const dy = static_cast<const TY*>(a.dy) + row * a.dy_stride;
+  for (; row < a.rows; row += step) {
+    const TX* const x_row = static_cast<const TX*>(a.x) + row * a.x_stride;
+    const TY* const dy_row = static_cast<const TY*>(a.dy) + row * a.dy_stride;
+    Raw<TX, VEC> raw_x[C];
+    Raw<TY, VEC> raw_dy[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      raw_x[c] = load_values<TX, VEC>(x_row, place[c].at);
+      raw_dy[c] = load_values<TY, VEC>(dy_row, place[c].at);
+    }
     const float mean = a.stats[row], rstd = a.stats[a.rows + row];
-    float h[C][VEC], g[C][VEC];
     float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int64_t col = first_col + c * kColStep;
-      widen_raw<TX>(load_raw(x + col, a.cols - col), h[c]);
-      load_values(dy + col, a.cols - col, g[c]);
-    }
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int64_t col = first_col + c * kColStep;
+      float x[VEC], d[VEC];
+      widened(raw_x[c], x);
+      widened(raw_dy[c], d);
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        const float hh = col + j < a.cols ? (h[c][j] - mean) * rstd : 0.0f;
-        const float d = g[c][j];
-        dw[c][j] = fmaf(d, hh, dw[c][j]);
-        db[c][j] += d;
-        const float gg = d * w[c][j];
-        h[c][j] = hh;
-        g[c][j] = gg;
-        s1 += gg;
-        s2 = fmaf(gg, hh, s2);
+        const float h = (x[j] - mean) * rstd, g = d[j] * w[c][j];
+        dw[c][j] = fmaf(d[j], h, dw[c][j]);
+        db[c][j] += d[j];
+        s1 += j < place[c].over ? 0.0f : g;
+        s2 = j < place[c].over ? s2 : fmaf(g, h, s2);
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
     const float m1 = row_sum<WAVES>(s1, slots[parity][0]) * a.inv_cols;
     const float m2 = row_sum<WAVES>(s2, slots[parity][1]) * a.inv_cols;
@@ -288,50 +289,50 @@ __global__ __launch_bounds__(WAVES == 8 ? 512 : 256) void norm_back_kernel(const
     TX* const dx = static_cast<TX*>(a.dx) + row * a.dx_stride;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int64_t col = first_col + c * kColStep;
-      float o[VEC];
+      // h and g once more, from what was loaded: held from above they would take a register for every value
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) o[j] = rstd * (g[c][j] - m1 - h[c][j] * m2);
-      store_values(dx + col, o, a.cols - col);
+      for (uint32_t& v : raw_x[c].w) asm("" : "+v"(v));
+#pragma unroll
+      for (uint32_t& v : raw_dy[c].w) asm("" : "+v"(v));
+      float x[VEC], d[VEC];
+      widened(raw_x[c], x);
+      widened(raw_dy[c], d);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) x[j] = rstd * (d[j] * w[c][j] - m1 - (x[j] - mean) * rstd * m2);
+      store_some<TX, VEC>(dx + place[c].at, x);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
   if (!a.partials) return;
-  float* const to = a.partials + int64_t(blockIdx.x) * 2 * a.cols;
+  float* const to = a.partials + int64_t(blockIdx.x) * 2 * cols;
+  if constexpr (WAVES == 1) {  // the wavefronts had the same columns: each adds up a part of them
+    constexpr int kSums = 2 * C * VEC;
 #pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    if constexpr (WAVES == 1) {  // the four wavefronts had the same columns
-      if (which) __syncthreads();
-      if (wave) {
+    for (int i = 0; i < kSums; ++i) joined[wave][i][lane] = i < C * VEC ? dw[i / VEC % C][i % VEC] : db[i / VEC % C][i % VEC];
+    __syncthreads();
+    for (int i = wave; i < kSums; i += kRows) {
+      const int at = i % (C * VEC);
+      float v = joined[0][i][lane];
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-          for (int j = 0; j < VEC; ++j) joined[((wave - 1) * C * VEC + c * VEC + j) * kWave + lane] = which ? db[c][j] : dw[c][j];
-      }
-      __syncthreads();
-      if (wave) continue;
-#pragma unroll
-      for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          float& v = which ? db[c][j] : dw[c][j];
-#pragma unroll
-          for (int i = 0; i < 3; ++i) v += joined[(i * C * VEC + c * VEC + j) * kWave + lane];
-        }
+      for (int k = 1; k < kRows; ++k) v += joined[k][i][lane];
+      to[i / (C * VEC) * cols + place_of<VEC>(first_col + at / VEC * kColStep, cols).at + at % VEC] = v;
     }
+  } else {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int64_t col = first_col + c * kColStep;
-      store_values(to + which * a.cols + col, which ? db[c] : dw[c], a.cols - col);
+      store_some<float, VEC>(to + place[c].at, dw[c]);
+      store_some<float, VEC>(to + cols + place[c].at, db[c]);
     }
   }
 }
 
-// dx of rows longer than a workgroup's registers hold: two reads.
+// dx of rows longer than a workgroup's registers hold, or shorter than a vector: two reads.
 template <typename TX, typename TY>
 __global__ __launch_bounds__(1024) void norm_back_long_kernel(const NormBackArgs a) {
   constexpr int VEC = Elem<TX>::VEC, WAVES = 16;
   __shared__ float slots[2][2][WAVES];
   int parity = 0;
+  const int64_t cols = a.cols;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const TX* const x = static_cast<const TX*>(a.x) + row * a.x_stride;
     const TY* const dy = static_cast<const TY*>(a.dy) + row * a.dy_stride;
@@ -340,23 +341,21 @@ __global__ __launch_bounds__(1024) void norm_back_long_kernel(const NormBackArgs
     float s1 = 0.0f, s2 = 0.0f, m1 = 0.0f, m2 = 0.0f;
 #pragma unroll 1
     for (int pass = 0; pass < 2; ++pass) {
-      for (int64_t col = int64_t(threadIdx.x) * VEC; col < a.cols; col += 1024 * VEC) {
+      for (int64_t col = int64_t(threadIdx.x) * VEC; col < cols; col += 1024 * VEC) {
         float h[VEC], g[VEC], w[VEC], o[VEC], p1 = 0.0f, p2 = 0.0f;
-        widen_raw<TX>(load_raw(x + col, a.cols - col), h);
-        load_values(dy + col, a.cols - col, g);
-        load_param(a.weight, a.param_bf16, col, a.cols, 1.0f, w);
+        load_short(x, col, cols, h);
+        load_short(dy, col, cols, g);
+        load_param_short(a.weight, a.param_bf16, col, cols, 1.0f, w);
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
           const float hh = (h[j] - mean) * rstd, gg = g[j] * w[j];
-          if (col + j < a.cols) {
-            p1 += gg;
-            p2 = fmaf(gg, hh, p2);
-          }
+          p1 += gg;
+          p2 = fmaf(gg, hh, p2);
           o[j] = rstd * (gg - m1 - hh * m2);
         }
         s1 += p1;
         s2 += p2;
-        if (pass) store_values(dx + col, o, a.cols - col);
+        if (pass) store_values(dx + col, o, cols - col);
       }
       if (!pass) {
         m1 = row_sum<WAVES>(s1, slots[parity][0]) * a.inv_cols;
@@ -374,6 +373,7 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(const NormBackArgs a,
   if (col >= a.cols) return;
   const int64_t from = blockIdx.y * rows_each, to = from + rows_each < a.rows ? from + rows_each : a.rows;
   float dw = 0.0f, db = 0.0f;
+#pragma unroll 4
   for (int64_t row = from; row < to; ++row) {
     const float h = (load_one(static_cast<const TX*>(a.x) + row * a.x_stride + col) - a.stats[row]) * a.stats[a.rows + row];
     const float d = load_one(static_cast<const TY*>(a.dy) + row * a.dy_stride + col);
@@ -394,6 +394,7 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const float* partials, 
   const int64_t col = int64_t(blockIdx.x) * kWave + lane;
   float sum = 0.0f;
   if (col < cols)
+#pragma unroll 16
     for (int r = wave; r < records; r += 16) sum += partials[(int64_t(r) * 2 + blockIdx.y) * cols + col];
   part[wave][lane] = sum;
   __syncthreads();
@@ -411,17 +412,18 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const float* partials, 
 template <typename TX, template <int, int> class Launch, int FLOATS, typename... Args>
 hipError_t by_width(int64_t cols, Args&&... args) {
   constexpr int VEC = Elem<TX>::VEC, F = FLOATS / VEC;
-  const int64_t v = blocks_of(cols, kWave * VEC);  // wavefronts' vectors in a row
+  if (cols < 8) return Launch<0, 0>::run(args...);  // for both types' vectors
+  const int64_t v = blocks_of(cols, kWave * VEC);   // wavefronts' vectors in a row
 #define ACCEPT_WIDTH(WAVES, CC) \
   if constexpr (CC <= F) if (v <= WAVES * CC) return Launch<WAVES, CC>::run(args...);
   ACCEPT_WIDTH(1, 1) ACCEPT_WIDTH(1, 2) ACCEPT_WIDTH(1, 3) ACCEPT_WIDTH(1, 4) ACCEPT_WIDTH(1, 6) ACCEPT_WIDTH(1, 8)
-  ACCEPT_WIDTH(4, 2) ACCEPT_WIDTH(4, 3) ACCEPT_WIDTH(4, 4) ACCEPT_WIDTH(4, 6) ACCEPT_WIDTH(4, 8)
+  ACCEPT_WIDTH(4, 1) ACCEPT_WIDTH(4, 2) ACCEPT_WIDTH(4, 3) ACCEPT_WIDTH(4, 4) ACCEPT_WIDTH(4, 6) ACCEPT_WIDTH(4, 8)
   ACCEPT_WIDTH(8, 2) ACCEPT_WIDTH(8, 3) ACCEPT_WIDTH(8, 4) ACCEPT_WIDTH(8, 6) ACCEPT_WIDTH(8, 8)
 #undef ACCEPT_WIDTH
   return Launch<0, 0>::run(args...);
 }
 
-constexpr int64_t kForwardGrid = 2048;
+constexpr int64_t kForwardGrid = 1024;
 
 template <typename TX, typename TY>
 struct Forward {
@@ -433,7 +435,7 @@ struct Forward {
         norm_long_kernel<TX, TY><<<grid, 1024, 0, s>>>(a);
       } else {
         const int64_t want = blocks_of(a.rows, WAVES == 1 ? 4 : 1);
-        const int grid = int(want < kForwardGrid ? want : kForwardGrid);
+        const int grid = int(blocks_of(want, blocks_of(want, kForwardGrid)));  // all with the same number of turns
         norm_kernel<TX, TY, WAVES, C><<<grid, WAVES == 8 ? 512 : 256, 0, s>>>(a);
       }
       return hipGetLastError();
@@ -447,8 +449,8 @@ hipError_t forward(int x_dtype, const NormArgs& a, hipStream_t s) {
                                : by_width<bf16_t, Forward<bf16_t, TY>::template At, 32>(a.cols, a, s);
 }
 
-constexpr int64_t kBackGrid = 512;
-constexpr int64_t kHeldCols = 8 * kWave * 16;  // longest row of norm_back_kernel
+constexpr int64_t kWaveCols = kWave * 16;      // longest row of norm_back_kernel for one wavefront
+constexpr int64_t kHeldCols = 8 * kWaveCols;  // longest row of norm_back_kernel
 
 template <typename TX, typename TY>
 struct Backward {
@@ -461,7 +463,7 @@ struct Backward {
         if (e != hipSuccess || !a.partials) return e;
         norm_columns_kernel<TX, TY><<<dim3(uint32_t(blocks_of(a.cols, 256)), uint32_t(records)), 256, 0, s>>>(a, blocks_of(a.rows, records));
       } else {
-        norm_back_kernel<TX, TY, WAVES, C><<<records, WAVES == 8 ? 512 : 256, 0, s>>>(a);
+        norm_back_kernel<TX, TY, WAVES, C><<<records, back_threads(Elem<TX>::VEC, WAVES, C), 0, s>>>(a);
       }
       return hipGetLastError();
     }
@@ -493,11 +495,23 @@ NormArgs forward_args(const accept_norm_desc& d, const void* x, const void* weig
 
 }  // namespace
 
+// Workgroups of the backward pass: as many as the chip holds at a time, or fewer, so that their partial sums (8 bytes a column
+// each, written and read) stay small beside the rows that they have.  us of the whole call with 256 / 512 / 768 of them, bfloat16:
+// 4096 x 4096 29.4 / 26.1 / 27.6, 2048 x 8192 26.9 / 29.7 / 37.1, 600 x 8192 16.6 / 20.7 / 24.8.
 NormPlan make_nplan(const accept_norm_desc& d) {
   NormPlan p{};
-  const int64_t units = d.cols > kHeldCols ? blocks_of(d.rows, 64) : blocks_of(d.rows, 4);
-  const int64_t most = d.cols > kHeldCols ? 64 : kBackGrid;
-  p.back_grid = int(units < 1 ? 1 : units < most ? units : most);
+  const bool held = d.cols >= 8 && d.cols <= kHeldCols;
+  int64_t grid;
+  if (!held) {
+    grid = blocks_of(d.rows, 64) < 64 ? blocks_of(d.rows, 64) : 64;
+  } else if (d.cols <= kWaveCols) {
+    grid = blocks_of(d.rows, 16) < 256 ? blocks_of(d.rows, 16) : 256;
+  } else {
+    const int64_t most = d.cols <= 4 * kWaveCols ? 768 : 512, by_rows = d.rows / 8 > 256 ? d.rows / 8 : 256;
+    grid = d.rows < by_rows ? d.rows : by_rows;
+    grid = grid < most ? grid : most;
+  }
+  p.back_grid = int(grid < 1 ? 1 : grid);
   p.bytes = size_t(up_to(int64_t(p.back_grid) * 2 * d.cols * 4, 256));
   return p;
 }

@@ -39,57 +39,107 @@ hipError_t launch_matmul(const accept_matmul_desc& d, const MatmulPlan& p, const
 
 #if defined(__HIPCC__)
 
-// VEC consecutive elements from any element's alignment; the ones from `left` on are zeros and are not read.
-typedef uint32_t v4u_elem_t __attribute__((ext_vector_type(4), aligned(2)));
-typedef uint32_t v4u_word_t __attribute__((ext_vector_type(4), aligned(4)));
-template <typename T>
-__device__ __forceinline__ uint4 load_raw(const T* p, int64_t left) {
-  constexpr int VEC = Elem<T>::VEC;
-  uint4 r = make_uint4(0, 0, 0, 0);
-  if (left >= VEC) {
-    if constexpr (VEC == 4) {
-      const v4u_word_t v = *reinterpret_cast<const v4u_word_t*>(p);
-      r = make_uint4(v.x, v.y, v.z, v.w);
-    } else {
-      const v4u_elem_t v = *reinterpret_cast<const v4u_elem_t*>(p);
-      r = make_uint4(v.x, v.y, v.z, v.w);
-    }
-  } else if (left > 0) {
-    uint32_t w[4] = {0, 0, 0, 0};
+// N consecutive values of a row, as they lie in memory.
+template <typename T, int N>
+struct Raw {
+  static constexpr int kWords = N * int(sizeof(T)) / 4;
+  uint32_t w[kWords];
+};
+
+// Values at .. at+N-1 of a row, from any element's alignment (vector memory takes it).
+template <typename T, int N, typename Col>
+__device__ __forceinline__ Raw<T, N> load_values(const T* row, Col at) {
+  const char* p = reinterpret_cast<const char*>(row);
+  if constexpr (sizeof(Col) == 4) p += uint32_t(at) * uint32_t(sizeof(T));  // one base for all lanes, 32 bits of each
+  else p += at * int64_t(sizeof(T));
+  constexpr int kPart = Raw<T, N>::kWords < 4 ? 2 : 4;
+  typedef uint32_t part_t __attribute__((ext_vector_type(kPart), aligned(sizeof(T))));
+  Raw<T, N> r;
 #pragma unroll
-    for (int j = 0; j < VEC - 1; ++j) {
-      if (j < left) {
-        if constexpr (VEC == 4) w[j] = f32_as_u32(p[j]);
-        else w[j / 2] |= uint32_t(p[j].bits) << (16 * (j & 1));
-      }
-    }
-    r = make_uint4(w[0], w[1], w[2], w[3]);
+  for (int i = 0; i < Raw<T, N>::kWords; i += kPart) {
+    const part_t v = *reinterpret_cast<const part_t*>(p + 4 * i);
+#pragma unroll
+    for (int j = 0; j < kPart; ++j) r.w[i + j] = v[j];
   }
   return r;
+}
+template <typename T, int N>
+__device__ __forceinline__ void widened(const Raw<T, N>& r, float (&f)[N]) {
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    if constexpr (sizeof(T) == 4) f[j] = u32_as_f32(r.w[j]);
+    else f[j] = u32_as_f32(j & 1 ? r.w[j / 2] & 0xFFFF0000u : r.w[j / 2] << 16);
+  }
+}
+// The values from `over` >= 0 on, moved to the front; zeros behind them.
+template <int N, typename Over>
+__device__ __forceinline__ void moved_up(float (&f)[N], Over over) {
+  if (over > 0) {
+#pragma unroll
+    for (int s = N / 2; s; s /= 2)
+      if (over & s) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) f[j] = j + s < N ? f[j + s < N ? j + s : 0] : 0.0f;
+      }
+    if (over >= N) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) f[j] = 0.0f;
+    }
+  }
+}
+// Values col .. col+N-1 of a row of `cols`, zeros behind its last one; nothing outside the row is read.
+template <typename T, int N, typename Col>
+__device__ __forceinline__ void load_short(const T* row, Col col, Col cols, float (&f)[N]) {
+  if (cols >= N) {
+    const Col at = col < cols - N ? col : cols - N;
+    widened(load_values<T, N>(row, at), f);
+    moved_up(f, col - at);
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) f[j] = col + j < cols ? load_one(row + col + j) : 0.0f;
+  }
 }
 
 // N values as elements of T from any element's alignment on; those from `left` on are not written.
 template <typename T, int N>
-__device__ __forceinline__ void store_values(T* p, const float (&f)[N], int64_t left) {
-  static_assert(N == 4 || N == 8, "a vector");
-  if (left >= N) {
-    if constexpr (sizeof(T) == 4) {
-      typedef float v4_t __attribute__((ext_vector_type(4), aligned(4)));
+__device__ __forceinline__ void store_some(T* p, const float* f) {
+  if constexpr (sizeof(T) == 4) {
+    typedef float vec_t __attribute__((ext_vector_type(N < 4 ? N : 4), aligned(4)));
 #pragma unroll
-      for (int i = 0; i < N; i += 4) *reinterpret_cast<v4_t*>(p + i) = v4_t{f[i], f[i + 1], f[i + 2], f[i + 3]};
-    } else {
-      typedef uint32_t vec_t __attribute__((ext_vector_type(N / 2), aligned(2)));
+    for (int i = 0; i < N; i += 4) {
       vec_t v;
 #pragma unroll
-      for (int i = 0; i < N; i += 2) v[i / 2] = bf16_pair(f[i], f[i + 1]);
-      *reinterpret_cast<vec_t*>(p) = v;
+      for (int j = 0; j < (N < 4 ? N : 4); ++j) v[j] = f[i + j];
+      *reinterpret_cast<vec_t*>(p + i) = v;
     }
+  } else if constexpr (N == 1) {
+    p->bits = uint16_t(bf16_pair(f[0], 0.0f));
   } else {
+    typedef uint32_t vec_t __attribute__((ext_vector_type(N / 2), aligned(2)));
+    vec_t v;
 #pragma unroll
-    for (int i = 0; i < N - 1; ++i)
-      if (i < left) {
-        if constexpr (sizeof(T) == 4) p[i] = f[i];
-        else p[i].bits = uint16_t(bf16_pair(f[i], 0.0f));
+    for (int i = 0; i < N; i += 2) v[i / 2] = bf16_pair(f[i], f[i + 1]);
+    *reinterpret_cast<vec_t*>(p) = v;
+  }
+}
+template <typename T, int N, typename Left>
+__device__ __forceinline__ void store_values(T* p, const float (&f)[N], Left left) {
+  static_assert(N == 4 || N == 8, "a vector");
+  if (left >= N) {
+    store_some<T, N>(p, f);
+  } else if (left > 0) {
+    float g[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) g[j] = f[j];
+#pragma unroll
+    for (int s = N / 2; s; s /= 2)
+      if (left & s) {
+        if (s == 4) store_some<T, 4>(p, g);
+        else if (s == 2) store_some<T, 2>(p, g);
+        else store_some<T, 1>(p, g);
+        p += s;
+#pragma unroll
+        for (int j = 0; j < N; ++j) g[j] = j + s < N ? g[j + s < N ? j + s : 0] : 0.0f;
       }
   }
 }
