@@ -95,6 +95,22 @@ __device__ __forceinline__ v4f_t multiply(const Fragment<true>& b, const Fragmen
   return sum;
 }
 
+// The same with the sums where they are, in an accumulation register.  The compiler gives results registers of their own, which leaves a
+// wavefront that holds 256 of them copying sums at every other instruction; tied, nothing moves.  It doesn't know either when they
+// can be read: see written_out.
+template <int ACODE, int BCODE, int SUB_A, int SUB_B>
+__device__ __forceinline__ void multiply_in_place(const Fragment<false>& b, const Fragment<false>& a, v4f_t& sum, int scale_b, int scale_a) {
+  asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[%5,%6,0] op_sel_hi:[%7,%8,0] cbsz:%9 blgp:%10"
+               : "+a"(sum)
+               : "v"(b.codes), "v"(a.codes), "v"(scale_b), "v"(scale_a), "n"(SUB_B & 1), "n"(SUB_A & 1), "n"(SUB_B / 2), "n"(SUB_A / 2),
+                 "n"(BCODE), "n"(ACODE));
+}
+// Eight sums, after the time that the longest matrix instruction takes to write its results (18 instructions' issues).
+__device__ __forceinline__ void written_out(v4f_t (&sum)[8]) {
+  asm volatile("s_nop 15\n\ts_nop 15"
+               : "+a"(sum[0]), "+a"(sum[1]), "+a"(sum[2]), "+a"(sum[3]), "+a"(sum[4]), "+a"(sum[5]), "+a"(sum[6]), "+a"(sum[7]));
+}
+
 // 16 codes with those from `left` on put to zero, whatever they are.
 __device__ __forceinline__ uint4 first_codes(uint4 v, int left) {
   uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -104,6 +120,13 @@ __device__ __forceinline__ uint4 first_codes(uint4 v, int left) {
     w[i] = here >= 4 ? w[i] : here <= 0 ? 0u : w[i] & ((1u << (8 * here)) - 1u);
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// What the lanes of a wavefront wrote to shared memory before is there for all of them behind.
+__device__ __forceinline__ void wavefront_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
 // Four results next to each other.
@@ -118,158 +141,313 @@ __device__ __forceinline__ void put_four(TO* y, int64_t at, v4f_t v, int left) {
 // tile's rows of both operands come into shared memory directly from memory (16 bytes a lane, no registers), one block ahead
 // of the one that is multiplied; one barrier a block.  A row is 128 bytes there, half of the banks, so its eight
 // 16-byte parts lie in an order of their own, part ^ (row % 8), and eight rows' reads meet no bank twice.
-template <int BM, int BN, int WM, int WN, int ACODE, int BCODE, typename TO, bool EXACT>
-__global__ __launch_bounds__(WM* WN* kWave, 2) void matmul_tile_kernel(const MatmulArgs args) {
-  constexpr int kWaves = WM * WN, kThreads = kWaves * kWave;
-  constexpr int MI = BM / WM / 16, NI = BN / WN / 16;  // 16 x 16 results of a wavefront
-  static_assert(MI % 4 == 0 && NI % 4 == 0, "a register holds the scales of four");
-  constexpr int kLoads = (BM + BN) / 8 / kWaves;  // of a wavefront and block: 8 rows each
-  static_assert(BM / 8 % kWaves == 0 && BN / 8 % kWaves == 0, "a load is of one operand");
-  __shared__ __align__(16) uint8_t tile0[(BM + BN) * kQBlock];
-  __shared__ __align__(16) uint8_t tile1[(BM + BN) * kQBlock];
-  __shared__ uint32_t scales[2][(BM + BN) / 4];
+constexpr int64_t kTileStride = int64_t(1) << 22;  // longest row: a tile's rows are told apart by 32 bits
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return uint32_t(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)p));
+}
+// 16 bytes a lane from base + offset to shared memory, `to` on, lane by lane.  Nothing waits for it but an explicit wait for
+// all loads: the compiler, where it knows of more such loads than it can tell apart, waits for all of them before every read of
+// shared memory, here for the block after the next one.
+__device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t offset, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(offset), "s"(base) : "memory");  // (m0 has no other use here)
+}
 
-  const int t = threadIdx.x, lane = t % kWave, wave = __builtin_amdgcn_readfirstlane(t / kWave);
-  // Workgroups are dealt to the chip's eight dies in turn; a die gets neighbouring tiles, in groups of kGroup rows of tiles, so
-  // that what its workgroups read at a time is in its cache.
-  constexpr int kDies = 8, kGroup = 8;
-  const int tiles_m = (args.m + BM - 1) / BM, tiles_n = (args.n + BN - 1) / BN, tiles = tiles_m * tiles_n;
-  const int split = blockIdx.x / tiles;
-  int id = blockIdx.x % tiles;
-  const int die = id % kDies, each = tiles / kDies, more = tiles % kDies;
-  id = die * each + (die < more ? die : more) + id / kDies;
-  const int group = id / (kGroup * tiles_n), in_group = id % (kGroup * tiles_n);
-  const int group_rows = tiles_m - group * kGroup < kGroup ? tiles_m - group * kGroup : kGroup;
-  const int m0 = (group * kGroup + in_group % group_rows) * BM, n0 = in_group / group_rows * BN;
-  const int first = int(int64_t(args.blocks) * split / args.splits), last = int(int64_t(args.blocks) * (split + 1) / args.splits);
+// A workgroup's tile, and its loads of one block: 8 rows of 128 codes a wavefront and load, a byte of scale a thread and turn.
+template <int BM, int BN, int WAVES>
+struct TileLoads {
+  static constexpr int kThreads = WAVES * kWave, kLoads = (BM + BN) / 8 / WAVES, kLoadsA = BM / 8 / WAVES;
+  static constexpr int kTurns = (BM + BN) / kThreads;
+  static_assert(BM / 8 % WAVES == 0 && BN / 8 % WAVES == 0, "a load is of one operand");
+  static_assert((BM + BN) % kThreads == 0 && (BM % kThreads == 0 || kTurns == 1), "every thread has a scale in every turn, of one operand or in the only turn");
+  const MatmulArgs& args;
+  const uint8_t *a0, *b0;
+  int lane, wave, m0, n0, part;
+  int split, first, whole, last;  // blocks of the contracted axis; [first, whole) are complete
+  uint32_t from[kLoads], scale_from[kTurns];
+  int scale_to[kTurns];
+  uint8_t scale_byte[kTurns];
 
-  // where this lane's loads come from: rows behind the last one give that one again, and are not used
-  const int part = (lane % 8) ^ (lane / 8);
-  const uint8_t* from[kLoads];
+  __device__ __forceinline__ explicit TileLoads(const MatmulArgs& g) : args(g) {
+    const int t = threadIdx.x;
+    lane = t % kWave;
+    wave = __builtin_amdgcn_readfirstlane(t / kWave);
+    // Workgroups are dealt to the chip's eight dies in turn; a die gets neighbouring tiles, in groups of kGroup rows of tiles, so
+    // that what its workgroups read at a time is in its cache.
+    constexpr int kDies = 8, kGroup = 8;
+    const int tiles_m = (args.m + BM - 1) / BM, tiles_n = (args.n + BN - 1) / BN, tiles = tiles_m * tiles_n;
+    split = blockIdx.x / tiles;
+    int id = blockIdx.x % tiles;
+    const int die = id % kDies, each = tiles / kDies, more = tiles % kDies;
+    id = die * each + (die < more ? die : more) + id / kDies;
+    const int group = id / (kGroup * tiles_n), in_group = id % (kGroup * tiles_n);
+    const int group_rows = tiles_m - group * kGroup < kGroup ? tiles_m - group * kGroup : kGroup;
+    m0 = (group * kGroup + in_group % group_rows) * BM;
+    n0 = in_group / group_rows * BN;
+    first = int(int64_t(args.blocks) * split / args.splits);
+    last = int(int64_t(args.blocks) * (split + 1) / args.splits);
+    whole = args.k % kQBlock && last == args.blocks ? last - 1 : last;
+    part = (lane % 8) ^ (lane / 8);
+    a0 = args.a + m0 * args.a_stride;
+    b0 = args.b + n0 * args.b_stride;
 #pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    const int row = (i * kWaves + wave) * 8 + lane / 8;
-    if (i < BM / 8 / kWaves) {
-      const int r = m0 + row < args.m ? m0 + row : args.m - 1;
-      from[i] = args.a + r * args.a_stride + part * 16;
-    } else {
-      const int r = n0 + row - BM < args.n ? n0 + row - BM : args.n - 1;
-      from[i] = args.b + r * args.b_stride + part * 16;
+    for (int i = 0; i < kLoads; ++i) from[i] = row_offset(i) + part * 16;
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+      const int row = i * kThreads + t;
+      if (row < BM) scale_from[i] = uint32_t(m0 + row < args.m ? m0 + row : args.m - 1) >> args.sa_shift;
+      else scale_from[i] = uint32_t(n0 + row - BM < args.n ? n0 + row - BM : args.n - 1) >> args.sb_shift;
+      scale_to[i] = (row / 64 * 16 + row % 16) * 4 + row / 16 % 4;  // a lane's four in a word
     }
   }
-  static_assert(BM + BN <= kThreads || (BM + BN) % kThreads == 0, "scales of a block: one byte per thread and turn");
-  constexpr int kScaleTurns = (BM + BN + kThreads - 1) / kThreads;
-  const uint8_t* scale_from[kScaleTurns];
-  int64_t scale_step[kScaleTurns];
-  int scale_to[kScaleTurns];
-#pragma unroll
-  for (int i = 0; i < kScaleTurns; ++i) {
-    const int row = i * kThreads + t;
-    if (row < BM) {
-      const int r = m0 + row < args.m ? m0 + row : args.m - 1;
-      scale_from[i] = args.sa + (r >> args.sa_shift);
-      scale_step[i] = args.sa_rows;
-    } else {
-      const int r = n0 + row - BM < args.n ? n0 + row - BM : args.n - 1;
-      scale_from[i] = args.sb + (r >> args.sb_shift);
-      scale_step[i] = args.sb_rows;
-    }
-    scale_to[i] = (row / 64 * 16 + row % 16) * 4 + row / 16 % 4;
+  // of load i's row, from the tile's first: rows behind the last one give that one again, and are not used
+  __device__ __forceinline__ uint32_t row_offset(int i) const {
+    const int row = (i * WAVES + wave) * 8 + lane / 8;
+    if (i < kLoadsA) return uint32_t(row < args.m - m0 ? row : args.m - m0 - 1) * uint32_t(args.a_stride);
+    return uint32_t(row - BM < args.n - n0 ? row - BM : args.n - n0 - 1) * uint32_t(args.b_stride);
   }
-
-  uint8_t scale_byte[kScaleTurns];
-  auto fetch = [&](int block, uint8_t* tile) {
+  __device__ __forceinline__ void fetch_scales(int block) {
 #pragma unroll
-    for (int i = 0; i < kScaleTurns; ++i) scale_byte[i] = scale_from[i][block * scale_step[i]];
+    for (int i = 0; i < kTurns; ++i) {
+      const bool of_a = i * kThreads + int(threadIdx.x) < BM;
+      scale_byte[i] = (of_a ? args.sa + block * args.sa_rows : args.sb + block * args.sb_rows)[scale_from[i]];
+    }
+  }
+  // loads FROM .. TO-1 of a block that is complete
+  template <int FROM, int TO>
+  __device__ __forceinline__ void fetch_some(int block, uint8_t* tile) {
     const int64_t col = int64_t(block) * kQBlock;
-    if (args.k - col >= kQBlock) {
+    const uint32_t to = lds_address(tile) + uint32_t(wave) * 8 * kQBlock;
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i)
-        __builtin_amdgcn_global_load_lds(
-            (const __attribute__((address_space(1))) void*)(from[i] + col),
-            (__attribute__((address_space(3))) void*)(tile + (i * kWaves + wave) * 8 * kQBlock), 16, 0, 0);
-    } else {  // the last, incomplete one goes through registers, where what is behind column k is put to zero
-      const int left = int(args.k - col) - part * 16;
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (left > 0) v = first_codes(load16(from[i] + col), left);
-        *reinterpret_cast<uint4*>(tile + (i * kWaves + wave) * 8 * kQBlock + lane * 16) = v;
-      }
+    for (int i = FROM; i < TO; ++i) load_to_lds((i < kLoadsA ? a0 : b0) + col, from[i], to + i * WAVES * 8 * kQBlock);
+  }
+  __device__ __forceinline__ void fetch(int block, uint8_t* tile) {
+    fetch_scales(block);
+    fetch_some<0, kLoads>(block, tile);
+  }
+  // the last, incomplete one: through registers, where what is behind column k is put to zero
+  __device__ __forceinline__ void fetch_short(int block, uint8_t* tile) {
+    fetch_scales(block);
+    const int64_t col = int64_t(block) * kQBlock;
+    const int left = int(args.k - col) - part * 16;
+#pragma unroll 1
+    for (int i = 0; i < kLoads; ++i) {
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (left > 0) v = first_codes(load16((i < kLoadsA ? a0 : b0) + col + row_offset(i) + part * 16), left);
+      *reinterpret_cast<uint4*>(tile + (i * WAVES + wave) * 8 * kQBlock + lane * 16) = v;
     }
-  };
-  auto put_scales = [&](int slot) {
-#pragma unroll
-    for (int i = 0; i < kScaleTurns; ++i)
-      if (BM + BN >= kThreads || t < BM + BN) reinterpret_cast<uint8_t*>(scales[slot])[scale_to[i]] = scale_byte[i];
-  };
-
-  const int wm = wave / WN, wn = wave % WN;
-  v4f_t sum[MI][NI];
-#pragma unroll
-  for (int i = 0; i < MI; ++i)
-#pragma unroll
-    for (int j = 0; j < NI; ++j) sum[i][j] = v4f_t{0, 0, 0, 0};
-
-  const int swap = lane % 8;
-  const int at0 = (lane % 16) * kQBlock + ((lane / 16 * 2) ^ swap) * 16, at1 = (lane % 16) * kQBlock + ((lane / 16 * 2 + 1) ^ swap) * 16;
-  auto codes_of = [&](const uint8_t* rows) {
-    const uint4 lo = *reinterpret_cast<const uint4*>(rows + at0), hi = *reinterpret_cast<const uint4*>(rows + at1);
-    return v8i_t{int(lo.x), int(lo.y), int(lo.z), int(lo.w), int(hi.x), int(hi.y), int(hi.z), int(hi.w)};
-  };
-  auto work = [&](const uint8_t* tile, int slot) {
-    const uint8_t* const ta = tile + wm * (BM / WM) * kQBlock;
-    const uint8_t* const tb = tile + (BM + wn * (BN / WN)) * kQBlock;
-    int sa[MI / 4], sb[NI / 4];
-#pragma unroll
-    for (int i = 0; i < MI / 4; ++i) sa[i] = int(scales[slot][(wm * (MI / 4) + i) * 16 + lane % 16]);
-#pragma unroll
-    for (int i = 0; i < NI / 4; ++i) sb[i] = int(scales[slot][BM / 4 + (wn * (NI / 4) + i) * 16 + lane % 16]);
-    Fragment<EXACT> fb[NI];
-    unrolled<0, NI>([&](auto j) {
-      fb[j.value] = fragment_of<BCODE>(codes_of(tb + j.value * 16 * kQBlock), sb[j.value / 4] >> (8 * (j.value % 4)) & 255, Int<EXACT>{});
-    });
-    unrolled<0, MI>([&](auto i) {
-      const Fragment<EXACT> fa =
-          fragment_of<ACODE>(codes_of(ta + i.value * 16 * kQBlock), sa[i.value / 4] >> (8 * (i.value % 4)) & 255, Int<EXACT>{});
-      unrolled<0, NI>([&](auto j) {
-        sum[i.value][j.value] = multiply<ACODE, BCODE, i.value % 4, j.value % 4>(fb[j.value], fa, sum[i.value][j.value],
-                                                                                 sb[j.value / 4], sa[i.value / 4]);
-      });
-    });
-  };
+  }
   // what was fetched last is in shared memory, for all
-  auto arrive = [&](int slot) {
-    put_scales(slot);
+  __device__ __forceinline__ void arrive(uint32_t* scales) {
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) reinterpret_cast<uint8_t*>(scales)[scale_to[i]] = scale_byte[i];
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
+  }
+};
+
+// 16 rows' codes out of a tile: a lane's 32 of row lane%16.
+__device__ __forceinline__ v8i_t codes_of(const uint8_t* rows, int lane) {
+  const uint8_t* const p = rows + lane % 16 * kQBlock;
+  const uint4 lo = *reinterpret_cast<const uint4*>(p + ((lane / 16 * 2) ^ (lane % 8)) * 16);
+  const uint4 hi = *reinterpret_cast<const uint4*>(p + ((lane / 16 * 2 + 1) ^ (lane % 8)) * 16);
+  return v8i_t{int(lo.x), int(lo.y), int(lo.z), int(lo.w), int(hi.x), int(hi.y), int(hi.z), int(hi.w)};
+}
+
+// A wavefront's results out through shared memory, 16 rows at a time, so that a row's leave in vectors and whole lines.
+template <typename TO, int MI, int NI>
+__device__ __forceinline__ void put_tile(const MatmulArgs& args, int split, float* out, int lane, int row0, int col0, const v4f_t (&sum)[MI][NI]) {
+  constexpr int TN = NI * 16, VEC = 16 / int(sizeof(TO)), kLanes = TN / VEC, kPad = 4;
+  TO* const y = static_cast<TO*>(args.y) + int64_t(split) * args.m * args.n;
+  const int col = col0 + lane % kLanes * VEC;
+  unrolled<0, MI>([&](auto i) {
+    unrolled<0, NI>([&](auto j) {
+      *reinterpret_cast<v4f_t*>(out + lane % 16 * (TN + kPad) + j.value * 16 + lane / 16 * 4) = sum[i.value][j.value];
+    });
+    wavefront_sync();
+#pragma unroll
+    for (int r = 0; r < 16; r += kWave / kLanes) {
+      const int in = r + lane / kLanes, row = row0 + i.value * 16 + in;
+      float f[VEC];
+#pragma unroll
+      for (int v = 0; v < VEC; v += 4) {
+        const v4f_t four = *reinterpret_cast<const v4f_t*>(out + in * (TN + kPad) + lane % kLanes * VEC + v);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) f[v + k] = four[k];
+      }
+      if (row < args.m) store_values(y + row * args.y_stride + col, f, args.n - col);
+    }
+    wavefront_sync();
+  });
+}
+
+// The 8-bit instruction: four wavefronts with S x S of 16 x 16 results each.  A wavefront reads 16 rows of a and of b at a time and multiplies
+// them with those that it has, 1, 3, 5, ... products, while the rows after the next are on their way.  Before the last 2S-1 all
+// rows are in registers: there the workgroup meets, the block after the next is fetched into this one's place, and the next one's
+// first rows are read meanwhile, so the matrix instructions stop for the meeting only.
+template <int S, int ACODE, int BCODE, typename TO>
+__global__ __launch_bounds__(4 * kWave, S == 8 ? 1 : 2) void matmul_tile_kernel(const MatmulArgs args) {
+  constexpr int kSide = 2 * S * 16;
+  __shared__ __align__(16) uint8_t tile0[2 * kSide * kQBlock];
+  __shared__ __align__(16) uint8_t tile1[2 * kSide * kQBlock];
+  __shared__ uint32_t scales0[2 * kSide / 4], scales1[2 * kSide / 4];
+  TileLoads<kSide, kSide, 4> loads(args);
+  const int lane = loads.lane, wm = loads.wave / 2, wn = loads.wave % 2;
+
+  v4f_t sum[S][S];
+#pragma unroll
+  for (int i = 0; i < S; ++i)
+#pragma unroll
+    for (int j = 0; j < S; ++j) sum[i][j] = v4f_t{0, 0, 0, 0};
+  Fragment<false> fa[S], fb[S];
+  int sa[S / 4], sb[S / 4];
+  auto read = [&](const uint8_t* tile, auto i) {
+    fa[i.value].codes = codes_of(tile + (wm * S + i.value) * 16 * kQBlock, lane);
+    fb[i.value].codes = codes_of(tile + (kSide + (wn * S + i.value) * 16) * kQBlock, lane);
+  };
+  auto begin = [&](const uint8_t* tile, const uint32_t* scales) {
+#pragma unroll
+    for (int i = 0; i < S / 4; ++i) {
+      sa[i] = int(scales[(wm * (S / 4) + i) * 16 + lane % 16]);
+      sb[i] = int(scales[kSide / 4 + (wn * (S / 4) + i) * 16 + lane % 16]);
+    }
+    read(tile, Int<0>{});
+    read(tile, Int<1>{});
+  };
+  // A block's products; more: meanwhile the beginning of the next one (`soon`, half of whose loads are on their way already) and
+  // the first half of the loads of the one after it, into this one's place.  A load takes its 16 cycles of the compute unit's one
+  // address unit, so they are spread over the products: two of these a load.
+  constexpr int kHalf = 2 * S / 2;  // of the 2 * S loads of a block
+  static_assert(TileLoads<kSide, kSide, 4>::kLoads == 2 * S, "");
+  auto work = [&](auto more, uint8_t* tile, uint8_t* next_tile, uint32_t* next_scales, int soon, int after) {
+    int ma[S / 4], mb[S / 4];
+#pragma unroll
+    for (int i = 0; i < S / 4; ++i) ma[i] = sa[i], mb[i] = sb[i];
+    auto product = [&](auto i, auto j) {
+      v4f_t& to = sum[i.value][j.value];
+      if constexpr (S == 8) multiply_in_place<ACODE, BCODE, i.value % 4, j.value % 4>(fb[j.value], fa[i.value], to, mb[j.value / 4], ma[i.value / 4]);
+      else to = multiply<ACODE, BCODE, i.value % 4, j.value % 4>(fb[j.value], fa[i.value], to, mb[j.value / 4], ma[i.value / 4]);
+    };
+    unrolled<0, S - 1>([&](auto r) {
+      if constexpr (r.value + 2 < S) read(tile, Int<r.value + 2>{});
+      __builtin_amdgcn_sched_barrier(0);
+      unrolled<0, r.value + 1>([&](auto j) {
+        product(r, j);
+        if constexpr (j.value < r.value) product(j, r);
+        constexpr int load = kHalf + r.value * (r.value + 1) / 2 + j.value;  // after 1, 2, 4, 6, ... products
+        if constexpr (more.value && load < 2 * S) loads.template fetch_some<load, load + 1>(soon, next_tile);
+      });
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    constexpr Int<S - 1> r;
+    if constexpr (more.value) {
+      loads.arrive(next_scales);
+      loads.fetch_scales(after);
+    }
+    // first the products that need the rows which the next block's first take the place of
+    product(r, Int<0>{}), product(Int<0>{}, r);
+    if constexpr (more.value) loads.template fetch_some<0, 1>(after, tile);
+    product(r, Int<1>{}), product(Int<1>{}, r);
+    if constexpr (more.value) {
+      loads.template fetch_some<1, 2>(after, tile);
+      begin(next_tile, next_scales);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    unrolled<2, S>([&](auto j) {
+      product(r, j);
+      if constexpr (j.value < r.value) product(j, r);
+      if constexpr (more.value) loads.template fetch_some<j.value, j.value + 1>(after, tile);
+    });
+    __builtin_amdgcn_sched_barrier(0);
   };
 
-  if (first < last) {
-    fetch(first, tile0);
-    arrive(0);
-    for (int block = first; block < last; block += 2) {
-      if (block + 1 < last) fetch(block + 1, tile1);
-      work(tile0, 0);
-      if (block + 1 >= last) break;
-      arrive(1);
-      if (block + 2 < last) fetch(block + 2, tile0);
-      work(tile1, 1);
-      if (block + 2 < last) arrive(0);
+  int block = loads.first;
+  if (block < loads.whole) {
+    // the one after the last is the last again, so that nothing branches between the instructions
+    const auto or_last = [&](int b) { return b < loads.whole ? b : loads.whole - 1; };
+    loads.fetch(block, tile0);
+    loads.arrive(scales0);
+    loads.fetch_scales(or_last(block + 1));
+    loads.template fetch_some<0, kHalf>(or_last(block + 1), tile1);
+    begin(tile0, scales0);
+#pragma unroll 1
+    for (; block + 1 < loads.whole; block += 2) {
+      work(Int<1>{}, tile0, tile1, scales1, block + 1, or_last(block + 2));
+      work(Int<1>{}, tile1, tile0, scales0, or_last(block + 2), or_last(block + 3));
     }
+    if (block < loads.whole) work(Int<0>{}, tile0, tile1, scales1, 0, 0), ++block;
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
   }
+  if (block < loads.last) {
+    loads.fetch_short(block, tile0);
+    loads.arrive(scales0);
+    begin(tile0, scales0);
+    work(Int<0>{}, tile0, tile1, scales1, 0, 0);
+  }
+  if constexpr (S == 8) {
+#pragma unroll
+    for (int i = 0; i < S; ++i) written_out(sum[i]);
+  }
+  __syncthreads();
+  constexpr int kFloats = 16 * (S * 16 + 4);  // of a wavefront's rows on their way out
+  static_assert(4 * kFloats * 4 <= 2 * kSide * kQBlock, "they fit");
+  put_tile<TO>(args, loads.split, reinterpret_cast<float*>(tile0) + loads.wave * kFloats, lane, loads.m0 + wm * S * 16, loads.n0 + wn * S * 16, sum);
+}
 
-  TO* const y = static_cast<TO*>(args.y) + int64_t(split) * args.m * args.n;
+// The 16-bit instructions: four wavefronts with S x S of 16 x 16 results each.  b's rows of a block are converted and held, a's
+// come 16 at a time, the next ones on their way while these are multiplied.
+template <int S, int ACODE, int BCODE>
+__global__ __launch_bounds__(4 * kWave, 2) void matmul_exact_kernel(const MatmulArgs args) {
+  constexpr int kSide = 2 * S * 16;
+  __shared__ __align__(16) uint8_t tile0[2 * kSide * kQBlock];
+  __shared__ __align__(16) uint8_t tile1[2 * kSide * kQBlock];
+  __shared__ uint32_t scales0[2 * kSide / 4], scales1[2 * kSide / 4];
+  TileLoads<kSide, kSide, 4> loads(args);
+  const int lane = loads.lane, wm = loads.wave / 2, wn = loads.wave % 2;
+  v4f_t sum[S][S];
 #pragma unroll
-  for (int i = 0; i < MI; ++i) {
-    const int row = m0 + wm * (BM / WM) + i * 16 + lane % 16;
-    if (row < args.m)
+  for (int i = 0; i < S; ++i)
 #pragma unroll
-      for (int j = 0; j < NI; ++j) {
-        const int col = n0 + wn * (BN / WN) + j * 16 + lane / 16 * 4;
-        put_four(y, row * args.y_stride + col, sum[i][j], args.n - col);
-      }
+    for (int j = 0; j < S; ++j) sum[i][j] = v4f_t{0, 0, 0, 0};
+  auto work = [&](const uint8_t* tile, const uint32_t* scales) {
+    const uint8_t* const ta = tile + wm * S * 16 * kQBlock;
+    const uint8_t* const tb = tile + (kSide + wn * S * 16) * kQBlock;
+    const int sa = int(scales[wm * 16 + lane % 16]), sb = int(scales[kSide / 4 + wn * 16 + lane % 16]);
+    static_assert(S == 4, "a word of scales");
+    v8i_t next = codes_of(ta, lane);
+    Fragment<true> fb[S];
+    unrolled<0, S>([&](auto j) { fb[j.value] = fragment_of<BCODE>(codes_of(tb + j.value * 16 * kQBlock, lane), sb >> (8 * j.value) & 255, Int<1>{}); });
+    unrolled<0, S>([&](auto i) {
+      const Fragment<true> fa = fragment_of<ACODE>(next, sa >> (8 * i.value) & 255, Int<1>{});
+      if constexpr (i.value + 1 < S) next = codes_of(ta + (i.value + 1) * 16 * kQBlock, lane);
+      unrolled<0, S>([&](auto j) { sum[i.value][j.value] = multiply<ACODE, BCODE, 0, 0>(fb[j.value], fa, sum[i.value][j.value], 0, 0); });
+    });
+  };
+  int block = loads.first;
+  if (block < loads.whole) {
+    const auto or_last = [&](int b) { return b < loads.whole ? b : loads.whole - 1; };
+    loads.fetch(block, tile0);
+    loads.arrive(scales0);
+#pragma unroll 1
+    for (; block + 1 < loads.whole; block += 2) {
+      loads.fetch(block + 1, tile1);
+      work(tile0, scales0);
+      loads.arrive(scales1);
+      loads.fetch(or_last(block + 2), tile0);
+      work(tile1, scales1);
+      loads.arrive(scales0);
+    }
+    if (block < loads.whole) work(tile0, scales0), ++block;
+    __syncthreads();
   }
+  if (block < loads.last) {
+    loads.fetch_short(block, tile0);
+    loads.arrive(scales0);
+    work(tile0, scales0);
+  }
+  __syncthreads();
+  constexpr int kFloats = 16 * (S * 16 + 4);
+  put_tile<float>(args, loads.split, reinterpret_cast<float*>(tile0) + loads.wave * kFloats, lane, loads.m0 + wm * S * 16, loads.n0 + wn * S * 16, sum);
 }
 
 // ---- few rows ---------------------------------------------------------------------------------
@@ -280,7 +458,7 @@ template <int MT, int ACODE, int BCODE, typename TO, bool EXACT>
 __global__ __launch_bounds__(kFewWaves* kWave) void matmul_few_kernel(const MatmulArgs args) {
   __shared__ v4f_t parts[kFewWaves - 1][MT][kWave];
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const int n0 = blockIdx.x * 16;
+  const int n0 = blockIdx.x * 16, m0 = blockIdx.z * 16 * MT;
   const int split = blockIdx.y;
   const int first = int(int64_t(args.blocks) * split / args.splits), last = int(int64_t(args.blocks) * (split + 1) / args.splits);
   const int rb = n0 + lane % 16 < args.n ? n0 + lane % 16 : args.n - 1;
@@ -291,7 +469,7 @@ __global__ __launch_bounds__(kFewWaves* kWave) void matmul_few_kernel(const Matm
   v4f_t sum[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
-    const int ra = i * 16 + lane % 16 < args.m ? i * 16 + lane % 16 : args.m - 1;
+    const int ra = m0 + i * 16 + lane % 16 < args.m ? m0 + i * 16 + lane % 16 : args.m - 1;
     a[i] = args.a + ra * args.a_stride + lane / 16 * 32;
     sa[i] = args.sa + (ra >> args.sa_shift);
     sum[i] = v4f_t{0, 0, 0, 0};
@@ -331,7 +509,7 @@ __global__ __launch_bounds__(kFewWaves* kWave) void matmul_few_kernel(const Matm
     v4f_t v = sum[i];
 #pragma unroll
     for (int w = 0; w < kFewWaves - 1; ++w) v += parts[w][i][lane];
-    const int row = i * 16 + lane % 16;
+    const int row = m0 + i * 16 + lane % 16;
     if (row < args.m) put_four(y, row * args.y_stride + col, v, args.n - col);
   }
 }
@@ -363,17 +541,23 @@ __global__ __launch_bounds__(256) void matmul_join_kernel(const float* parts, in
   }
 }
 
-enum { kFew1, kFew2, kFew4, kTile128 };
+enum { kFew1, kFew2, kFew4, kTile128, kTile256 };
 
 template <int ACODE, int BCODE, typename TO, bool EXACT>
 hipError_t run(const MatmulArgs& a, const MatmulPlan& p, hipStream_t s) {
   const auto tiles = [&](int size) { return uint32_t(blocks_of(a.m, size) * blocks_of(a.n, size) * a.splits); };
-  const dim3 few(uint32_t(blocks_of(a.n, 16)), uint32_t(a.splits));
+  const dim3 few(uint32_t(blocks_of(a.n, 16)), uint32_t(a.splits), uint32_t(blocks_of(a.m, 64)));
   switch (p.tile) {
     case kFew1: matmul_few_kernel<1, ACODE, BCODE, TO, EXACT><<<few, kFewWaves * kWave, 0, s>>>(a); break;
     case kFew2: matmul_few_kernel<2, ACODE, BCODE, TO, EXACT><<<few, kFewWaves * kWave, 0, s>>>(a); break;
     case kFew4: matmul_few_kernel<4, ACODE, BCODE, TO, EXACT><<<few, kFewWaves * kWave, 0, s>>>(a); break;
-    default: matmul_tile_kernel<128, 128, 2, 2, ACODE, BCODE, TO, EXACT><<<tiles(128), 256, 0, s>>>(a); break;
+    case kTile128:
+      if constexpr (EXACT) matmul_exact_kernel<4, ACODE, BCODE><<<tiles(128), 256, 0, s>>>(a);
+      else matmul_tile_kernel<4, ACODE, BCODE, TO><<<tiles(128), 256, 0, s>>>(a);
+      break;
+    default:
+      if constexpr (!EXACT) matmul_tile_kernel<8, ACODE, BCODE, TO><<<tiles(256), 256, 0, s>>>(a);
+      break;
   }
   return hipGetLastError();
 }
@@ -400,10 +584,16 @@ MatmulPlan make_matmul_plan(const accept_matmul_desc& d) {
   const int64_t blocks = blocks_of(d.k, kQBlock);
   int64_t groups;  // workgroups without splits
   int64_t least;   // blocks that a split is worth
-  if (d.m <= 64) {
+  const int64_t whole = accept_block_stride(d.k);
+  const bool long_rows = (d.a_stride ? d.a_stride : whole) > kTileStride || (d.b_stride ? d.b_stride : whole) > kTileStride;
+  if (d.m <= 64 || long_rows) {
     p.tile = d.m <= 16 ? kFew1 : d.m <= 32 ? kFew2 : kFew4;
-    groups = blocks_of(d.n, 16);
+    groups = blocks_of(d.n, 16) * blocks_of(d.m, 64);
     least = kFewWaves;
+  } else if (d.out_dtype == ACCEPT_BF16 && blocks_of(d.m, 256) * blocks_of(d.n, 256) >= 192) {
+    p.tile = kTile256;
+    groups = 256;
+    least = 1;
   } else {
     p.tile = kTile128;
     groups = blocks_of(d.m, 128) * blocks_of(d.n, 128);
