@@ -451,67 +451,116 @@ __global__ __launch_bounds__(4 * kWave, 2) void matmul_exact_kernel(const Matmul
 }
 
 // ---- few rows ---------------------------------------------------------------------------------
-// Bound by reading b.  A workgroup has 16 rows of b and all (at most 16*MT) rows of a; its wavefronts take the blocks of the
-// contracted axis in turn, straight from memory into registers, and their sums are added up in shared memory, in order.
+// Bound by reading b.  A workgroup has 16 rows of b and 16*MT rows of a (nearly always all of them); its wavefronts take the blocks of
+// the contracted axis in turn, straight from memory into registers, AHEAD of a wavefront's at a time, and their sums are
+// added up in shared memory, in order.
 constexpr int kFewWaves = 8;
-template <int MT, int ACODE, int BCODE, typename TO, bool EXACT>
+template <int MT, int NT, int ACODE, int BCODE, typename TO, bool EXACT>
 __global__ __launch_bounds__(kFewWaves* kWave) void matmul_few_kernel(const MatmulArgs args) {
-  __shared__ v4f_t parts[kFewWaves - 1][MT][kWave];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const int n0 = blockIdx.x * 16, m0 = blockIdx.z * 16 * MT;
+  constexpr int AHEAD = MT == 1 ? 4 : 2;
+  __shared__ v4f_t parts[kFewWaves][MT * NT][kWave];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int n0 = blockIdx.x * 16 * NT, m0 = blockIdx.z * 16 * MT;
   const int split = blockIdx.y;
   const int first = int(int64_t(args.blocks) * split / args.splits), last = int(int64_t(args.blocks) * (split + 1) / args.splits);
-  const int rb = n0 + lane % 16 < args.n ? n0 + lane % 16 : args.n - 1;
-  const uint8_t* const b = args.b + rb * args.b_stride + lane / 16 * 32;
-  const uint8_t* const sb = args.sb + (rb >> args.sb_shift);
-  const uint8_t* a[MT];
-  const uint8_t* sa[MT];
-  v4f_t sum[MT];
+  const int whole = args.k % kQBlock && last == args.blocks ? last - 1 : last;  // blocks [first, whole) are complete ones
+  const uint8_t *a[MT], *b[NT], *sa[MT], *sb[NT];
+  v4f_t sum[MT][NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const int rb = n0 + j * 16 + lane % 16 < args.n ? n0 + j * 16 + lane % 16 : args.n - 1;
+    b[j] = args.b + rb * args.b_stride + lane / 16 * 32;
+    sb[j] = args.sb + (rb >> args.sb_shift);
+  }
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
     const int ra = m0 + i * 16 + lane % 16 < args.m ? m0 + i * 16 + lane % 16 : args.m - 1;
     a[i] = args.a + ra * args.a_stride + lane / 16 * 32;
     sa[i] = args.sa + (ra >> args.sa_shift);
-    sum[i] = v4f_t{0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < NT; ++j) sum[i][j] = v4f_t{0, 0, 0, 0};
   }
-  auto load = [&](const uint8_t* p, int64_t col) {
-    uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
-    const int left = int(args.k - col) - lane / 16 * 32;
-    if (left >= 32) {
-      lo = load16(p + col);
-      hi = load16(p + col + 16);
-    } else {
-      if (left > 0) lo = first_codes(load16(p + col), left);
-      if (left > 16) hi = first_codes(load16(p + col + 16), left - 16);
-    }
+  struct Loaded {
+    v8i_t b[NT], a[MT];
+    int scale_b[NT], scale_a[MT];
+  };
+  auto codes = [](uint4 lo, uint4 hi) {
     return v8i_t{int(lo.x), int(lo.y), int(lo.z), int(lo.w), int(hi.x), int(hi.y), int(hi.z), int(hi.w)};
   };
-  for (int block = first + wave; block < last; block += kFewWaves) {
+  auto load = [&](Loaded& l, int block) {
     const int64_t col = int64_t(block) * kQBlock;
-    const int scale_b = sb[block * args.sb_rows];
-    const Fragment<EXACT> fb = fragment_of<BCODE>(load(b, col), scale_b, Int<EXACT>{});
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      l.b[j] = codes(load16(b[j] + col), load16(b[j] + col + 16));
+      l.scale_b[j] = sb[j][block * args.sb_rows];
+    }
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-      const int scale_a = sa[i][block * args.sa_rows];
-      sum[i] = multiply<ACODE, BCODE, 0, 0>(fb, fragment_of<ACODE>(load(a[i], col), scale_a, Int<EXACT>{}), sum[i], scale_b, scale_a);
+      l.a[i] = codes(load16(a[i] + col), load16(a[i] + col + 16));
+      l.scale_a[i] = sa[i][block * args.sa_rows];
     }
-  }
-  if (wave) {
+  };
+  auto add = [&](const Loaded& l) {
+    Fragment<EXACT> fb[NT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) parts[wave - 1][i][lane] = sum[i];
+    for (int j = 0; j < NT; ++j) fb[j] = fragment_of<BCODE>(l.b[j], l.scale_b[j], Int<EXACT>{});
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const Fragment<EXACT> fa = fragment_of<ACODE>(l.a[i], l.scale_a[i], Int<EXACT>{});
+#pragma unroll
+      for (int j = 0; j < NT; ++j) sum[i][j] = multiply<ACODE, BCODE, 0, 0>(fb[j], fa, sum[i][j], l.scale_b[j], l.scale_a[i]);
+    }
+  };
+  int block = first + wave;
+#pragma unroll 1
+  for (; block + (AHEAD - 1) * kFewWaves < whole; block += AHEAD * kFewWaves) {
+    Loaded l[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) load(l[u], block + u * kFewWaves);
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) add(l[u]);
   }
+#pragma unroll 1
+  for (; block < whole; block += kFewWaves) {
+    Loaded l;
+    load(l, block);
+    add(l);
+  }
+  if (block < last) {  // the incomplete one
+    const int64_t col = int64_t(block) * kQBlock;
+    const int left = int(args.k - col) - lane / 16 * 32;
+    auto load_short = [&](const uint8_t* p) {
+      uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
+      if (left > 0) lo = first_codes(load16(p + col), left);
+      if (left > 16) hi = first_codes(load16(p + col + 16), left - 16);
+      return codes(lo, hi);
+    };
+    Loaded l;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      l.b[j] = load_short(b[j]);
+      l.scale_b[j] = sb[j][block * args.sb_rows];
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      l.a[i] = load_short(a[i]);
+      l.scale_a[i] = sa[i][block * args.sa_rows];
+    }
+    add(l);
+  }
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) parts[wave][i * NT + j][lane] = sum[i][j];
   __syncthreads();
-  if (wave) return;
+  static_assert(MT * NT <= kFewWaves, "a wavefront adds up 16 x 16 results");
+  if (wave >= MT * NT) return;
+  v4f_t v = parts[0][wave][lane];
+#pragma unroll
+  for (int w = 1; w < kFewWaves; ++w) v += parts[w][wave][lane];
+  const int row = m0 + wave / NT * 16 + lane % 16, col = n0 + wave % NT * 16 + lane / 16 * 4;
   TO* const y = static_cast<TO*>(args.y) + int64_t(split) * args.m * args.n;
-  const int col = n0 + lane / 16 * 4;
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    v4f_t v = sum[i];
-#pragma unroll
-    for (int w = 0; w < kFewWaves - 1; ++w) v += parts[w][i][lane];
-    const int row = m0 + i * 16 + lane % 16;
-    if (row < args.m) put_four(y, row * args.y_stride + col, v, args.n - col);
-  }
+  if (row < args.m) put_four(y, row * args.y_stride + col, v, args.n - col);
 }
 
 // Sum of the parts of the contracted axis, in order; zeros where there are none.
@@ -541,16 +590,27 @@ __global__ __launch_bounds__(256) void matmul_join_kernel(const float* parts, in
   }
 }
 
-enum { kFew1, kFew2, kFew4, kTile128, kTile256 };
+enum { kFew1, kFew2, kFew3, kFew4, kTile128, kTile256 };
 
 template <int ACODE, int BCODE, typename TO, bool EXACT>
 hipError_t run(const MatmulArgs& a, const MatmulPlan& p, hipStream_t s) {
   const auto tiles = [&](int size) { return uint32_t(blocks_of(a.m, size) * blocks_of(a.n, size) * a.splits); };
-  const dim3 few(uint32_t(blocks_of(a.n, 16)), uint32_t(a.splits), uint32_t(blocks_of(a.m, 64)));
+  const dim3 few(uint32_t(blocks_of(a.n, 16 * p.few_n)), uint32_t(a.splits), uint32_t(blocks_of(a.m, 64)));  // (all rows of a, but for long rows)
+  const int few_threads = kFewWaves * kWave;
   switch (p.tile) {
-    case kFew1: matmul_few_kernel<1, ACODE, BCODE, TO, EXACT><<<few, kFewWaves * kWave, 0, s>>>(a); break;
-    case kFew2: matmul_few_kernel<2, ACODE, BCODE, TO, EXACT><<<few, kFewWaves * kWave, 0, s>>>(a); break;
-    case kFew4: matmul_few_kernel<4, ACODE, BCODE, TO, EXACT><<<few, kFewWaves * kWave, 0, s>>>(a); break;
+    case kFew1: matmul_few_kernel<1, 1, ACODE, BCODE, TO, EXACT><<<few, few_threads, 0, s>>>(a); break;
+    case kFew2:
+      if (p.few_n == 2) matmul_few_kernel<2, 2, ACODE, BCODE, TO, EXACT><<<few, few_threads, 0, s>>>(a);
+      else matmul_few_kernel<2, 1, ACODE, BCODE, TO, EXACT><<<few, few_threads, 0, s>>>(a);
+      break;
+    case kFew3:
+      if (p.few_n == 2) matmul_few_kernel<3, 2, ACODE, BCODE, TO, EXACT><<<few, few_threads, 0, s>>>(a);
+      else matmul_few_kernel<3, 1, ACODE, BCODE, TO, EXACT><<<few, few_threads, 0, s>>>(a);
+      break;
+    case kFew4:
+      if (p.few_n == 2) matmul_few_kernel<4, 2, ACODE, BCODE, TO, EXACT><<<few, few_threads, 0, s>>>(a);
+      else matmul_few_kernel<4, 1, ACODE, BCODE, TO, EXACT><<<few, few_threads, 0, s>>>(a);
+      break;
     case kTile128:
       if constexpr (EXACT) matmul_exact_kernel<4, ACODE, BCODE><<<tiles(128), 256, 0, s>>>(a);
       else matmul_tile_kernel<4, ACODE, BCODE, TO><<<tiles(128), 256, 0, s>>>(a);
@@ -578,6 +638,13 @@ hipError_t join(const MatmulArgs& a, const void* parts, int splits, void* y, hip
 
 }  // namespace
 
+// Which kernel, and into how many parts the contracted axis goes: a part costs its results in float32, written and read, and the
+// second kernel, 2 to 4 us, so only where there are not workgroups for every compute unit, and a part is `least` blocks long.
+//   Up to 64 rows the kernel that streams b; 32 columns of results a workgroup where that still fills the chip (48 x 8192 x 2048 10.3 us
+//   with 16, 7.9 with 32, but 64 x 4096 x 4096 12.0 and 14.7).  Parts of 8 / 16 / 32 / 64 blocks: one row, 512 x 8192 9.6 / 8.2 / 10.4 / 7.1 us,
+//   2048 x 8192 10.0 / 8.6 / 10.0 / 7.3; 64 rows, 2048 x 4096 12.8 / 10.0 / 12.0 / 12.0, 128 x 8192 10.1 / 10.1 / 14.1 / 20.6.
+//   Then tiles of 256 x 256 where they are enough (us with tiles of 128 / 256: 4096^3 70.6 / 55.6, 8192 x 8192 x 1024 89.7 / 76.0, but 1024 x 8192 x
+//   8192, 128 large tiles, 64.2 / 99.7), else of 128 x 128.  Float32 results: 128 x 128.
 MatmulPlan make_matmul_plan(const accept_matmul_desc& d) {
   MatmulPlan p{};
   p.splits = 1;
@@ -587,9 +654,10 @@ MatmulPlan make_matmul_plan(const accept_matmul_desc& d) {
   const int64_t whole = accept_block_stride(d.k);
   const bool long_rows = (d.a_stride ? d.a_stride : whole) > kTileStride || (d.b_stride ? d.b_stride : whole) > kTileStride;
   if (d.m <= 64 || long_rows) {
-    p.tile = d.m <= 16 ? kFew1 : d.m <= 32 ? kFew2 : kFew4;
-    groups = blocks_of(d.n, 16) * blocks_of(d.m, 64);
-    least = kFewWaves;
+    p.tile = d.m <= 16 ? kFew1 : d.m <= 32 ? kFew2 : d.m <= 48 ? kFew3 : kFew4;
+    p.few_n = d.m > 16 && blocks_of(d.n, 32) >= 256 ? 2 : 1;
+    groups = blocks_of(d.n, 16 * p.few_n) * blocks_of(d.m, 64);
+    least = d.m <= 16 ? 64 : 16;
   } else if (d.out_dtype == ACCEPT_BF16 && blocks_of(d.m, 256) * blocks_of(d.n, 256) >= 192) {
     p.tile = kTile256;
     groups = 256;

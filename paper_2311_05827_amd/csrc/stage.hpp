@@ -30,6 +30,7 @@ hipError_t launch_block_quantize(const accept_block_desc& d, const void* x, void
 
 struct MatmulPlan {
   int tile;      // which kernel (see make_matmul_plan)
+  int few_n;     // few rows: 16 columns of results a workgroup, or 32
   int splits;    // parts of the contracted axis, joined by a second kernel where there are several
   size_t bytes;  // workspace
 };
