@@ -647,7 +647,7 @@ hipError_t join(const MatmulArgs& a, const void* parts, int splits, void* y, hip
 //   8192, 128 large tiles, 64.2 / 99.7), else of 128 x 128.  Float32 results: 128 x 128.
 MatmulPlan make_matmul_plan(const accept_matmul_desc& d) {
   MatmulPlan p{};
-  p.splits = 1;
+  p.splits = p.few_n = 1;
   const int64_t blocks = blocks_of(d.k, kQBlock);
   int64_t groups;  // workgroups without splits
   int64_t least;   // blocks that a split is worth
