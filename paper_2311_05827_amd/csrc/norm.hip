@@ -408,7 +408,7 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const float* partials, 
 
 // ---- dispatch ---------------------------------------------------------------------------------
 // Wavefronts per row and vectors per lane: one wavefront while a row fits in its registers with 32 values a lane (16 in the
-// backward pass, which holds five of them), then 4, then 8.
+// backward pass, which holds five of them), then 4, then 8, and 16 in the backward pass.
 template <typename TX, template <int, int> class Launch, int FLOATS, typename... Args>
 hipError_t by_width(int64_t cols, Args&&... args) {
   constexpr int VEC = Elem<TX>::VEC, F = FLOATS / VEC;
@@ -419,6 +419,10 @@ hipError_t by_width(int64_t cols, Args&&... args) {
   ACCEPT_WIDTH(1, 1) ACCEPT_WIDTH(1, 2) ACCEPT_WIDTH(1, 3) ACCEPT_WIDTH(1, 4) ACCEPT_WIDTH(1, 6) ACCEPT_WIDTH(1, 8)
   ACCEPT_WIDTH(4, 1) ACCEPT_WIDTH(4, 2) ACCEPT_WIDTH(4, 3) ACCEPT_WIDTH(4, 4) ACCEPT_WIDTH(4, 6) ACCEPT_WIDTH(4, 8)
   ACCEPT_WIDTH(8, 2) ACCEPT_WIDTH(8, 3) ACCEPT_WIDTH(8, 4) ACCEPT_WIDTH(8, 6) ACCEPT_WIDTH(8, 8)
+  if constexpr (FLOATS == 16) {  // the backward pass: 128 registers hold 16 bfloat16 or 12 float32 values' sums and inputs
+    ACCEPT_WIDTH(16, 2)
+    if constexpr (VEC == 4) { ACCEPT_WIDTH(16, 3) }
+  }
 #undef ACCEPT_WIDTH
   return Launch<0, 0>::run(args...);
 }
@@ -450,7 +454,8 @@ hipError_t forward(int x_dtype, const NormArgs& a, hipStream_t s) {
 }
 
 constexpr int64_t kWaveCols = kWave * 16;      // longest row of norm_back_kernel for one wavefront
-constexpr int64_t kHeldCols = 8 * kWaveCols;  // longest row of norm_back_kernel
+// longest row of norm_back_kernel
+constexpr int64_t held_cols(int x_dtype) { return x_dtype == ACCEPT_F32 ? 12 * kWaveCols : 16 * kWaveCols; }
 
 template <typename TX, typename TY>
 struct Backward {
@@ -500,14 +505,14 @@ NormArgs forward_args(const accept_norm_desc& d, const void* x, const void* weig
 // 4096 x 4096 29.4 / 26.1 / 27.6, 2048 x 8192 26.9 / 29.7 / 37.1, 600 x 8192 16.6 / 20.7 / 24.8.
 NormPlan make_nplan(const accept_norm_desc& d) {
   NormPlan p{};
-  const bool held = d.cols >= 8 && d.cols <= kHeldCols;
+  const bool held = d.cols >= 8 && d.cols <= held_cols(d.x_dtype);
   int64_t grid;
   if (!held) {
     grid = blocks_of(d.rows, 64) < 64 ? blocks_of(d.rows, 64) : 64;
   } else if (d.cols <= kWaveCols) {
     grid = blocks_of(d.rows, 16) < 256 ? blocks_of(d.rows, 16) : 256;
   } else {
-    const int64_t most = d.cols <= 4 * kWaveCols ? 768 : 512, by_rows = d.rows / 8 > 256 ? d.rows / 8 : 256;
+    const int64_t most = d.cols <= 4 * kWaveCols ? 768 : d.cols <= 8 * kWaveCols ? 512 : 256, by_rows = d.rows / 8 > 256 ? d.rows / 8 : 256;
     grid = d.rows < by_rows ? d.rows : by_rows;
     grid = grid < most ? grid : most;
   }
