@@ -286,7 +286,10 @@ __device__ __forceinline__ void put_tile(const MatmulArgs& args, int split, floa
 // The 8-bit instruction: four wavefronts with S x S of 16 x 16 results each.  A wavefront reads 16 rows of a and of b at a time and multiplies
 // them with those that it has, 1, 3, 5, ... products, while the rows after the next are on their way.  Before the last 2S-1 all
 // rows are in registers: there the workgroup meets, the block after the next is fetched into this one's place, and the next one's
-// first rows are read meanwhile, so the matrix instructions stop for the meeting only.
+// first rows are read meanwhile, so the matrix instructions stop for the meeting only.  S = 8: tiles of 256 x 256, one wavefront a SIMD; S = 4:
+// 128 x 128, two workgroups a compute unit.  8192^3 in 411 us (2.68 PFLOP/s; the first form, all rows read before the first product and
+// two 128 x 128 tiles a compute unit, 612): the matrix units work 63 % of the cycles, 13 % go for waits at the meetings, about 9 %
+// for a tile's first loads and its results' way out, which overlap with nothing; the clock sinks to 1.9 GHz meanwhile.
 template <int S, int ACODE, int BCODE, typename TO>
 __global__ __launch_bounds__(4 * kWave, S == 8 ? 1 : 2) void matmul_tile_kernel(const MatmulArgs args) {
   constexpr int kSide = 2 * S * 16;
@@ -398,7 +401,8 @@ __global__ __launch_bounds__(4 * kWave, S == 8 ? 1 : 2) void matmul_tile_kernel(
 }
 
 // The 16-bit instructions: four wavefronts with S x S of 16 x 16 results each.  b's rows of a block are converted and held, a's
-// come 16 at a time, the next ones on their way while these are multiplied.
+// come 16 at a time, the next ones on their way while these are multiplied.  2048 x 768 over 8144 in five parts 32 us (0.8
+// PFLOP/s): the matrix units work 43 % of the cycles, the conversions take the issue of 128 instructions beside each 64.
 template <int S, int ACODE, int BCODE>
 __global__ __launch_bounds__(4 * kWave, 2) void matmul_exact_kernel(const MatmulArgs args) {
   constexpr int kSide = 2 * S * 16;
@@ -456,7 +460,8 @@ __global__ __launch_bounds__(4 * kWave, 2) void matmul_exact_kernel(const Matmul
 // ---- few rows ---------------------------------------------------------------------------------
 // Bound by reading b.  A workgroup has 16 rows of b and 16*MT rows of a (nearly always all of them); its wavefronts take the blocks of
 // the contracted axis in turn, straight from memory into registers, AHEAD of a wavefront's at a time, and their sums are
-// added up in shared memory, in order.
+// added up in shared memory, in order.  One row by 8192 x 8192 14.1 us (4.8 TB/s), by 4096 x 4096 5.8 a call; 48 rows by 8192 x 2048 7.5, where a's
+// rows, read by every workgroup, take as many loads as b's.
 constexpr int kFewWaves = 8;
 template <int MT, int NT, int ACODE, int BCODE, typename TO, bool EXACT>
 __global__ __launch_bounds__(kFewWaves* kWave) void matmul_few_kernel(const MatmulArgs args) {

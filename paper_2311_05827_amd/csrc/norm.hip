@@ -110,7 +110,9 @@ __device__ __forceinline__ Place place_of(int col, int cols) {
 }
 
 // One row at a time per WAVES wavefronts, C vectors of it in a lane's registers and the next row's on their way: x is read
-// once, the variance is that of the differences.  Bound by memory.
+// once, the variance is that of the differences.  Bound by memory: 8144 x 768 float32 8.2 us a call (6.1 TB/s, part of it in the memory-side
+// cache), 16384 x 4096 bfloat16 43.7 (6.1 TB/s), to codes 42.9; 1531 x 5003 bfloat16 9.2 (3.3 TB/s), two rows a workgroup one
+// after the other; one row of 4096 to codes 2.7 in the kernel: two trips to memory and two meetings of four wavefronts.
 template <typename TX, typename TY, int WAVES, int C>
 __global__ __launch_bounds__(WAVES == 8 ? 512 : 256) void norm_kernel(const NormArgs a) {
   constexpr int VEC = Elem<TX>::VEC;
@@ -181,6 +183,7 @@ __global__ __launch_bounds__(WAVES == 8 ? 512 : 256) void norm_kernel(const Norm
 }
 
 // Rows longer than a workgroup's registers hold, or shorter than a vector: read three times, from the caches the second and third.
+// 2048 x 20000 bfloat16 67.7 us (2.4 TB/s of one read; 16384 values a row, in registers, 30.2).
 template <typename TX, typename TY>
 __global__ __launch_bounds__(1024) void norm_long_kernel(const NormArgs a) {
   constexpr int VEC = Elem<TX>::VEC, WAVES = 16;
@@ -230,7 +233,9 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const NormArgs a) {
 }
 
 // Backward: rows as in norm_kernel, with the two row sums that dx needs; every lane sums its columns' dy*h and dy over the rows
-// that it meets, and the workgroup leaves these sums for join_kernel.  One read of x and dy.
+// that it meets, and the workgroup leaves these sums for norm_join_kernel.  One read of x and dy.  With the join, bfloat16: 16384 x 8192 158 us
+// (5.1 TB/s), 8192 x 2048 25.6, 8144 x 768 12.1 (3.1 TB/s: 11 of this kernel, 9.3 without sums, 3.8 of the join).  The next row's loads
+// ahead of this one's sums cost registers and with them wavefronts: 164 us at 16384 x 8192.
 // (Rows of a workgroup at a time: 16 wavefronts where their 128 registers do for one's vectors, so that there are few partial sums.)
 constexpr int back_rows(int vec, int waves, int c) { return waves != 1 ? 1 : vec == 4 && c == 4 ? 8 : 16; }
 constexpr int back_threads(int vec, int waves, int c) { return back_rows(vec, waves, c) * waves * kWave; }
@@ -326,7 +331,8 @@ __global__ __launch_bounds__(back_threads(Elem<TX>::VEC, WAVES, C)) void norm_ba
   }
 }
 
-// dx of rows longer than a workgroup's registers hold, or shorter than a vector: two reads.
+// dx of rows longer than a workgroup's registers hold, or shorter than a vector: two reads.  With the sums below, 2048 x 20000
+// bfloat16 115 us.
 template <typename TX, typename TY>
 __global__ __launch_bounds__(1024) void norm_back_long_kernel(const NormBackArgs a) {
   constexpr int VEC = Elem<TX>::VEC, WAVES = 16;
@@ -384,7 +390,8 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(const NormBackArgs a,
   a.partials[(int64_t(blockIdx.y) * 2 + 1) * a.cols + col] = db;
 }
 
-// Sums of the workgroups' column sums: 64 columns a workgroup, its 16 wavefronts take every 16th record each.
+// Sums of the workgroups' column sums: 64 columns a workgroup, its 16 wavefronts take every 16th record each, 16 loads on their way at a
+// time (one after the other: 10.5 us for 512 records of 768 columns, now 3.8 for 256).  Bound by the trips to memory.
 __global__ __launch_bounds__(1024) void norm_join_kernel(const float* partials, int records, int64_t cols, void* dweight,
                                                          void* dbias, int param_bf16) {
   __shared__ float part[16][kWave];
@@ -414,19 +421,22 @@ hipError_t by_width(int64_t cols, Args&&... args) {
   constexpr int VEC = Elem<TX>::VEC, F = FLOATS / VEC;
   if (cols < 8) return Launch<0, 0>::run(args...);  // for both types' vectors
   const int64_t v = blocks_of(cols, kWave * VEC);   // wavefronts' vectors in a row
-#define ACCEPT_WIDTH(WAVES, CC) \
-  if constexpr (CC <= F) if (v <= WAVES * CC) return Launch<WAVES, CC>::run(args...);
-  ACCEPT_WIDTH(1, 1) ACCEPT_WIDTH(1, 2) ACCEPT_WIDTH(1, 3) ACCEPT_WIDTH(1, 4) ACCEPT_WIDTH(1, 6) ACCEPT_WIDTH(1, 8)
-  ACCEPT_WIDTH(4, 1) ACCEPT_WIDTH(4, 2) ACCEPT_WIDTH(4, 3) ACCEPT_WIDTH(4, 4) ACCEPT_WIDTH(4, 6) ACCEPT_WIDTH(4, 8)
-  ACCEPT_WIDTH(8, 2) ACCEPT_WIDTH(8, 3) ACCEPT_WIDTH(8, 4) ACCEPT_WIDTH(8, 6) ACCEPT_WIDTH(8, 8)
+  // (a form is built where the one with fewer wavefronts and all its vectors does not reach)
+#define ACCEPT_WIDTH(WAVES, FEWER, CC) \
+  if constexpr (CC <= F && WAVES * CC > FEWER * F) if (v <= WAVES * CC) return Launch<WAVES, CC>::run(args...);
+  ACCEPT_WIDTH(1, 0, 1) ACCEPT_WIDTH(1, 0, 2) ACCEPT_WIDTH(1, 0, 3) ACCEPT_WIDTH(1, 0, 4) ACCEPT_WIDTH(1, 0, 6) ACCEPT_WIDTH(1, 0, 8)
+  ACCEPT_WIDTH(4, 1, 1) ACCEPT_WIDTH(4, 1, 2) ACCEPT_WIDTH(4, 1, 3) ACCEPT_WIDTH(4, 1, 4) ACCEPT_WIDTH(4, 1, 6) ACCEPT_WIDTH(4, 1, 8)
+  ACCEPT_WIDTH(8, 4, 2) ACCEPT_WIDTH(8, 4, 3) ACCEPT_WIDTH(8, 4, 4) ACCEPT_WIDTH(8, 4, 6) ACCEPT_WIDTH(8, 4, 8)
   if constexpr (FLOATS == 16) {  // the backward pass: 128 registers hold 16 bfloat16 or 12 float32 values' sums and inputs
-    ACCEPT_WIDTH(16, 2)
-    if constexpr (VEC == 4) { ACCEPT_WIDTH(16, 3) }
+    if constexpr (VEC == 8) { ACCEPT_WIDTH(16, 8, 2) }
+    if constexpr (VEC == 4) { ACCEPT_WIDTH(16, 8, 3) }
   }
 #undef ACCEPT_WIDTH
   return Launch<0, 0>::run(args...);
 }
 
+// Workgroups of the forward pass: few enough that each has several rows, loads its parameters once and has the next row on its way. Kernel,
+// us, with up to 512 / 1024 / 2048: 8144 x 768 float32 9.1 / 8.8 / 11.6, 1531 x 5003 bfloat16 9.9 / 10.3 / 12.6.
 constexpr int64_t kForwardGrid = 1024;
 
 template <typename TX, typename TY>
