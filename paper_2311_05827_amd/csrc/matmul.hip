@@ -571,17 +571,30 @@ __global__ __launch_bounds__(kFewWaves* kWave) void matmul_few_kernel(const Matm
   if (row < args.m) put_four(y, row * args.y_stride + col, v, args.n - col);
 }
 
-// Sum of the parts of the contracted axis, in order; zeros where there are none.
+// Sum of the parts of the contracted axis, in order; zeros where there are none.  Four parts' loads are on their way at a time:
+// eight parts of 300 x 300 over 8192 17.4 -> 15.6 us a call; five of 2048 x 768 take 6.8, the memory's rate.
 template <typename TO>
 __global__ __launch_bounds__(256) void matmul_join_kernel(const float* parts, int splits, int64_t m, int64_t n, TO* y, int64_t y_stride) {
   const int64_t total = m * n;
   for (int64_t at = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4; at < total; at += int64_t(gridDim.x) * 1024) {
     float sum[4] = {0, 0, 0, 0};
-    for (int s = 0; s < splits; ++s) {
-      float f[4];
-      load_short(parts + s * total, at, total, f);
+    if (total >= 4) {
+      const int64_t from = at < total - 4 ? at : total - 4;
+#pragma unroll 4
+      for (int s = 0; s < splits; ++s) {
+        float f[4];
+        widened(load_values<float, 4>(parts + s * total, from), f);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) sum[j] += f[j];
+        for (int j = 0; j < 4; ++j) sum[j] += f[j];
+      }
+      moved_up(sum, at - from);
+    } else {
+      for (int s = 0; s < splits; ++s) {
+        float f[4];
+        load_short(parts + s * total, at, total, f);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[j] += f[j];
+      }
     }
     const int64_t row = at / n, col = at % n;
     if (col + 4 <= n) {
@@ -651,7 +664,8 @@ hipError_t join(const MatmulArgs& a, const void* parts, int splits, void* y, hip
 //   Up to 64 rows the kernel that streams b; 32 columns of results a workgroup where that still fills the chip (48 x 8192 x 2048 10.3 us
 //   with 16, 7.9 with 32, but 64 x 4096 x 4096 12.0 and 14.7).  Parts of 8 / 16 / 32 / 64 blocks: one row, 512 x 8192 9.6 / 8.2 / 10.4 / 7.1 us,
 //   2048 x 8192 10.0 / 8.6 / 10.0 / 7.3; 64 rows, 2048 x 4096 12.8 / 10.0 / 12.0 / 12.0, 128 x 8192 10.1 / 10.1 / 14.1 / 20.6.
-//   Then tiles of 256 x 256 where they are enough (us with tiles of 128 / 256: 4096^3 70.6 / 55.6, 8192 x 8192 x 1024 89.7 / 76.0, but 1024 x 8192 x
+//   Tiles: parts of 8 blocks (float32, 200 x 4096 x 1024: one part of 8 12.0 us, two of 4 13.6; 300 x 300 x 8192: 1 / 4 / 8 parts 63 / 23 / 17).
+//   256 x 256 where they are enough (us with tiles of 128 / 256: 4096^3 70.6 / 55.6, 8192 x 8192 x 1024 89.7 / 76.0, but 1024 x 8192 x
 //   8192, 128 large tiles, 64.2 / 99.7), else of 128 x 128.  Float32 results: 128 x 128.
 MatmulPlan make_matmul_plan(const accept_matmul_desc& d) {
   MatmulPlan p{};
@@ -673,7 +687,7 @@ MatmulPlan make_matmul_plan(const accept_matmul_desc& d) {
   } else {
     p.tile = kTile128;
     groups = blocks_of(d.m, 128) * blocks_of(d.n, 128);
-    least = 4;
+    least = 8;
   }
   if (groups < 256 && d.m > 0 && d.n > 0) {
     const int64_t most = blocks / least, want = 512 / (groups < 1 ? 1 : groups);

@@ -172,6 +172,30 @@ def test_product(A, m, n, k, out):
 
 
 @pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n,k", [(1, 20, 16500), (9, 33, 20001), (20, 130, 4200), (64, 40, 5000), (130, 140, 2100), (1, 1, 16400)])
+def test_product_in_parts(A, m, n, k, out):
+    """Few results over a long axis: parts of it, of unequal length, the last one with an incomplete block."""
+    assert A.accept_matmul_workspace_size(A.make_matmul_desc(m, n, k, out_dtype=code_of(A, out))) > 0
+    y, a, b = multiply(A, np.random.default_rng(k), m, n, k, out)
+    check_product(y, a, b, out)
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n,k", [(40, 8200, 300), (64, 8300, 1100), (17, 8192, 129)])
+def test_product_of_few_rows_with_many(A, m, n, k, out):
+    """Up to 64 rows and enough columns for 32 of them a workgroup."""
+    y, a, b = multiply(A, np.random.default_rng(n), m, n, k, out)
+    check_product(y, a, b, out)
+
+
+@pytest.mark.parametrize("m,n,k", [(3600, 3500, 130), (4000, 3400, 1), (3585, 3585, 400)])
+def test_product_of_large_tiles(A, m, n, k):
+    """Enough results for tiles of 256 x 256, none of them whole at the edges."""
+    y, a, b = multiply(A, np.random.default_rng(m), m, n, k, "bf16")
+    check_product(y, a, b, "bf16")
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
 @pytest.mark.parametrize("codes", [(0, 0), (0, 1), (1, 0), (1, 1)])
 @pytest.mark.parametrize("m,n,k", [(3, 50, 200), (40, 300, 1500), (200, 150, 700)])
 def test_product_of_types(A, m, n, k, codes, out):
