@@ -79,7 +79,8 @@ accept_status accept_layer_norm_backward(const accept_norm_desc* desc, const voi
  * M = 57344).  Values that share a scale are 128 neighbours of a row (group 1), or the 128 x 128 of a square (group 128);
  * what is left at the ends of rows and columns makes smaller ones.  With c the largest magnitude among them, the scale is
  * 2^e with the smallest e >= -100 for which c <= M * 2^e, and a value's code is x * 2^-e rounded to the nearest, ties to even.
- * It is kept as the byte e + 127 (E8M0), 27 to 247; the products' results are unspecified for bytes outside that.  A power of two is exact to divide and to multiply by, and it is what the
+ * It is kept as the byte e + 127 (E8M0), 27 to 247; the products' results are unspecified for bytes outside that.
+ * A power of two is exact to divide and to multiply by, and it is what the
  * matrix instruction applies by itself; the codes being floating-point numbers, the up to one bit that it leaves unused
  * at the top costs range at the bottom, and no relative precision.
  * A NaN stays one and takes no part in c; an infinity gives its values e = 120 (E4M3; its own code is NaN) or 113 (E5M2, an infinity).
@@ -139,7 +140,8 @@ typedef struct {
  * y[i][j] = sum over blocks q of 128 of 2^(ea[q][i] + eb[q][j]) * sum over l in q of a[i][l] * b[j][l], summed in float32, rounded once.
  * Float32 results: the products are exact and their sums float32's.  Bfloat16 results: the 8-bit matrix instruction adds products in
  * eights and cuts them off 13 bits below the largest one's first, so a result is off by up to 2^-10 of the sum of its terms'
- * magnitudes before it is rounded (about 1e-5 of itself in practice; the rounding is up to 2^-8).
+ * magnitudes before it is rounded (about 1e-5 of itself in practice; the rounding is up to 2^-8).  Where a sum on the way is beyond the
+ * largest float32, the result is an infinity of either sign or a NaN.
  * a_dev, b_dev 16-byte aligned; scales as accept_block_quantize lays them.  workspace_dev: accept_matmul_workspace_size bytes, 16-byte
  * aligned (null where that is 0).
  */

@@ -31,7 +31,11 @@ struct MatmulArgs {
 //
 // Results in float32 (EXACT true): that would be 100 times a float32's rounding.  The codes are converted to bfloat16, scale
 // and all, which is exact (4 bits and a power of two; two values an instruction), and go through four 16-bit matrix
-// instructions, which add in float32: 5e-9 and 5e-8 on the same operands, at half the instructions' rate.
+// instructions, which add in float32: 5e-9 and 5e-8 on the same operands, at half the instructions' rate.  Only the largest codes times
+// the largest scales are beyond bfloat16 (E4M3: 256 and more at 2^120; E5M2: from 2^113 on), where the other operand's scale may still
+// bring the products back.  They become infinities, which no later addition takes away: where a sum is not finite in the end, the
+// blocks are gone through once more, as bare codes, each block's sums take both scales (add_scaled), and that result takes the place of
+// this one (no other: a result does not depend on other rows).  It costs a product without infinities 64 instructions a tile.
 typedef __bf16 v8b_t __attribute__((ext_vector_type(8)));
 typedef __bf16 v2b_t __attribute__((ext_vector_type(2)));
 
@@ -110,6 +114,42 @@ __device__ __forceinline__ void multiply_in_place(const Fragment<false>& b, cons
 __device__ __forceinline__ void written_out(v4f_t (&sum)[8]) {
   asm volatile("s_nop 15\n\ts_nop 15"
                : "+a"(sum[0]), "+a"(sum[1]), "+a"(sum[2]), "+a"(sum[3]), "+a"(sum[4]), "+a"(sum[5]), "+a"(sum[6]), "+a"(sum[7]));
+}
+
+constexpr int kScaleOne = 127;
+template <int MI, int NI>
+__device__ __forceinline__ bool all_finite(const v4f_t (&sum)[MI][NI]) {
+  float zero = 0.0f;
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NI; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) zero = fmaf(sum[i][j][r], 0.0f, zero);
+  return zero == 0.0f;
+}
+template <int MI, int NI>
+__device__ __forceinline__ void where_not_finite(v4f_t (&sum)[MI][NI], const v4f_t (&other)[MI][NI]) {
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NI; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sum[i][j][r] = fmaf(sum[i][j][r], 0.0f, 0.0f) == 0.0f ? sum[i][j][r] : other[i][j][r];
+}
+template <int MI, int NI>
+__device__ __forceinline__ void put_to_zero(v4f_t (&sum)[MI][NI]) {
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NI; ++j) sum[i][j] = v4f_t{0, 0, 0, 0};
+}
+// A block's sums of bare codes, times 2^(ea + eb - 254), added to `sum`.  ea, the byte of row lane%16 of a; eb, that of row lane%16 of b: a
+// lane's four results are of b's rows 4*(lane/16) on.
+__device__ __forceinline__ v4f_t add_scaled(v4f_t sum, v4f_t part, int ea, int eb) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) sum[r] += __builtin_ldexpf(part[r], ea + __shfl(eb, threadIdx.x % kWave / 16 * 4 + r, kWave) - 2 * kScaleOne);
+  return sum;
 }
 
 // 16 codes with those from `left` on put to zero, whatever they are.
@@ -430,29 +470,52 @@ __global__ __launch_bounds__(4 * kWave, 2) void matmul_exact_kernel(const Matmul
       unrolled<0, S>([&](auto j) { sum[i.value][j.value] = multiply<ACODE, BCODE, 0, 0>(fb[j.value], fa, sum[i.value][j.value], 0, 0); });
     });
   };
-  int block = loads.first;
-  if (block < loads.whole) {
-    const auto or_last = [&](int b) { return b < loads.whole ? b : loads.whole - 1; };
-    loads.fetch(block, tile0);
-    loads.arrive(scales0);
-#pragma unroll 1
-    for (; block + 1 < loads.whole; block += 2) {
-      loads.fetch(block + 1, tile1);
-      work(tile0, scales0);
-      loads.arrive(scales1);
-      loads.fetch(or_last(block + 2), tile0);
-      work(tile1, scales1);
+  v4f_t far[S][S];
+  auto bare = [&](const uint8_t* tile, const uint32_t* scales) {
+    const uint8_t* const ta = tile + wm * S * 16 * kQBlock;
+    const uint8_t* const tb = tile + (kSide + wn * S * 16) * kQBlock;
+    const int sa = int(scales[wm * 16 + lane % 16]), sb = int(scales[kSide / 4 + wn * 16 + lane % 16]);
+    unrolled<0, S>([&](auto i) {
+      const Fragment<true> fa = fragment_of<ACODE>(codes_of(ta + i.value * 16 * kQBlock, lane), kScaleOne, Int<1>{});
+      unrolled<0, S>([&](auto j) {
+        const Fragment<true> fb = fragment_of<BCODE>(codes_of(tb + j.value * 16 * kQBlock, lane), kScaleOne, Int<1>{});
+        const v4f_t part = multiply<ACODE, BCODE, 0, 0>(fb, fa, v4f_t{0, 0, 0, 0}, 0, 0);
+        far[i.value][j.value] = add_scaled(far[i.value][j.value], part, sa >> (8 * i.value) & 255, sb >> (8 * j.value) & 255);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    });
+  };
+  auto walk = [&](const auto& work) {
+    int block = loads.first;
+    if (block < loads.whole) {
+      const auto or_last = [&](int b) { return b < loads.whole ? b : loads.whole - 1; };
+      loads.fetch(block, tile0);
       loads.arrive(scales0);
+#pragma unroll 1
+      for (; block + 1 < loads.whole; block += 2) {
+        loads.fetch(block + 1, tile1);
+        work(tile0, scales0);
+        loads.arrive(scales1);
+        loads.fetch(or_last(block + 2), tile0);
+        work(tile1, scales1);
+        loads.arrive(scales0);
+      }
+      if (block < loads.whole) work(tile0, scales0), ++block;
+      __syncthreads();
     }
-    if (block < loads.whole) work(tile0, scales0), ++block;
+    if (block < loads.last) {
+      loads.fetch_short(block, tile0);
+      loads.arrive(scales0);
+      work(tile0, scales0);
+    }
     __syncthreads();
+  };
+  walk(work);
+  if (__syncthreads_or(!all_finite(sum))) {
+    put_to_zero(far);
+    walk(bare);
+    where_not_finite(sum, far);
   }
-  if (block < loads.last) {
-    loads.fetch_short(block, tile0);
-    loads.arrive(scales0);
-    work(tile0, scales0);
-  }
-  __syncthreads();
   constexpr int kFloats = 16 * (S * 16 + 4);
   put_tile<float>(args, loads.split, reinterpret_cast<float*>(tile0) + loads.wave * kFloats, lane, loads.m0 + wm * S * 16, loads.n0 + wn * S * 16, sum);
 }
@@ -534,7 +597,8 @@ __global__ __launch_bounds__(kFewWaves* kWave) void matmul_few_kernel(const Matm
     load(l, block);
     add(l);
   }
-  if (block < last) {  // the incomplete one
+  // the incomplete one
+  auto load_last = [&](Loaded& l, int block) {
     const int64_t col = int64_t(block) * kQBlock;
     const int left = int(args.k - col) - lane / 16 * 32;
     auto load_short = [&](const uint8_t* p) {
@@ -543,7 +607,6 @@ __global__ __launch_bounds__(kFewWaves* kWave) void matmul_few_kernel(const Matm
       if (left > 16) hi = first_codes(load16(p + col + 16), left - 16);
       return codes(lo, hi);
     };
-    Loaded l;
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
       l.b[j] = load_short(b[j]);
@@ -554,7 +617,32 @@ __global__ __launch_bounds__(kFewWaves* kWave) void matmul_few_kernel(const Matm
       l.a[i] = load_short(a[i]);
       l.scale_a[i] = sa[i][block * args.sa_rows];
     }
+  };
+  if (block < last) {
+    Loaded l;
+    load_last(l, block);
     add(l);
+  }
+  if constexpr (EXACT) {
+    if (__any(!all_finite(sum))) {  // this wavefront's blocks once more, as bare codes
+      v4f_t far[MT][NT];
+      put_to_zero(far);
+#pragma unroll 1
+      for (block = first + wave; block < last; block += kFewWaves) {
+        Loaded l;
+        if (block < whole) load(l, block);
+        else load_last(l, block);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int j = 0; j < NT; ++j) {
+            const Fragment<true> fa = fragment_of<ACODE>(l.a[i], kScaleOne, Int<1>{}), fb = fragment_of<BCODE>(l.b[j], kScaleOne, Int<1>{});
+            far[i][j] = add_scaled(far[i][j], multiply<ACODE, BCODE, 0, 0>(fb, fa, v4f_t{0, 0, 0, 0}, 0, 0), l.scale_a[i], l.scale_b[j]);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+      }
+      where_not_finite(sum, far);
+    }
   }
 #pragma unroll
   for (int i = 0; i < MT; ++i)
