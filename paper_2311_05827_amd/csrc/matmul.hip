@@ -99,23 +99,6 @@ __device__ __forceinline__ v4f_t multiply(const Fragment<true>& b, const Fragmen
   return sum;
 }
 
-// The same with the sums where they are, in an accumulation register.  The compiler gives results registers of their own, which leaves a
-// wavefront that holds 256 of them copying sums at every other instruction; tied, nothing moves.  Nor does it know the instruction's waits:
-// two instructions' issues after a vector instruction that wrote an operand (here, in the shadow of the one before), and see
-// written_out.
-template <int ACODE, int BCODE, int SUB_A, int SUB_B>
-__device__ __forceinline__ void multiply_in_place(const Fragment<false>& b, const Fragment<false>& a, v4f_t& sum, int scale_b, int scale_a) {
-  asm volatile("s_nop 1\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[%5,%6,0] op_sel_hi:[%7,%8,0] cbsz:%9 blgp:%10"
-               : "+a"(sum)
-               : "v"(b.codes), "v"(a.codes), "v"(scale_b), "v"(scale_a), "n"(SUB_B & 1), "n"(SUB_A & 1), "n"(SUB_B / 2), "n"(SUB_A / 2),
-                 "n"(BCODE), "n"(ACODE));
-}
-// Eight sums, after the time that the longest matrix instruction takes to write its results (18 instructions' issues).
-__device__ __forceinline__ void written_out(v4f_t (&sum)[8]) {
-  asm volatile("s_nop 15\n\ts_nop 15"
-               : "+a"(sum[0]), "+a"(sum[1]), "+a"(sum[2]), "+a"(sum[3]), "+a"(sum[4]), "+a"(sum[5]), "+a"(sum[6]), "+a"(sum[7]));
-}
-
 constexpr int kScaleOne = 127;
 template <int MI, int NI>
 __device__ __forceinline__ bool all_finite(const v4f_t (&sum)[MI][NI]) {
@@ -192,7 +175,7 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
 // all loads: the compiler, where it knows of more such loads than it can tell apart, waits for all of them before every read of
 // shared memory, here for the block after the next one.
 __device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t offset, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(offset), "s"(base) : "memory");  // (m0 has no other use here)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(offset), "s"(base) : "memory");  // (m0 is reserved: the compiler keeps nothing in it)
 }
 
 // A workgroup's tile, and its loads of one block: 8 rows of 128 codes a wavefront and load, a byte of scale a thread and turn.
@@ -370,8 +353,7 @@ __global__ __launch_bounds__(4 * kWave, S == 8 ? 1 : 2) void matmul_tile_kernel(
     for (int i = 0; i < S / 4; ++i) ma[i] = sa[i], mb[i] = sb[i];
     auto product = [&](auto i, auto j) {
       v4f_t& to = sum[i.value][j.value];
-      if constexpr (S == 8) multiply_in_place<ACODE, BCODE, i.value % 4, j.value % 4>(fb[j.value], fa[i.value], to, mb[j.value / 4], ma[i.value / 4]);
-      else to = multiply<ACODE, BCODE, i.value % 4, j.value % 4>(fb[j.value], fa[i.value], to, mb[j.value / 4], ma[i.value / 4]);
+      to = multiply<ACODE, BCODE, i.value % 4, j.value % 4>(fb[j.value], fa[i.value], to, mb[j.value / 4], ma[i.value / 4]);
     };
     unrolled<0, S - 1>([&](auto r) {
       if constexpr (r.value + 2 < S) read(tile, Int<r.value + 2>{});
@@ -380,7 +362,11 @@ __global__ __launch_bounds__(4 * kWave, S == 8 ? 1 : 2) void matmul_tile_kernel(
         product(r, j);
         if constexpr (j.value < r.value) product(j, r);
         constexpr int load = kHalf + r.value * (r.value + 1) / 2 + j.value;  // after 1, 2, 4, 6, ... products
-        if constexpr (more.value && load < 2 * S) loads.template fetch_some<load, load + 1>(soon, next_tile);
+        if constexpr (more.value && load < 2 * S) {
+          __builtin_amdgcn_sched_barrier(0);
+          loads.template fetch_some<load, load + 1>(soon, next_tile);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       });
       __builtin_amdgcn_sched_barrier(0);
     });
@@ -401,38 +387,75 @@ __global__ __launch_bounds__(4 * kWave, S == 8 ? 1 : 2) void matmul_tile_kernel(
     unrolled<2, S>([&](auto j) {
       product(r, j);
       if constexpr (j.value < r.value) product(j, r);
-      if constexpr (more.value) loads.template fetch_some<j.value, j.value + 1>(after, tile);
+      if constexpr (more.value) {
+        __builtin_amdgcn_sched_barrier(0);
+        loads.template fetch_some<j.value, j.value + 1>(after, tile);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     });
     __builtin_amdgcn_sched_barrier(0);
   };
 
   int block = loads.first;
-  if (block < loads.whole) {
-    // the one after the last is the last again, so that nothing branches between the instructions
-    const auto or_last = [&](int b) { return b < loads.whole ? b : loads.whole - 1; };
+  // the one after the last is the last again, so that nothing branches between the instructions
+  const auto or_last = [&](int b) { return b < loads.whole ? b : loads.whole - 1; };
+  auto first_blocks = [&] {
     loads.fetch(block, tile0);
     loads.arrive(scales0);
     loads.fetch_scales(or_last(block + 1));
     loads.template fetch_some<0, kHalf>(or_last(block + 1), tile1);
     begin(tile0, scales0);
+  };
+  if constexpr (S == 4) {
+    if (block < loads.whole) {
+      first_blocks();
 #pragma unroll 1
-    for (; block + 1 < loads.whole; block += 2) {
-      work(Int<1>{}, tile0, tile1, scales1, block + 1, or_last(block + 2));
-      work(Int<1>{}, tile1, tile0, scales0, or_last(block + 2), or_last(block + 3));
+      for (; block + 1 < loads.whole; block += 2) {
+        work(Int<1>{}, tile0, tile1, scales1, block + 1, or_last(block + 2));
+        work(Int<1>{}, tile1, tile0, scales0, or_last(block + 2), or_last(block + 3));
+      }
+      if (block < loads.whole) work(Int<0>{}, tile0, tile1, scales1, 0, 0), ++block;
+      __builtin_amdgcn_s_waitcnt(0);
+      __syncthreads();
     }
-    if (block < loads.whole) work(Int<0>{}, tile0, tile1, scales1, 0, 0), ++block;
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-  }
-  if (block < loads.last) {
-    loads.fetch_short(block, tile0);
-    loads.arrive(scales0);
-    begin(tile0, scales0);
-    work(Int<0>{}, tile0, tile1, scales1, 0, 0);
-  }
-  if constexpr (S == 8) {
-#pragma unroll
-    for (int i = 0; i < S; ++i) written_out(sum[i]);
+    if (block < loads.last) {
+      loads.fetch_short(block, tile0);
+      loads.arrive(scales0);
+      begin(tile0, scales0);
+      work(Int<0>{}, tile0, tile1, scales1, 0, 0);
+    }
+  } else {
+    // The sums fill all 256 accumulation registers.  With one body for all blocks but the last, and one for the last and the
+    // incomplete one, each stays where it is; with a body for each place a block's rows can lie in, as above, the compiler has 130
+    // registers of them change places in every block.
+    uint8_t *here = tile0, *there = tile1;
+    uint32_t *scales_here = scales0, *scales_there = scales1;
+    if (block < loads.whole) {
+      first_blocks();
+#pragma unroll 1
+      for (; block + 1 < loads.whole; ++block) {
+        work(Int<1>{}, here, there, scales_there, block + 1, or_last(block + 2));
+        uint8_t* const tile = here;
+        here = there, there = tile;
+        uint32_t* const scales = scales_here;
+        scales_here = scales_there, scales_there = scales;
+      }
+    } else {
+      loads.fetch_short(block, here);
+      loads.arrive(scales_here);
+      begin(here, scales_here);
+    }
+#pragma unroll 1
+    for (;;) {
+      work(Int<0>{}, here, there, scales_there, 0, 0);
+      // loads that nothing uses may still be on their way to `there`
+      __builtin_amdgcn_s_waitcnt(0);
+      if (++block >= loads.last) break;
+      __syncthreads();
+      loads.fetch_short(block, here);
+      loads.arrive(scales_here);
+      begin(here, scales_here);
+    }
   }
   __syncthreads();
   constexpr int kFloats = 16 * (S * 16 + 4);  // of a wavefront's rows on their way out
