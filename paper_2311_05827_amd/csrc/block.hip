@@ -22,7 +22,7 @@ struct BlockArgs {
 template <typename T>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const BlockArgs a) {
   constexpr int VEC = Elem<T>::VEC, LANES = kQBlock / VEC, kBlocks = 2;
-  const int64_t row = int64_t(blockIdx.x) * (256 / LANES) + threadIdx.x / LANES;
+  const int64_t row = (int64_t(blockIdx.z) * gridDim.x + blockIdx.x) * (256 / LANES) + threadIdx.x / LANES;
   if (row >= a.rows) return;  // whole groups of lanes
   const T* const x = static_cast<const T*>(a.x) + row * a.x_stride;
   for (int64_t first = int64_t(blockIdx.y) * kBlocks; first < a.col_blocks; first += int64_t(gridDim.y) * kBlocks) {
@@ -74,7 +74,9 @@ __global__ __launch_bounds__(256) void quantize_square_kernel(const BlockArgs a)
   __shared__ float most[4][kQBlock];
   __shared__ __align__(16) uint8_t turned[COLS ? kQBlock * (kQBlock + kPad) : 16];
   const int t = threadIdx.x, cx = t % 16, ry = t / 16, wave = t / kWave;
-  const int64_t rb = blockIdx.x / a.col_blocks, cb = blockIdx.x % a.col_blocks;
+  const uint32_t square = blockIdx.y * gridDim.x + blockIdx.x, col_blocks = uint32_t(a.col_blocks);
+  if (square >= uint32_t(a.row_blocks) * col_blocks) return;  // the whole workgroup
+  const int64_t rb = square / col_blocks, cb = square % col_blocks;
   const int64_t row0 = rb * kQBlock + 8 * ry, col0 = cb * kQBlock + 8 * cx;
   float f[8][8];
   if (a.cols >= 8) {  // the same in all lanes
@@ -183,11 +185,12 @@ template <typename T>
 hipError_t quantize(const BlockArgs& a, int group, hipStream_t s) {
   if (group == 1 && !a.codes_t) {
     constexpr int kRows = 256 / (kQBlock / Elem<T>::VEC);
-    const int64_t turns = blocks_of(a.col_blocks, 2), y = turns < 65535 ? turns : 65535;
-    quantize_rows_kernel<T><<<dim3(uint32_t(blocks_of(a.rows, kRows)), uint32_t(y)), 256, 0, s>>>(a);
+    const int64_t turns = blocks_of(a.col_blocks, 2), y = turns < 65535 ? turns : 65535, groups = blocks_of(a.rows, kRows);
+    quantize_rows_kernel<T><<<dim3(grid_x(groups), uint32_t(y), grid_rest(groups)), 256, 0, s>>>(a);
     return hipGetLastError();
   }
-  const dim3 grid = dim3(uint32_t(a.row_blocks * a.col_blocks));  // (at most 2^26 by the limits on sizes)
+  const int64_t squares = a.row_blocks * a.col_blocks;  // (below 2^27 by the limits on sizes)
+  const dim3 grid = dim3(grid_x(squares), grid_rest(squares));
   if (group == 1) {
     if (a.codes) quantize_square_kernel<T, 1, true, true><<<grid, 256, 0, s>>>(a);
     else quantize_square_kernel<T, 1, false, true><<<grid, 256, 0, s>>>(a);

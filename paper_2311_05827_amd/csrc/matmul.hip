@@ -760,6 +760,29 @@ hipError_t by_code(int a_code, int b_code, const MatmulArgs& a, const MatmulPlan
   return b_code == ACCEPT_E4M3 ? run<1, 0, TO, EXACT>(a, p, s) : run<1, 1, TO, EXACT>(a, p, s);
 }
 
+// One part.  The kernel for few rows has its columns in the grid's x and its rows, 64 at a time, in z: what is beyond a launch goes into
+// another.  (The tiles never are: 2^24 of 128 x 128 have more results than the memory.)
+template <typename TO, bool EXACT>
+hipError_t in_launches(int a_code, int b_code, const MatmulArgs& a, const MatmulPlan& p, hipStream_t s) {
+  constexpr int64_t kRows = int64_t(1) << 21, kCols = kGridX * 16;
+  const bool whole = p.tile >= kTile128 || (a.m <= kRows && a.n <= kCols);
+  if (whole) return by_code<TO, EXACT>(a_code, b_code, a, p, s);
+  for (int64_t row = 0; row < a.m; row += kRows)
+    for (int64_t col = 0; col < a.n; col += kCols) {
+      MatmulArgs c = a;
+      c.m = int(a.m - row < kRows ? a.m - row : kRows);
+      c.n = int(a.n - col < kCols ? a.n - col : kCols);
+      c.a += row * a.a_stride;
+      c.sa += row >> a.sa_shift;
+      c.b += col * a.b_stride;
+      c.sb += col >> a.sb_shift;
+      c.y = static_cast<TO*>(a.y) + row * a.y_stride + col;
+      const hipError_t e = by_code<TO, EXACT>(a_code, b_code, c, p, s);
+      if (e != hipSuccess) return e;
+    }
+  return hipSuccess;
+}
+
 template <typename TO>
 hipError_t join(const MatmulArgs& a, const void* parts, int splits, void* y, hipStream_t s) {
   const int64_t want = blocks_of(int64_t(a.m) * a.n, 1024);
@@ -833,7 +856,7 @@ hipError_t launch_matmul(const accept_matmul_desc& d, const MatmulPlan& p, const
   if (d.k == 0) return f32 ? join<float>(g, nullptr, 0, y, s) : join<bf16_t>(g, nullptr, 0, y, s);
   if (p.splits == 1) {
     g.y = y;
-    return f32 ? by_code<float, true>(d.a_code, d.b_code, g, p, s) : by_code<bf16_t, false>(d.a_code, d.b_code, g, p, s);
+    return f32 ? in_launches<float, true>(d.a_code, d.b_code, g, p, s) : in_launches<bf16_t, false>(d.a_code, d.b_code, g, p, s);
   }
   g.y = ws;
   g.y_stride = d.n;

@@ -398,7 +398,7 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const float* partials, 
   void* const to = blockIdx.y ? dbias : dweight;
   if (!to) return;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const int64_t col = int64_t(blockIdx.x) * kWave + lane;
+  const int64_t col = (int64_t(blockIdx.z) * gridDim.x + blockIdx.x) * kWave + lane;
   float sum = 0.0f;
   if (col < cols)
 #pragma unroll 16
@@ -573,8 +573,9 @@ hipError_t launch_norm_backward(const accept_norm_desc& d, const NormPlan& p, co
     if (e != hipSuccess) return e;
   }
   if (!a.partials) return hipSuccess;
-  norm_join_kernel<<<dim3(uint32_t(blocks_of(d.cols, kWave)), 2), 1024, 0, s>>>(a.partials, records, d.cols, dweight, dbias,
-                                                                               a.param_bf16);
+  const int64_t groups = blocks_of(d.cols, kWave);
+  norm_join_kernel<<<dim3(grid_x(groups), 2, grid_rest(groups)), 1024, 0, s>>>(a.partials, records, d.cols, dweight, dbias,
+                                                                              a.param_bf16);
   return hipGetLastError();
 }
 

@@ -11,6 +11,11 @@ constexpr int kMinExponent = -100;   // of a scale
 
 inline int64_t up_to(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 inline int64_t blocks_of(int64_t v, int64_t by) { return (v + by - 1) / by; }
+// Workgroups in a launch's x: a launch takes fewer than 2^32 threads in a dimension, so where there are more workgroups than
+// this, another dimension has the rest (65535 at most).
+constexpr int64_t kGridX = int64_t(1) << 21;
+inline uint32_t grid_x(int64_t groups) { return uint32_t(groups < kGridX ? groups : kGridX); }
+inline uint32_t grid_rest(int64_t groups) { return uint32_t(blocks_of(groups, kGridX)); }
 
 struct NormPlan {
   int back_grid;  // workgroups of the backward pass = number of partial column sums
