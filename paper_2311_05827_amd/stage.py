@@ -89,6 +89,11 @@ def quantize_weight(weight, colwise):
     return S.accept_block_quantize(_block_desc(w.shape[0], w.shape[1], group=S.BLOCK, in_dtype=B.dtype_code(w)), w, colwise=colwise)
 
 
+def _version(t):
+    """Counts the changes that PyTorch sees (a tensor made in inference mode has no count)."""
+    return None if t.is_inference() else t._version
+
+
 class BlockLinear(torch.nn.Module):
     """y = x w^T with x and w in 8-bit blocks (see the module's text).  The weight is kept in float32 (or bfloat16) for the
     optimizer and quantized in every call, unless it was laid out for serving: see `freeze`."""
@@ -100,23 +105,40 @@ class BlockLinear(torch.nn.Module):
         self._frozen = None
 
     def freeze(self):
-        """Keep the codes of the weight as it is now for the calls without gradients that follow.  A later change of the weight
-        takes another `freeze`, or `unfreeze`; calls with gradients always use the weight itself."""
-        self._frozen = quantize_weight(self.weight, colwise=False)[:2]
+        """Keep the codes of the weight as it is now for the calls without gradients that follow, until the weight changes: by an
+        optimizer, `load_state_dict`, `to`, another parameter in its place or any other way that PyTorch counts, or by a call that
+        will have a gradient for it.  From then on it is quantized in every call again.  A change behind PyTorch's back (`weight.data`)
+        takes another `freeze`, or `unfreeze`."""
+        self._frozen = (self.weight, _version(self.weight), quantize_weight(self.weight, colwise=False)[:2])
         return self
 
     def unfreeze(self):
         self._frozen = None
         return self
 
+    def _apply(self, fn, recurse=True):
+        self._frozen = None  # `to` and its like put other data into the parameter without a count
+        return super()._apply(fn, recurse)
+
+    def _weight_codes(self):
+        frozen = self._frozen
+        if frozen is not None:
+            weight, version, codes = frozen
+            if weight is self.weight and version == _version(weight):
+                return codes
+            self._frozen = None
+        return quantize_weight(self.weight, colwise=False)[:2]
+
     def serve(self, codes, scales, out_dtype):
         """The product of codes (m, in_features), without gradients."""
         (m, k), n = codes.shape, self.weight.shape[0]
-        w, ws = self._frozen or quantize_weight(self.weight, colwise=False)[:2]
+        w, ws = self._weight_codes()
         return S.accept_block_matmul(_matmul_desc(m, n, k, out_dtype=out_dtype), codes, scales, w, ws)
 
     def forward(self, x):
         if torch.is_grad_enabled():
+            if self.weight.requires_grad:
+                self._frozen = None  # (an optimizer's fused step is not counted)
             return _BlockLinear.apply(x, self.weight)
         flat = _flat(x)
         codes, scales, _, _ = S.accept_block_quantize(_block_desc(*flat.shape, in_dtype=B.dtype_code(flat)), flat)
