@@ -50,8 +50,8 @@ def train(tokens, hidden, inner, steps, dtype=torch.bfloat16, seed=0, say=print)
 @torch.no_grad()
 def serve(entry, out, tokens, dtype=torch.bfloat16):
     """One token after the other through the stage, its weights laid out once."""
-    entry.linear.freeze()
-    out.freeze()
+    entry.eval().linear.freeze()
+    out.eval().freeze()
     return torch.cat([out(torch.relu(entry(t[None]))) for t in tokens.to(dtype)])
 
 

@@ -7,7 +7,7 @@ which operand:
 * ``layer_norm(x, weight, bias)``: the statistics are saved for the backward pass.
 * ``BlockLinear``: y = x w^T with both operands in E4M3 blocks of 128.  x is quantized once, along its rows for y and along its
   columns for the weight's gradient; the weight once, in squares, for y and for x's gradient; the incoming gradient once, in E5M2, along its rows (dx = dy w) and along its columns (dw = dy^T x, in float32).
-* ``NormLinear``: the two behind each other; without gradients the norm writes the product's codes itself.
+* ``NormLinear``: the two behind each other; in evaluation mode without gradients the norm writes the product's codes itself.
 """
 from __future__ import annotations
 
@@ -146,8 +146,9 @@ class BlockLinear(torch.nn.Module):
 
 
 class NormLinear(torch.nn.Module):
-    """A block's entry: layer norm, then a product.  Where no gradient is asked for, the norm writes its output as the
-    product's codes, and no float of it is ever stored."""
+    """A block's entry: layer norm, then a product.  In evaluation mode (`eval`), where no gradient is asked for, the norm writes its
+    output as the product's codes, and no float of it is ever stored.  In training mode the norm's output is rounded to x's type first
+    with and without gradients: a pass that is computed again for its gradients, as in activation checkpointing, gives the same bits."""
 
     def __init__(self, in_features, out_features, eps=1e-5, device="cuda", dtype=torch.float32):
         super().__init__()
@@ -157,7 +158,7 @@ class NormLinear(torch.nn.Module):
         self.eps = eps
 
     def forward(self, x):
-        if torch.is_grad_enabled():
+        if self.training or torch.is_grad_enabled():
             return self.linear(layer_norm(x, self.norm_weight, self.norm_bias, self.eps))
         flat = _flat(x)
         code = B.dtype_code(flat)
