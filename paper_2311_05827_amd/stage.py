@@ -142,7 +142,7 @@ class BlockLinear(torch.nn.Module):
             return _BlockLinear.apply(x, self.weight)
         flat = _flat(x)
         codes, scales, _, _ = S.accept_block_quantize(_block_desc(*flat.shape, in_dtype=B.dtype_code(flat)), flat)
-        return self.serve(codes, scales, B.dtype_code(flat)).view(*x.shape[:-1], -1)
+        return self.serve(codes, scales, B.dtype_code(flat)).view(*x.shape[:-1], self.weight.shape[0])
 
 
 class NormLinear(torch.nn.Module):
@@ -164,4 +164,4 @@ class NormLinear(torch.nn.Module):
         code = B.dtype_code(flat)
         desc = _norm_desc(*flat.shape, x_dtype=code, param_dtype=B.dtype_code(self.norm_weight), eps=self.eps)
         codes, scales, _ = S.accept_layer_norm_quantize(desc, flat, self.norm_weight, self.norm_bias)
-        return self.linear.serve(codes, scales, code).view(*x.shape[:-1], -1)
+        return self.linear.serve(codes, scales, code).view(*x.shape[:-1], self.linear.weight.shape[0])
