@@ -39,6 +39,7 @@ class _LayerNorm(torch.autograd.Function):
         y, stats = S.accept_layer_norm(desc, flat, weight, bias)
         ctx.save_for_backward(flat, weight, stats)
         ctx.desc = desc
+        ctx.shapes = [None if t is None else t.shape for t in (weight, bias)]
         return y.view(x.shape)
 
     @staticmethod
@@ -47,6 +48,7 @@ class _LayerNorm(torch.autograd.Function):
         x, weight, stats = ctx.saved_tensors
         dx, dweight, dbias = S.accept_layer_norm_backward(ctx.desc, _flat(dy), x, weight, stats,
                                                           need_weight=ctx.needs_input_grad[1], need_bias=ctx.needs_input_grad[2])
+        dweight, dbias = (g if g is None else g.view(shape) for g, shape in zip((dweight, dbias), ctx.shapes))
         return dx.view(dy.shape), dweight, dbias, None
 
 

@@ -48,3 +48,19 @@ def test_one_vector(A, name):
     x.requires_grad_(True)
     layer(x).sum().backward()
     assert x.grad.shape == (96,)
+
+
+@pytest.mark.parametrize("shape", [(96,), (1, 96), (1, 1, 96), (96, 1)])
+def test_gradients_have_their_parameters_shapes(A, shape):
+    """Weights and biases of as many elements as a row may be of any shape; so are their gradients."""
+    torch = torch_mod()
+    torch.manual_seed(1)
+    x, w, b, dy = (torch.randn(s, device="cuda") for s in ((5, 96), (96,), (96,), (5, 96)))
+    got = []
+    for s in ((96,), shape):
+        leaves = [x.clone().requires_grad_(True), w.clone().view(s).requires_grad_(True), b.clone().view(s).requires_grad_(True)]
+        A.stage.layer_norm(*leaves).backward(dy)
+        assert leaves[1].grad.shape == leaves[2].grad.shape == s
+        got.append([leaves[0].grad, *(t.grad.reshape(-1) for t in leaves[1:])])
+    for p, q in zip(*got):
+        assert torch.equal(p, q)
