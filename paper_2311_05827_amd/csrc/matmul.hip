@@ -747,8 +747,8 @@ hipError_t run(const MatmulArgs& a, const MatmulPlan& p, hipStream_t s) {
       if constexpr (EXACT) matmul_exact_kernel<4, ACODE, BCODE><<<tiles(128), 256, 0, s>>>(a);
       else matmul_tile_kernel<4, ACODE, BCODE, TO><<<tiles(128), 256, 0, s>>>(a);
       break;
-    default:
-      if constexpr (!EXACT) matmul_tile_kernel<8, ACODE, BCODE, TO><<<tiles(256), 256, 0, s>>>(a);
+    default:  // (bfloat16 results in one part)
+      if constexpr (!EXACT && sizeof(TO) == 2) matmul_tile_kernel<8, ACODE, BCODE, TO><<<tiles(256), 256, 0, s>>>(a);
       break;
   }
   return hipGetLastError();
