@@ -66,7 +66,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const BlockArgs a) {
 
 // A square of 128 x 128 per workgroup, held in registers: thread t has rows 8*(t/16) .. +7 and columns 8*(t%16) .. +7, so
 // a row's block lies in 16 neighbouring lanes, and a thread's part of a column is 8 bytes of codes.  The transposed codes
-// go through shared memory, to be written in whole lines.  Bound by memory: 8192 x 8192 float32 in squares, both ways, 78 us (5.1 TB/s);
+// go through shared memory, to be written in whole lines.  Bound by memory: 8192 x 8192 float32 in squares, both ways, 79 us (5.1 TB/s);
 // 8144 x 2048 bfloat16, both ways, 15.4 (4.3 TB/s), columns only 13.0, of which two are the launch and the first rows' way from memory.
 template <typename T, int GROUP, bool ROWS, bool COLS>
 __global__ __launch_bounds__(256) void quantize_square_kernel(const BlockArgs a) {

@@ -35,7 +35,8 @@ struct MatmulArgs {
 // the largest scales are beyond bfloat16 (E4M3: 256 and more at 2^120; E5M2: from 2^113 on), where the other operand's scale may still
 // bring the products back.  They become infinities, which no later addition takes away: where a sum is not finite in the end, the
 // blocks are gone through once more, as bare codes, each block's sums take both scales (add_scaled), and that result takes the place of
-// this one (no other: a result does not depend on other rows).  It costs a product without infinities 64 instructions a tile.
+// this one (no other: a result does not depend on other rows).  That costs a product without infinities 64 instructions a tile; one
+// with infinities or NaN of its own goes through its blocks twice.
 typedef __bf16 v8b_t __attribute__((ext_vector_type(8)));
 typedef __bf16 v2b_t __attribute__((ext_vector_type(2)));
 
@@ -310,9 +311,9 @@ __device__ __forceinline__ void put_tile(const MatmulArgs& args, int split, floa
 // them with those that it has, 1, 3, 5, ... products, while the rows after the next are on their way.  Before the last 2S-1 all
 // rows are in registers: there the workgroup meets, the block after the next is fetched into this one's place, and the next one's
 // first rows are read meanwhile, so the matrix instructions stop for the meeting only.  S = 8: tiles of 256 x 256, one wavefront a SIMD; S = 4:
-// 128 x 128, two workgroups a compute unit.  8192^3 in 411 us (2.68 PFLOP/s; the first form, all rows read before the first product and
-// two 128 x 128 tiles a compute unit, 612): the matrix units work 63 % of the cycles, 13 % go for waits at the meetings, about 9 %
-// for a tile's first loads and its results' way out, which overlap with nothing; the clock sinks to 1.9 GHz meanwhile.
+// 128 x 128, two workgroups a compute unit.  8192^3 in 414 us (2.66 PFLOP/s; the first form, all rows read before the first product and
+// two 128 x 128 tiles a compute unit, 612): the matrix units work 62 % of the cycles and the wavefronts wait 16 % of them, mostly for
+// a tile's first loads and its results' way out, which overlap with nothing; the clock sinks to 1.9 GHz meanwhile.
 template <int S, int ACODE, int BCODE, typename TO>
 __global__ __launch_bounds__(4 * kWave, S == 8 ? 1 : 2) void matmul_tile_kernel(const MatmulArgs args) {
   constexpr int kSide = 2 * S * 16;
@@ -465,7 +466,7 @@ __global__ __launch_bounds__(4 * kWave, S == 8 ? 1 : 2) void matmul_tile_kernel(
 
 // The 16-bit instructions: four wavefronts with S x S of 16 x 16 results each.  b's rows of a block are converted and held, a's
 // come 16 at a time, the next ones on their way while these are multiplied.  2048 x 768 over 8144 in five parts 32 us (0.8
-// PFLOP/s): the matrix units work 43 % of the cycles, the conversions take the issue of 128 instructions beside each 64.
+// PFLOP/s): the matrix units work 44 % of a compute unit's cycles, the conversions take the issue of 128 instructions beside each 64.
 template <int S, int ACODE, int BCODE>
 __global__ __launch_bounds__(4 * kWave, 2) void matmul_exact_kernel(const MatmulArgs args) {
   constexpr int kSide = 2 * S * 16;
@@ -545,9 +546,11 @@ __global__ __launch_bounds__(4 * kWave, 2) void matmul_exact_kernel(const Matmul
 
 // ---- few rows ---------------------------------------------------------------------------------
 // Bound by reading b.  A workgroup has 16 rows of b and 16*MT rows of a (nearly always all of them); its wavefronts take the blocks of
-// the contracted axis in turn, straight from memory into registers, AHEAD of a wavefront's at a time, and their sums are
-// added up in shared memory, in order.  One row by 8192 x 8192 14.1 us (4.8 TB/s), by 4096 x 4096 5.8 a call; 48 rows by 8192 x 2048 7.5, where a's
-// rows, read by every workgroup, take as many loads as b's.
+// the contracted axis in turn, straight from memory into registers, AHEAD of them without a branch between, and their sums are
+// added up in shared memory, in order.  One row by 8192 x 8192 14.1 us a call (4.8 TB/s), by 4096 x 4096 5.8, 48 rows by 8192 x 2048 7.5.  The small
+// ones are trips to memory in series: the compiler waits for a block's loads before its product and asks for the next block's after
+// that (one row of 4096: four trips; 48 rows: the second block's among the first's products), and as a lane takes 32 bytes next to each
+// other by two loads, each load touches all lines of its 16 rows for half of their bytes.
 constexpr int kFewWaves = 8;
 template <int MT, int NT, int ACODE, int BCODE, typename TO, bool EXACT>
 __global__ __launch_bounds__(kFewWaves* kWave) void matmul_few_kernel(const MatmulArgs args) {
@@ -801,6 +804,9 @@ hipError_t join(const MatmulArgs& a, const void* parts, int splits, void* y, hip
 //   Tiles: parts of 8 blocks (float32, 200 x 4096 x 1024: one part of 8 12.0 us, two of 4 13.6; 300 x 300 x 8192: 1 / 4 / 8 parts 63 / 23 / 17).
 //   256 x 256 where they are enough (us with tiles of 128 / 256: 4096^3 70.6 / 55.6, 8192 x 8192 x 1024 89.7 / 76.0, but 1024 x 8192 x
 //   8192, 128 large tiles, 64.2 / 99.7), else of 128 x 128.  Float32 results: 128 x 128.
+//   Not measured, or known to cost: large tiles a little beyond one for each compute unit take a second round for few of them (by 768: 8144 x 2048,
+//   256 tiles, 20 us, 8300 x 2048, 264 tiles, 32), and few results over an axis that is no two parts long are the walk of a few workgroups
+//   (128 x 128 over 1920: one, 9.7 us, float32 17.6).
 MatmulPlan make_matmul_plan(const accept_matmul_desc& d) {
   MatmulPlan p{};
   p.splits = p.few_n = 1;

@@ -109,10 +109,13 @@ __device__ __forceinline__ Place place_of(int col, int cols) {
   return {at, col - at};
 }
 
-// One row at a time per WAVES wavefronts, C vectors of it in a lane's registers and the next row's on their way: x is read
-// once, the variance is that of the differences.  Bound by memory: 8144 x 768 float32 8.2 us a call (6.1 TB/s, part of it in the memory-side
-// cache), 16384 x 4096 bfloat16 43.7 (6.1 TB/s), to codes 42.9; 1531 x 5003 bfloat16 9.2 (3.3 TB/s), two rows a workgroup one
-// after the other; one row of 4096 to codes 2.7 in the kernel: two trips to memory and two meetings of four wavefronts.
+// One row at a time per WAVES wavefronts, C vectors of it in a lane's registers and the next row's asked for before this one's sums: x is
+// read once, the variance is that of the differences.  Bound by memory: 8144 x 768 float32 8.2 us a call (6.1 TB/s, part of it in the
+// memory-side cache), 16384 x 4096 bfloat16 43.7 (6.1 TB/s), to codes 42.9; 1531 x 5003 bfloat16 9.2 (3.3 TB/s): two rows a workgroup, and
+// the second one's turn begins with a wait for all that is on its way, the first one's stores too (the compiler cannot tell there whether the
+// parameters have come); one row of 4096 to codes 2.6 in the kernel: two trips to memory and two meetings of four wavefronts.  Parameters in
+// bfloat16 come one vector after the other, each waited for (load_param widens them in the branch that loads them): 2 * C trips at
+// a kernel's start, where float32 ones are one.
 template <typename TX, typename TY, int WAVES, int C>
 __global__ __launch_bounds__(WAVES == 8 ? 512 : 256) void norm_kernel(const NormArgs a) {
   constexpr int VEC = Elem<TX>::VEC;
