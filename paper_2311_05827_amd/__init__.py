@@ -2,7 +2,8 @@
 
 The product is libaccept.so (HIP kernels behind a C ABI, see include/accept.h); this
 package holds its sources (csrc/), the build step (build.py) and a ctypes binding
-(binding.py; stage_binding.py for the stage operators of include/accept_stage.h).  The binding is imported lazily so that ``python -m
+(binding.py; stage_binding.py for the stage operators of include/accept_stage.h, attention_binding.py
+for those of include/accept_attention.h).  The binding is imported lazily so that ``python -m
 paper_2311_05827_amd.build`` works before the library exists.
 """
 import importlib
@@ -19,6 +20,12 @@ _STAGE_NAMES = (
     "accept_matmul_workspace_size", "accept_block_stride", "accept_layer_norm", "accept_layer_norm_quantize",
     "accept_layer_norm_backward", "accept_block_quantize", "accept_block_matmul", "E4M3", "E5M2",
 )
+_ATTENTION_NAMES = (
+    "RotateDesc", "AttentionDesc", "CacheDesc", "make_rotate_desc", "make_attention_desc", "make_cache_desc", "accept_rotate",
+    "accept_attention_workspace_size", "accept_attention", "accept_attention_backward_workspace_size", "accept_attention_backward",
+    "accept_cache_append", "accept_cache_workspace_size", "accept_cache_attention", "REST_KEPT", "REST_ZEROS", "ROTATE_HALVES",
+    "ROTATE_NEIGHBOURS",
+)
 
 
 def __getattr__(name):
@@ -32,6 +39,11 @@ def __getattr__(name):
     if name == "stage_binding" or name in _STAGE_NAMES:
         mod = importlib.import_module(__name__ + ".stage_binding")
         value = mod if name == "stage_binding" else getattr(mod, name)
+        globals()[name] = value
+        return value
+    if name == "attention_binding" or name in _ATTENTION_NAMES:
+        mod = importlib.import_module(__name__ + ".attention_binding")
+        value = mod if name == "attention_binding" else getattr(mod, name)
         globals()[name] = value
         return value
     raise AttributeError(name)

@@ -18,7 +18,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libaccept.so")
 NATIVE_PATH = os.path.join(HERE, "_native.so")  # csrc/native.cpp: the Python binding's calls
 SOURCES = ["api.hip", "uniform.hip", "uniform_chip_f32.hip", "uniform_chip_bf16.hip", "mbq.hip",
-           "stage_api.hip", "norm.hip", "block.hip", "matmul.hip"]
+           "stage_api.hip", "norm.hip", "block.hip", "matmul.hip",
+           "attention_api.hip", "rotate.hip", "attention.hip", "attention_back.hip", "cached.hip"]
 
 HIPCC_FLAGS = [
     "-O3",

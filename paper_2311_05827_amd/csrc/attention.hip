@@ -1,0 +1,213 @@
+// Attention over sequences: one pass over the keys with the running maximum and sum of a softmax.
+#include "attention.hpp"
+
+namespace accept {
+namespace {
+
+struct AttentionArgs {
+  const void* q;
+  const void* k;
+  const void* v;
+  void* o;
+  float* lse;
+  const int32_t* q_offsets;
+  const int32_t* k_offsets;
+  int64_t q_stride, k_stride, v_stride, o_stride;
+  int sequences, q_tokens, k_tokens, q_each, k_each;
+  int heads, group, head;
+  int tiles;      // of a head: at most so many
+  int causal, zeros;
+  float scale;    // times log2(e)
+};
+
+constexpr int kRows = 128;     // queries of a workgroup, 32 of a wavefront
+constexpr int kWaves = 4;
+// Sums are taken relative to a maximum that may be this much (in powers of two) behind the true one: results are put to a new
+// one only where it grows by more, once or twice a row instead of with every tile.  Sums stay below 2^8 times the
+// number of keys, and p has the same relative precision at any size.
+constexpr float kBehind = 8.0f;
+
+// A workgroup has 128 queries of a head, a wavefront 32 of them: as columns, so that a lane has a query of its own (its
+// maximum, sum and factor are the lane's, two lanes' together) and the weights come out of the first product in the registers that the second one
+// takes them from.  Tiles of keys and values come into shared memory one ahead.
+template <typename T, int DB>
+__global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) void attention_kernel(const AttentionArgs g) {
+  constexpr int NB = sizeof(T) == 2 ? 2 : 1, BN = 32 * NB;
+  constexpr int kTile = BN * Head<T, DB>::kRowBytes;
+  __shared__ __align__(16) uint8_t tiles[4 * kTile];  // keys, values; and the next ones
+  const int lane = threadIdx.x % kWave, wave = uniform(int(threadIdx.x / kWave));
+  const int half = lane / 32, column = lane % 32;
+  const HeadTile ht = deal(blockIdx.x, g.heads, g.tiles);
+  const int head = ht.head;
+
+  int seq = 0, tile = ht.tile;
+  if (g.q_offsets) {
+    const Found f = find_among(g.sequences, ht.tile, [&](int s) { return pieces(span_of(g.q_offsets, s, g.q_tokens, 0).size(), kRows); });
+    seq = uniform(f.seq);
+    tile = int(ht.tile - uniform(f.before));
+    if (seq < 0) {  // tiles that no sequence has: the tokens behind the last one
+      if (!g.zeros) return;
+      const int rest = rest_of(g.q_offsets, g.sequences, g.q_tokens);
+      const int parts = g.head * int(sizeof(T)) / 16;
+      for (int i = threadIdx.x; i < kRows * parts; i += kWaves * kWave) {
+        const int row = rest + tile * kRows + i / parts;
+        if (row >= g.q_tokens) break;
+        T* const to = static_cast<T*>(g.o) + row * g.o_stride + int64_t(head) * g.head;
+        reinterpret_cast<uint4*>(to)[i % parts] = make_uint4(0, 0, 0, 0);
+        if (g.lse && i % parts == 0) g.lse[int64_t(head) * g.q_tokens + row] = -INFINITY;
+      }
+      return;
+    }
+  } else {
+    const int each = pieces(g.q_each, kRows);
+    seq = ht.tile / each;
+    tile = ht.tile - seq * each;
+  }
+  const Span qs = span_of(g.q_offsets, seq, g.q_tokens, g.q_each), ks = span_of(g.k_offsets, seq, g.k_tokens, g.k_each);
+  const int rows = qs.size(), keys = ks.size();
+  const int more = keys - rows;  // query i sees keys up to i + more
+
+  const int row0 = tile * kRows + wave * 32, row = row0 + column;
+  const bool is_row = row < rows;
+  const auto seen_by = [&](int i) { return !g.causal ? keys : i + 1 + more < 0 ? 0 : i + 1 + more; };
+  const int last = rows - 1;
+  const int limit = seen_by(row < rows ? row : last);         // this lane's query sees keys before it
+  const int first_limit = row0 < rows ? seen_by(row0) : 0;    // all of the wavefront's queries do
+  const int wave_limit = row0 < rows ? seen_by(row0 + 31 < last ? row0 + 31 : last) : 0;
+  const int end = tile * kRows + kRows - 1;
+  const int steps = pieces(seen_by(end < last ? end : last), BN);
+
+  const int parts = g.head * int(sizeof(T)) / 16;
+  RowParts<T, DB> q;
+  q.load(static_cast<const T*>(g.q) + (qs.begin + (is_row ? row : last)) * g.q_stride + int64_t(head) * g.head, half, parts);
+  const T* const k0 = static_cast<const T*>(g.k) + ks.begin * g.k_stride + int64_t(head / g.group) * g.head;
+  const T* const v0 = static_cast<const T*>(g.v) + ks.begin * g.v_stride + int64_t(head / g.group) * g.head;
+  const TileRows<T, DB, BN, kWaves> k_rows(wave, lane, g.k_stride, parts), v_rows(wave, lane, g.v_stride, parts);
+  const auto fetch = [&](int step) {
+    uint8_t* const to = tiles + step % 2 * 2 * kTile;
+    k_rows.fetch(k0 + int64_t(step) * BN * g.k_stride, keys - step * BN, to);
+    v_rows.fetch(v0 + int64_t(step) * BN * g.v_stride, keys - step * BN, to + kTile);
+  };
+  if (g.head < DB * 32) {
+    clear_tiles<4 * kTile, kWaves * kWave>(tiles);
+    __syncthreads();
+  }
+
+  v16f_t acc[DB];
+  float largest, sum;
+  // A second time where a result is not finite, with products that keep away from a row what it does not see: zero times an
+  // infinity or NaN of a hidden value would not.
+  const auto run = [&](auto apart) {
+#pragma unroll
+    for (int db = 0; db < DB; ++db) acc[db] = v16f_t{};
+    largest = -INFINITY;
+    sum = 0.0f;
+    if (steps > 0) fetch(0);
+    for (int step = 0; step < steps; ++step) {
+      __builtin_amdgcn_s_waitcnt(0);
+      __syncthreads();
+      if (step + 1 < steps) fetch(step + 1);
+      const int key0 = step * BN;
+      if (key0 >= wave_limit) continue;
+      const uint8_t* const kt = tiles + step % 2 * 2 * kTile;
+      const uint8_t* const vt = kt + kTile;
+      v16f_t s[NB];
+      float most = -INFINITY;
+      const bool masked = key0 + BN > first_limit;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        s[nb] = rows_product<T, DB>(kt, nb * 32 + column, half, q);
+        if (masked) {
+          const int left = limit - key0 - nb * 32;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[nb][r] = result_row(r, half) < left ? s[nb][r] : -INFINITY;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) most = fmaxf(most, s[nb][r]);
+      }
+      most = halves_max(most) * g.scale;
+      if (__any(most > largest + kBehind)) {
+        const float now = fmaxf(largest, most);
+        const float factor = largest == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(largest - now);
+        largest = now;
+        sum *= factor;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) acc[db] *= factor;
+      }
+      const float base = largest == -INFINITY ? 0.0f : -largest;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        float p[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          p[r] = __builtin_amdgcn_exp2f(fmaf(s[nb][r], g.scale, base));
+          sum += p[r];
+        }
+        if (apart.value && masked) {
+          weighted_rows_apart<T, DB>(acc, vt, nb * 32, lane, p, bits_between(0, limit - key0 - nb * 32));
+        } else {
+          Weights<T> w;
+          set_weights(w, p);
+          weighted_rows<T, DB>(acc, vt, nb * 32, lane, w);
+        }
+      }
+    }
+  };
+  run(Flag<false>{});
+  if (__syncthreads_or(is_row && !finite_column<DB>(acc))) run(Flag<true>{});
+  sum = halves_sum(sum);
+  if (!is_row) return;
+  const int64_t token = qs.begin + row;
+  store_column<T, DB>(static_cast<T*>(g.o) + token * g.o_stride + int64_t(head) * g.head, acc, half, g.head, sum == 0.0f ? 0.0f : 1.0f / sum);
+  if (g.lse && half == 0)
+    g.lse[int64_t(head) * g.q_tokens + token] = sum == 0.0f ? -INFINITY : (largest + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
+template <typename T>
+hipError_t launch(const AttentionArgs& g, hipStream_t s) {
+  const int64_t groups = int64_t(g.heads) * g.tiles;
+  const dim3 grid(static_cast<uint32_t>(groups));
+  constexpr int kThreads = kWaves * kWave;
+  if (g.head <= 32) attention_kernel<T, 1><<<grid, kThreads, 0, s>>>(g);
+  else if (g.head <= 64) attention_kernel<T, 2><<<grid, kThreads, 0, s>>>(g);
+  else if (g.head <= 96) attention_kernel<T, 3><<<grid, kThreads, 0, s>>>(g);
+  else if (g.head <= 128) attention_kernel<T, 4><<<grid, kThreads, 0, s>>>(g);
+  else attention_kernel<T, 8><<<grid, kThreads, 0, s>>>(g);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+AttentionPlan make_attention_plan(const accept_attention_desc&) { return {0}; }
+
+hipError_t launch_attention(const accept_attention_desc& d, const AttentionPlan&, const void* q, const void* k, const void* v,
+                            const int32_t* q_offsets, const int32_t* k_offsets, void* o, float* lse, void*, hipStream_t s) {
+  AttentionArgs g{};
+  const int64_t whole = int64_t(d.heads) * d.head_size, kv_whole = int64_t(d.kv_heads) * d.head_size;
+  g.q = q;
+  g.k = k;
+  g.v = v;
+  g.o = o;
+  g.lse = lse;
+  g.q_offsets = q_offsets;
+  g.k_offsets = k_offsets;
+  g.q_stride = d.q_stride ? d.q_stride : whole;
+  g.k_stride = d.k_stride ? d.k_stride : kv_whole;
+  g.v_stride = d.v_stride ? d.v_stride : kv_whole;
+  g.o_stride = d.o_stride ? d.o_stride : whole;
+  g.sequences = int(d.sequences);
+  g.q_tokens = int(d.q_tokens);
+  g.k_tokens = int(d.k_tokens);
+  g.q_each = q_offsets || d.sequences == 0 ? 0 : int(d.q_tokens / d.sequences);
+  g.k_each = k_offsets || d.sequences == 0 ? 0 : int(d.k_tokens / d.sequences);
+  g.heads = d.heads;
+  g.group = d.heads / d.kv_heads;
+  g.head = d.head_size;
+  g.tiles = int(q_offsets ? blocks_of(d.q_tokens, kRows) + d.sequences : d.sequences * blocks_of(g.q_each, kRows));
+  g.causal = d.causal;
+  g.zeros = d.rest == ACCEPT_REST_ZEROS;
+  g.scale = float(d.scale * 1.4426950408889634074);
+  return d.dtype == ACCEPT_F32 ? launch<float>(g, s) : launch<bf16_t>(g, s);
+}
+
+}  // namespace accept

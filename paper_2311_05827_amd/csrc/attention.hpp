@@ -1,0 +1,366 @@
+// Internal declarations of the attention operators: rotation, attention with its gradients, the cache of pages.
+#pragma once
+
+#include "accept_attention.h"
+#include "pages.hpp"
+#include "stage.hpp"
+
+namespace accept {
+
+constexpr int64_t kMaxTokenStride = int64_t(1) << 22;  // elements: a tile's rows are told apart by 32 bits
+
+hipError_t launch_rotate(const accept_rotate_desc& d, const void* x, const float* frequencies, const int32_t* offsets,
+                         const int32_t* positions, void* y, hipStream_t s);
+hipError_t launch_cache_append(const accept_cache_desc& d, const void* q, const void* k, const void* v, const float* frequencies,
+                               const int32_t* offsets, const int32_t* lengths, const int32_t* positions, const int32_t* table,
+                               void* qo, void* k_cache, void* v_cache, hipStream_t s);
+struct AttentionPlan {
+  size_t bytes;  // workspace
+};
+AttentionPlan make_attention_plan(const accept_attention_desc& d);
+hipError_t launch_attention(const accept_attention_desc& d, const AttentionPlan& p, const void* q, const void* k, const void* v,
+                            const int32_t* q_offsets, const int32_t* k_offsets, void* o, float* lse, void* ws, hipStream_t s);
+struct AttentionBackPlan {
+  size_t bytes;
+};
+AttentionBackPlan make_attention_back_plan(const accept_attention_desc& d);
+hipError_t launch_attention_backward(const accept_attention_desc& d, const AttentionBackPlan& p, const void* dout, const void* q,
+                                     const void* k, const void* v, const void* o, const float* lse, const int32_t* q_offsets,
+                                     const int32_t* k_offsets, void* dq, void* dk, void* dv, void* ws, hipStream_t s);
+
+struct CachePlan {
+  int64_t items;  // at most so many pieces of 32 rows
+  int parts;      // of the work of a key head
+  size_t bytes;   // workspace
+};
+CachePlan make_cache_plan(const accept_cache_desc& d);
+hipError_t launch_cache_attention(const accept_cache_desc& d, const CachePlan& p, const void* q, const void* k_cache, const void* v_cache,
+                                  const int32_t* offsets, const int32_t* lengths, const int32_t* table, const uint64_t* tree, void* o,
+                                  void* ws, hipStream_t s);
+
+#if defined(__HIPCC__)
+
+__device__ __forceinline__ int pieces(int v, int of) { return (v + of - 1) / of; }
+
+template <bool B>
+struct Flag {
+  static constexpr bool value = B;
+};
+
+// ---- sequences ---------------------------------------------------------------------------------
+// First token and end of a sequence; whatever the offsets hold, inside 0 .. tokens.
+struct Span {
+  int begin, end;
+  __device__ __forceinline__ int size() const { return end - begin; }
+};
+__device__ __forceinline__ Span span_of(const int32_t* offsets, int s, int tokens, int each) {
+  if (!offsets) return {s * each, s * each + each};
+  int b = offsets[s], e = offsets[s + 1];
+  b = b < 0 ? 0 : b > tokens ? tokens : b;
+  e = e < b ? b : e > tokens ? tokens : e;
+  return {b, e};
+}
+// The tokens behind the last sequence begin here.
+__device__ __forceinline__ int rest_of(const int32_t* offsets, int sequences, int tokens) {
+  if (!offsets || sequences == 0) return offsets ? 0 : tokens;
+  const int e = offsets[sequences];
+  return e < 0 ? 0 : e > tokens ? tokens : e;
+}
+
+// Where number `at` is when the sequences have size(s) numbers each: the sequence, and its first number; seq = -1 where there
+// are fewer, `before` being how many there are then.  A wavefront together; the same for all of its lanes.
+struct Found {
+  int seq;
+  int64_t before;
+};
+template <typename F>
+__device__ __forceinline__ Found find_among(int sequences, int64_t at, const F& size) {
+  const int lane = threadIdx.x % kWave;
+  int64_t before = 0;
+  for (int base = 0; base < sequences; base += kWave) {
+    const int64_t n = base + lane < sequences ? int64_t(size(base + lane)) : 0;
+    int64_t incl = n;
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+      const int64_t up = __shfl_up(incl, d, kWave);
+      if (lane >= d) incl += up;
+    }
+    const uint64_t past = __ballot(before + incl > at);
+    if (past) {
+      const int first = __builtin_ctzll(past);
+      return {base + first, before + __shfl(incl - n, first, kWave)};
+    }
+    before += __shfl(incl, kWave - 1, kWave);
+  }
+  return {-1, before};
+}
+// (both of them uniform values: in scalar registers)
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+  return int64_t(uint64_t(uint32_t(uniform(int(v >> 32)))) << 32 | uint32_t(uniform(int(v))));
+}
+
+// ---- tiles in shared memory, and products of 32 x 32 ---------------------------------------------
+// A tile is rows of ROWB bytes, head_size up to a power of two; a row's 16-byte parts lie in an order of their own, part ^ turn(row), so that
+// 16 rows' parts of one number, and four rows' 64 neighbouring bytes (which a transposing read takes), meet no bank twice.
+template <int ROWB>
+__device__ __forceinline__ int turn(int row) {
+  if constexpr (ROWB >= 256) return (row & 3) << 2 | (row >> 2 & 3);
+  else if constexpr (ROWB == 128) return (row >> 1 & 1) << 2 | (row >> 2 & 3);
+  else return row >> 2 & 3;
+}
+template <int ROWB>
+__device__ __forceinline__ int part_at(int row, int part) { return row * ROWB + ((part ^ turn<ROWB>(row)) << 4); }
+
+typedef float v16f_t __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+
+// The sum of products over one part of 16 bytes of each operand's rows: lanes 0-31 give row lane of a and column lane of b in the first part
+// of a pair, lanes 32-63 in the second.  A lane gets column lane%32 of the result, rows result_row(r): 32 values are as a
+// right operand of the next product what they were as a result of this one, as long as its left operand takes the same order.
+__device__ __forceinline__ int result_row(int r, int half) { return r / 4 * 8 + half * 4 + r % 4; }
+template <typename T>
+__device__ __forceinline__ v16f_t multiply_parts(uint4 a, uint4 b, v16f_t c) {
+  if constexpr (sizeof(T) == 2) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+  } else {
+    c = __builtin_amdgcn_mfma_f32_32x32x2f32(u32_as_f32(a.x), u32_as_f32(b.x), c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_32x32x2f32(u32_as_f32(a.y), u32_as_f32(b.y), c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_32x32x2f32(u32_as_f32(a.z), u32_as_f32(b.z), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x2f32(u32_as_f32(a.w), u32_as_f32(b.w), c, 0, 0, 0);
+  }
+}
+
+// DB blocks of 32 values of a head (the last ones zeros where head_size is less).
+template <typename T, int DB>
+struct Head {
+  static constexpr int kParts = DB * 32 * int(sizeof(T)) / 16;  // of 16 bytes
+  static constexpr int kRowBytes = (DB <= 1 ? 32 : DB <= 2 ? 64 : DB <= 4 ? 128 : 256) * int(sizeof(T));
+  static constexpr int kRowParts = kRowBytes / 16;
+  static constexpr int kPairs = kParts / 2;
+};
+
+// A lane's half of a row: parts 2i + lane/32, from memory (zeros behind head_size, and where there is no row).
+template <typename T, int DB>
+struct RowParts {
+  uint4 p[Head<T, DB>::kPairs];
+  __device__ __forceinline__ void load(const T* row, int half, int parts) {
+#pragma unroll
+    for (int i = 0; i < Head<T, DB>::kPairs; ++i) {
+      const int part = 2 * i + half;
+      p[i] = part < parts ? load16(row + part * (16 / int(sizeof(T)))) : make_uint4(0, 0, 0, 0);
+    }
+  }
+};
+
+// 32 rows of a tile times 32 rows in registers: result[row of the tile][row of the registers].
+template <typename T, int DB>
+__device__ __forceinline__ v16f_t rows_product(const uint8_t* tile, int row, int half, const RowParts<T, DB>& b) {
+  v16f_t c = {};
+#pragma unroll
+  for (int i = 0; i < Head<T, DB>::kPairs; ++i)
+    c = multiply_parts<T>(*reinterpret_cast<const uint4*>(tile + part_at<Head<T, DB>::kRowBytes>(row, 2 * i + half)), b.p[i], c);
+  return c;
+}
+
+// 16 columns (of 32 that this lane's half has 16 of) of a result, as right operand of the next product.
+template <typename T>
+struct Weights;
+template <>
+struct Weights<float> {
+  float w[16];
+};
+template <>
+struct Weights<bf16_t> {
+  bf16x8_t w[2];
+};
+__device__ __forceinline__ void set_weights(Weights<float>& o, const float (&f)[16]) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) o.w[r] = f[r];
+}
+__device__ __forceinline__ void set_weights(Weights<bf16_t>& o, const float (&f)[16]) {
+#pragma unroll
+  for (int s = 0; s < 2; ++s)
+    o.w[s] = __builtin_bit_cast(bf16x8_t, make_uint4(bf16_pair(f[8 * s], f[8 * s + 1]), bf16_pair(f[8 * s + 2], f[8 * s + 3]),
+                                                     bf16_pair(f[8 * s + 4], f[8 * s + 5]), bf16_pair(f[8 * s + 6], f[8 * s + 7])));
+}
+
+typedef short short4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) short4_t lds_short4_t;
+// 4 rows x 16 columns of 16 bits, transposed: each lane of 16 gives the address of four neighbours, lane i of row i/4 and columns 4*(i%4), and
+// gets column i of the four rows.
+__device__ __forceinline__ short4_t transposed(const uint8_t* p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t*)(p));
+}
+
+// acc[value of a head][lane's column] += sum over 32 rows of a tile, from row0 (a multiple of 32) on, of x[row][value] * w[row][column].
+template <typename T, int DB>
+__device__ __forceinline__ void weighted_rows(v16f_t (&acc)[DB], const uint8_t* tile, int row0, int lane, const Weights<T>& w) {
+  constexpr int ROWB = Head<T, DB>::kRowBytes;
+  const int half = lane / 32;
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const int row = row0 + 16 * s + 4 * half + lane % 16 / 4;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const int part = db * 4 + lane % 32 / 16 * 2 + lane % 4 / 2, in = lane % 2 * 8;
+        const short4_t lo = transposed(tile + part_at<ROWB>(row, part) + in), hi = transposed(tile + part_at<ROWB>(row + 8, part) + in);
+        typedef short short8_t __attribute__((ext_vector_type(8)));
+        const short8_t a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), w.w[s], acc[db], 0, 0, 0);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int row = row0 + result_row(r, half);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const float a = *reinterpret_cast<const float*>(tile + part_at<ROWB>(row, db * 8 + lane % 32 / 4) + lane % 4 * 4);
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w.w[r], acc[db], 0, 0, 0);
+      }
+    }
+  }
+}
+// The same where not every column takes every row (bit i of `seen`: lane's column takes row row0 + i), and what it does not take may
+// be an infinity or NaN, which a product with zero would bring in: one row after the other, and none of it where it is not taken.
+template <typename T, int DB>
+__device__ __forceinline__ void weighted_rows_apart(v16f_t (&acc)[DB], const uint8_t* tile, int row0, int lane, const float (&w)[16],
+                                                 uint32_t seen) {
+  constexpr int ROWB = Head<T, DB>::kRowBytes;
+  const int half = lane / 32;
+#pragma unroll 1
+  for (int i = 0; i < 32; ++i) {
+    float mine = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) mine = result_row(r, half) == i ? w[r] : mine;
+    const float weight = __shfl(mine, lane % 32 + (i >> 2 & 1) * 32, kWave);
+    const bool taken = seen >> i & 1;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int value = db * 32 + result_row(r, half);
+        const uint8_t* const p = tile + part_at<ROWB>(row0 + i, value * int(sizeof(T)) / 16) + value * int(sizeof(T)) % 16;
+        float x;
+        if constexpr (sizeof(T) == 4) x = *reinterpret_cast<const float*>(p);
+        else x = u32_as_f32(uint32_t(*reinterpret_cast<const uint16_t*>(p)) << 16);
+        acc[db][r] = taken ? fmaf(x, weight, acc[db][r]) : acc[db][r];
+      }
+  }
+}
+
+// The lane's column: values result_row of block db, as elements of T in a row, times `factor`.
+template <typename T, int DB>
+__device__ __forceinline__ void store_column(T* row, const v16f_t (&acc)[DB], int half, int head, float factor) {
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int value = db * 32 + q * 8 + half * 4;
+      if (value >= head) continue;  // (head is a multiple of 8)
+      const float f[4] = {acc[db][4 * q] * factor, acc[db][4 * q + 1] * factor, acc[db][4 * q + 2] * factor, acc[db][4 * q + 3] * factor};
+      if constexpr (sizeof(T) == 4) {
+        *reinterpret_cast<float4*>(row + value) = make_float4(f[0], f[1], f[2], f[3]);
+      } else {
+        *reinterpret_cast<uint2*>(row + value) = make_uint2(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3]));
+      }
+    }
+}
+// Not finite anywhere in the values that are stored?
+template <int DB>
+__device__ __forceinline__ bool finite_column(const v16f_t (&acc)[DB]) {
+  float zero = 0.0f;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) zero = fmaf(acc[db][r], 0.0f, zero);
+  return zero == 0.0f;
+}
+
+// The two halves of a column (lanes l and l + 32): largest, sum.
+__device__ __forceinline__ float other_half(float v, bool second) {
+  const auto r = __builtin_amdgcn_permlane32_swap(f32_as_u32(v), f32_as_u32(v), false, false);
+  return u32_as_f32(second ? r[0] : r[1]);
+}
+__device__ __forceinline__ float halves_max(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(f32_as_u32(v), f32_as_u32(v), false, false);
+  return fmaxf(u32_as_f32(r[0]), u32_as_f32(r[1]));
+}
+__device__ __forceinline__ float halves_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(f32_as_u32(v), f32_as_u32(v), false, false);
+  return u32_as_f32(r[0]) + u32_as_f32(r[1]);
+}
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// Bits first .. end-1 of 32.
+__device__ __forceinline__ uint32_t bits_between(int first, int end) {
+  const uint32_t below_end = end >= 32 ? ~0u : end <= 0 ? 0u : (1u << end) - 1u;
+  const uint32_t below_first = first >= 32 ? ~0u : first <= 0 ? 0u : (1u << first) - 1u;
+  return below_end & ~below_first;
+}
+
+// ---- loads straight into shared memory -------------------------------------------------------------
+__device__ __forceinline__ uint32_t lds_offset(const void* p) {
+  return uint32_t(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)p));
+}
+// 16 bytes a lane from base + offset to shared memory, `to` on, lane by lane; lanes that are off load and write nothing.  Nothing waits for it but an
+// explicit wait for all loads (the compiler would wait before every read of shared memory).
+__device__ __forceinline__ void load_tile_part(const void* base, uint32_t offset, uint32_t to) {
+  base = reinterpret_cast<const void*>(uniform(int64_t(reinterpret_cast<uintptr_t>(base))));  // (the same for all lanes, whatever register it is in)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(uniform(int(to))), "v"(offset), "s"(base) : "memory");
+}
+
+// Rows of a tensor into a tile, ROWS of them by WAVES wavefronts: 1024 bytes a wavefront and load.  Rows from `end` on give the last one
+// again; they are not used.  Parts behind head_size are not loaded.
+template <typename T, int DB, int ROWS, int WAVES>
+struct TileRows {
+  static constexpr int kRowBytes = Head<T, DB>::kRowBytes, kRowParts = Head<T, DB>::kRowParts;
+  static constexpr int kRowsPer = 1024 / kRowBytes, kLoads = ROWS / kRowsPer / WAVES;
+  static_assert(kRowsPer >= 1 && ROWS % (kRowsPer * WAVES) == 0, "whole loads");
+  uint32_t stride;  // bytes
+  int wave, lane, parts;
+  uint32_t from[kLoads];
+  __device__ __forceinline__ TileRows(int wave_, int lane_, int64_t stride_elements, int parts_)
+      : stride(uint32_t(stride_elements) * uint32_t(sizeof(T))), wave(wave_), lane(lane_), parts(parts_) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) from[i] = uint32_t(row(i)) * stride + uint32_t(part(i)) * 16u;
+  }
+  __device__ __forceinline__ int row(int i) const { return (i * WAVES + wave) * kRowsPer + lane / kRowParts; }
+  __device__ __forceinline__ int part(int i) const { return lane % kRowParts ^ turn<kRowBytes>(row(i)); }
+  // rows first .. first + ROWS - 1 behind `base`, of which there are `left`, at least one
+  __device__ __forceinline__ void fetch(const void* base, int left, const uint8_t* tile) const {
+    const uint32_t to = lds_offset(tile) + uint32_t(wave) * 1024u;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      uint32_t at = from[i];
+      if (left < ROWS) at = uint32_t(row(i) < left ? row(i) : left - 1) * stride + uint32_t(part(i)) * 16u;
+      if (part(i) < parts) load_tile_part(base, at, to + uint32_t(i * WAVES) * 1024u);
+    }
+  }
+};
+// Tiles' parts that no load fills are zeros.
+template <int BYTES, int THREADS>
+__device__ __forceinline__ void clear_tiles(uint8_t* tiles) {
+  for (int i = threadIdx.x * 16; i < BYTES; i += THREADS * 16) *reinterpret_cast<uint4*>(tiles + i) = make_uint4(0, 0, 0, 0);
+}
+
+// Workgroups are dealt to the chip's eight dies in turn; a die gets neighbouring heads, all of their tiles, so that the keys and values
+// its workgroups read at a time are in its cache.  Tiles in falling order: with a causal mask the later ones are longer.
+struct HeadTile {
+  int head, tile;
+};
+__device__ __forceinline__ HeadTile deal(int id, int heads, int tiles) {
+  constexpr int kDies = 8;
+  if (heads % kDies == 0) {
+    const int each = heads / kDies, in = id / kDies;
+    return {id % kDies * each + in % each, tiles - 1 - in / each};
+  }
+  return {id % heads, tiles - 1 - id / heads};
+}
+
+#endif  // __HIPCC__
+
+}  // namespace accept

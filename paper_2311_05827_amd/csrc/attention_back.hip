@@ -1,0 +1,336 @@
+// Gradients of attention.  The weights are computed again from the scores and the logarithms of the rows' sums; one kernel goes over the
+// keys of its queries (dq, and the sums of do * o), a second one over the queries of its keys (dk and dv).  That is seven products
+// of tiles where a single kernel would do with five, but each gradient is one workgroup's own sum, in a fixed order: no atomics.
+#include "attention.hpp"
+
+namespace accept {
+namespace {
+
+struct BackArgs {
+  const void* dout;
+  const void* q;
+  const void* k;
+  const void* v;
+  const void* o;
+  const float* lse;
+  float* along;  // heads x q_tokens: sums of do * o
+  void* dq;
+  void* dk;
+  void* dv;
+  const int32_t* q_offsets;
+  const int32_t* k_offsets;
+  int64_t q_stride, k_stride, v_stride, o_stride, dq_stride, dk_stride, dv_stride;
+  int sequences, q_tokens, k_tokens, q_each, k_each;
+  int heads, kv_heads, group, head;
+  int tiles;
+  int causal, zeros;
+  float scale, scale2;  // as it is, and times log2(e)
+};
+
+constexpr int kRows = 128;  // of a workgroup, 32 of a wavefront
+constexpr int kWaves = 4;
+
+// A workgroup's piece of kRows tokens of a sequence; seq -1: `tile` counts the pieces of the tokens behind the last one.
+struct Piece {
+  int seq, tile;
+};
+__device__ __forceinline__ Piece find_piece(const int32_t* offsets, int sequences, int tokens, int each, int tile) {
+  if (!offsets) {
+    const int per = pieces(each, kRows);
+    return {tile / per, tile % per};
+  }
+  const Found f = find_among(sequences, tile, [&](int s) { return pieces(span_of(offsets, s, tokens, 0).size(), kRows); });
+  return {uniform(f.seq), int(tile - uniform(f.before))};
+}
+// Zeros for this piece of the tokens behind the last sequence.
+template <typename T>
+__device__ __forceinline__ void clear_rest(T* to, int64_t stride, int head, int first, int tile, int tokens) {
+  const int parts = head * int(sizeof(T)) / 16;
+  for (int i = threadIdx.x; i < kRows * parts; i += kWaves * kWave) {
+    const int row = first + tile * kRows + i / parts;
+    if (row >= tokens) break;
+    reinterpret_cast<uint4*>(to + row * stride)[i % parts] = make_uint4(0, 0, 0, 0);
+  }
+}
+
+// dq: 128 queries of a head, a lane has a query of its own as in the forward pass.
+template <typename T, int DB>
+__global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) void back_queries_kernel(const BackArgs g) {
+  constexpr int BN = 32 * (sizeof(T) == 2 && DB <= 4 ? 2 : 1);
+  constexpr int kTile = BN * Head<T, DB>::kRowBytes;
+  __shared__ __align__(16) uint8_t tiles[4 * kTile];
+  const int lane = threadIdx.x % kWave, wave = uniform(int(threadIdx.x / kWave));
+  const int half = lane / 32, column = lane % 32;
+  const HeadTile ht = deal(blockIdx.x, g.heads, g.tiles);
+  const int head = ht.head;
+  const Piece piece = find_piece(g.q_offsets, g.sequences, g.q_tokens, g.q_each, ht.tile);
+  T* const dq = static_cast<T*>(g.dq) + int64_t(head) * g.head;
+  if (piece.seq < 0) {
+    if (g.zeros) clear_rest(dq, g.dq_stride, g.head, rest_of(g.q_offsets, g.sequences, g.q_tokens), piece.tile, g.q_tokens);
+    return;
+  }
+  const Span qs = span_of(g.q_offsets, piece.seq, g.q_tokens, g.q_each), ks = span_of(g.k_offsets, piece.seq, g.k_tokens, g.k_each);
+  const int rows = qs.size(), keys = ks.size(), more = keys - rows, last = rows - 1;
+  const int row0 = piece.tile * kRows + wave * 32, row = row0 + column;
+  const bool is_row = row < rows;
+  const auto seen_by = [&](int i) { return !g.causal ? keys : i + 1 + more < 0 ? 0 : i + 1 + more; };
+  const int limit = seen_by(is_row ? row : last);
+  const int first_limit = row0 < rows ? seen_by(row0) : 0;
+  const int wave_limit = row0 < rows ? seen_by(row0 + 31 < last ? row0 + 31 : last) : 0;
+  const int end = piece.tile * kRows + kRows - 1;
+  const int steps = pieces(seen_by(end < last ? end : last), BN);
+
+  const int parts = g.head * int(sizeof(T)) / 16;
+  const int64_t token = qs.begin + (is_row ? row : last);
+  RowParts<T, DB> q, dout;
+  float along = 0.0f;
+  {
+    RowParts<T, DB> o;
+    dout.load(static_cast<const T*>(g.dout) + token * g.o_stride + int64_t(head) * g.head, half, parts);
+    o.load(static_cast<const T*>(g.o) + token * g.o_stride + int64_t(head) * g.head, half, parts);
+#pragma unroll
+    for (int i = 0; i < Head<T, DB>::kPairs; ++i) {
+      constexpr int VEC = 16 / int(sizeof(T));
+      float a[VEC], b[VEC];
+      widened(Raw<T, VEC>{dout.p[i].x, dout.p[i].y, dout.p[i].z, dout.p[i].w}, a);
+      widened(Raw<T, VEC>{o.p[i].x, o.p[i].y, o.p[i].z, o.p[i].w}, b);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) along = fmaf(a[j], b[j], along);
+    }
+    along = halves_sum(along);
+  }
+  if (is_row && half == 0) g.along[int64_t(head) * g.q_tokens + token] = along;
+  const float lse = g.lse[int64_t(head) * g.q_tokens + token] * kLog2e;
+  q.load(static_cast<const T*>(g.q) + token * g.q_stride + int64_t(head) * g.head, half, parts);
+
+  const T* const k0 = static_cast<const T*>(g.k) + ks.begin * g.k_stride + int64_t(head / g.group) * g.head;
+  const T* const v0 = static_cast<const T*>(g.v) + ks.begin * g.v_stride + int64_t(head / g.group) * g.head;
+  const TileRows<T, DB, BN, kWaves> k_rows(wave, lane, g.k_stride, parts), v_rows(wave, lane, g.v_stride, parts);
+  const auto fetch = [&](int step) {
+    uint8_t* const to = tiles + step % 2 * 2 * kTile;
+    k_rows.fetch(k0 + int64_t(step) * BN * g.k_stride, keys - step * BN, to);
+    v_rows.fetch(v0 + int64_t(step) * BN * g.v_stride, keys - step * BN, to + kTile);
+  };
+  if (g.head < DB * 32) {
+    clear_tiles<4 * kTile, kWaves * kWave>(tiles);
+    __syncthreads();
+  }
+  v16f_t acc[DB];
+  const auto run = [&](auto apart) {  // (see attention_kernel)
+#pragma unroll
+    for (int db = 0; db < DB; ++db) acc[db] = v16f_t{};
+    if (steps > 0) fetch(0);
+    for (int step = 0; step < steps; ++step) {
+      __builtin_amdgcn_s_waitcnt(0);
+      __syncthreads();
+      if (step + 1 < steps) fetch(step + 1);
+      const int key0 = step * BN;
+      if (key0 >= wave_limit) continue;
+      const uint8_t* const kt = tiles + step % 2 * 2 * kTile;
+      const uint8_t* const vt = kt + kTile;
+      const bool masked = key0 + BN > first_limit;
+#pragma unroll
+      for (int n = 0; n < BN; n += 32) {
+        const v16f_t s = rows_product<T, DB>(kt, n + column, half, q);
+        const v16f_t dp = rows_product<T, DB>(vt, n + column, half, dout);
+        float ds[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], g.scale2, -lse)) * (dp[r] - along);
+        const int left = limit - key0 - n;
+        if (masked) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) ds[r] = result_row(r, half) < left ? ds[r] : 0.0f;
+        }
+        if (apart.value && masked) {
+          weighted_rows_apart<T, DB>(acc, kt, n, lane, ds, bits_between(0, left));
+        } else {
+          Weights<T> w;
+          set_weights(w, ds);
+          weighted_rows<T, DB>(acc, kt, n, lane, w);
+        }
+      }
+    }
+  };
+  run(Flag<false>{});
+  if (__syncthreads_or(is_row && !finite_column<DB>(acc))) run(Flag<true>{});
+  if (is_row) store_column<T, DB>(dq + token * g.dq_stride, acc, half, g.head, g.scale);
+}
+
+// dk and dv: 128 keys of a key head, a lane has a key of its own; tiles of queries and their do come through shared memory, head after head of
+// those that share the key head.
+template <typename T, int DB>
+__global__ __launch_bounds__(kWaves * kWave, DB <= 2 && sizeof(T) == 2 ? 2 : 1) void back_keys_kernel(const BackArgs g) {
+  constexpr int BM = 32 * (sizeof(T) == 2 && DB <= 4 ? 2 : 1);
+  constexpr int kTile = BM * Head<T, DB>::kRowBytes;
+  __shared__ __align__(16) uint8_t tiles[4 * kTile];
+  __shared__ float stats[2][2][BM];  // logarithms, sums of do * o
+  const int lane = threadIdx.x % kWave, wave = uniform(int(threadIdx.x / kWave));
+  const int half = lane / 32, column = lane % 32;
+  const HeadTile ht = deal(blockIdx.x, g.kv_heads, g.tiles);
+  const int head = ht.head;
+  const Piece piece = find_piece(g.k_offsets, g.sequences, g.k_tokens, g.k_each, g.tiles - 1 - ht.tile);  // (the first keys have most queries)
+  T* const dk = static_cast<T*>(g.dk) + int64_t(head) * g.head;
+  T* const dv = static_cast<T*>(g.dv) + int64_t(head) * g.head;
+  if (piece.seq < 0) {
+    if (g.zeros) {
+      const int rest = rest_of(g.k_offsets, g.sequences, g.k_tokens);
+      clear_rest(dk, g.dk_stride, g.head, rest, piece.tile, g.k_tokens);
+      clear_rest(dv, g.dv_stride, g.head, rest, piece.tile, g.k_tokens);
+    }
+    return;
+  }
+  const Span qs = span_of(g.q_offsets, piece.seq, g.q_tokens, g.q_each), ks = span_of(g.k_offsets, piece.seq, g.k_tokens, g.k_each);
+  const int rows = qs.size(), keys = ks.size(), more = keys - rows, last = keys - 1;
+  const int key0 = piece.tile * kRows + wave * 32, key = key0 + column;
+  const bool is_key = key < keys;
+  // the first query that sees a key
+  const auto seen_from = [&](int j) { return !g.causal || j - more < 0 ? 0 : j - more; };
+  const int from = seen_from(is_key ? key : last);
+  const int wave_from = seen_from(key0), wave_all = seen_from(key0 + 31);
+  const int first = seen_from(piece.tile * kRows) / BM;  // tile of queries
+  const int each = pieces(rows, BM) - first, steps = each > 0 ? each * g.group : 0;
+
+  const int parts = g.head * int(sizeof(T)) / 16;
+  const int64_t token = ks.begin + (is_key ? key : last);
+  RowParts<T, DB> k, v;
+  k.load(static_cast<const T*>(g.k) + token * g.k_stride + int64_t(head) * g.head, half, parts);
+  v.load(static_cast<const T*>(g.v) + token * g.v_stride + int64_t(head) * g.head, half, parts);
+  const TileRows<T, DB, BM, kWaves> q_rows(wave, lane, g.q_stride, parts), o_rows(wave, lane, g.o_stride, parts);
+  const auto fetch = [&](int step) {
+    uint8_t* const to = tiles + step % 2 * 2 * kTile;
+    const int h = head * g.group + step / each, row = (first + step % each) * BM, left = rows - row;
+    const int64_t at = qs.begin + row;
+    q_rows.fetch(static_cast<const T*>(g.q) + at * g.q_stride + int64_t(h) * g.head, left, to);
+    o_rows.fetch(static_cast<const T*>(g.dout) + at * g.o_stride + int64_t(h) * g.head, left, to + kTile);
+  };
+  // rows' statistics: loaded with the tile, stored when it has come
+  const auto statistic = [&](int step) {
+    const int h = head * g.group + step / each, row = (first + step % each) * BM + int(threadIdx.x) % BM;
+    const int64_t at = int64_t(h) * g.q_tokens + qs.begin + (row < rows ? row : rows - 1);
+    return int(threadIdx.x) < BM ? g.lse[at] * kLog2e : int(threadIdx.x) < 2 * BM ? g.along[at] : 0.0f;
+  };
+  if (g.head < DB * 32) {
+    clear_tiles<4 * kTile, kWaves * kWave>(tiles);
+    __syncthreads();
+  }
+  v16f_t sum_k[DB], sum_v[DB];
+  const auto run = [&](auto apart) {  // (see attention_kernel)
+#pragma unroll
+    for (int db = 0; db < DB; ++db) sum_k[db] = v16f_t{}, sum_v[db] = v16f_t{};
+    float mine = 0.0f;
+    if (steps > 0) {
+      mine = statistic(0);
+      fetch(0);
+    }
+    for (int step = 0; step < steps; ++step) {
+      if (int(threadIdx.x) < 2 * BM) stats[step % 2][threadIdx.x / BM][threadIdx.x % BM] = mine;
+      __builtin_amdgcn_s_waitcnt(0);
+      __syncthreads();
+      if (step + 1 < steps) {
+        mine = statistic(step + 1);
+        fetch(step + 1);
+      }
+      const int row0 = (first + step % each) * BM;
+      const uint8_t* const qt = tiles + step % 2 * 2 * kTile;
+      const uint8_t* const ot = qt + kTile;
+#pragma unroll
+      for (int n = 0; n < BM; n += 32) {
+        if (row0 + n + 31 < wave_from || row0 + n >= rows || key0 >= keys) continue;
+        const bool masked = row0 + n < wave_all || row0 + n + 32 > rows || key0 + 32 > keys;
+        const v16f_t s = rows_product<T, DB>(qt, n + column, half, k);
+        const v16f_t dp = rows_product<T, DB>(ot, n + column, half, v);
+        float p[16], ds[16];
+        const uint32_t seen = bits_between(from - row0 - n, rows - row0 - n);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int i = result_row(r, half);
+          p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], g.scale2, -stats[step % 2][0][n + i]));
+          ds[r] = p[r] * (dp[r] - stats[step % 2][1][n + i]);
+          if (masked) {
+            const bool sees = seen >> i & 1;
+            p[r] = sees ? p[r] : 0.0f;
+            ds[r] = sees ? ds[r] : 0.0f;
+          }
+        }
+        if (apart.value && masked) {
+          weighted_rows_apart<T, DB>(sum_v, ot, n, lane, p, seen);
+          weighted_rows_apart<T, DB>(sum_k, qt, n, lane, ds, seen);
+        } else {
+          Weights<T> w;
+          set_weights(w, p);
+          weighted_rows<T, DB>(sum_v, ot, n, lane, w);
+          set_weights(w, ds);
+          weighted_rows<T, DB>(sum_k, qt, n, lane, w);
+        }
+      }
+    }
+  };
+  run(Flag<false>{});
+  if (__syncthreads_or(is_key && !(finite_column<DB>(sum_k) && finite_column<DB>(sum_v)))) run(Flag<true>{});
+  if (!is_key) return;
+  store_column<T, DB>(dk + token * g.dk_stride, sum_k, half, g.head, g.scale);
+  store_column<T, DB>(dv + token * g.dv_stride, sum_v, half, g.head, 1.0f);
+}
+
+template <typename T, int DB>
+void launch_both(BackArgs g, int q_tiles, int k_tiles, hipStream_t s) {
+  constexpr int kThreads = kWaves * kWave;
+  if (q_tiles > 0) {
+    g.tiles = q_tiles;
+    back_queries_kernel<T, DB><<<dim3(uint32_t(q_tiles) * g.heads), kThreads, 0, s>>>(g);
+  }
+  if (k_tiles > 0) {
+    g.tiles = k_tiles;
+    back_keys_kernel<T, DB><<<dim3(uint32_t(k_tiles) * g.kv_heads), kThreads, 0, s>>>(g);
+  }
+}
+template <typename T>
+hipError_t launch(const BackArgs& g, int q_tiles, int k_tiles, hipStream_t s) {
+  if (g.head <= 32) launch_both<T, 1>(g, q_tiles, k_tiles, s);
+  else if (g.head <= 64) launch_both<T, 2>(g, q_tiles, k_tiles, s);
+  else if (g.head <= 96) launch_both<T, 3>(g, q_tiles, k_tiles, s);
+  else if (g.head <= 128) launch_both<T, 4>(g, q_tiles, k_tiles, s);
+  else launch_both<T, 8>(g, q_tiles, k_tiles, s);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+AttentionBackPlan make_attention_back_plan(const accept_attention_desc& d) {
+  return {size_t(up_to(4 * int64_t(d.heads) * d.q_tokens, 256))};
+}
+
+hipError_t launch_attention_backward(const accept_attention_desc& d, const AttentionBackPlan&, const void* dout, const void* q,
+                                     const void* k, const void* v, const void* o, const float* lse, const int32_t* q_offsets,
+                                     const int32_t* k_offsets, void* dq, void* dk, void* dv, void* ws, hipStream_t s) {
+  BackArgs g{};
+  const int64_t whole = int64_t(d.heads) * d.head_size, kv_whole = int64_t(d.kv_heads) * d.head_size;
+  const auto stride = [](int64_t given, int64_t otherwise) { return given ? given : otherwise; };
+  g.dout = dout, g.q = q, g.k = k, g.v = v, g.o = o, g.lse = lse;
+  g.along = static_cast<float*>(ws);
+  g.dq = dq, g.dk = dk, g.dv = dv;
+  g.q_offsets = q_offsets, g.k_offsets = k_offsets;
+  g.q_stride = stride(d.q_stride, whole), g.o_stride = stride(d.o_stride, whole), g.dq_stride = stride(d.dq_stride, whole);
+  g.k_stride = stride(d.k_stride, kv_whole), g.v_stride = stride(d.v_stride, kv_whole);
+  g.dk_stride = stride(d.dk_stride, kv_whole), g.dv_stride = stride(d.dv_stride, kv_whole);
+  g.sequences = int(d.sequences);
+  g.q_tokens = int(d.q_tokens);
+  g.k_tokens = int(d.k_tokens);
+  g.q_each = q_offsets || d.sequences == 0 ? 0 : int(d.q_tokens / d.sequences);
+  g.k_each = k_offsets || d.sequences == 0 ? 0 : int(d.k_tokens / d.sequences);
+  g.heads = d.heads;
+  g.kv_heads = d.kv_heads;
+  g.group = d.heads / d.kv_heads;
+  g.head = d.head_size;
+  g.causal = d.causal;
+  g.zeros = d.rest == ACCEPT_REST_ZEROS;
+  g.scale = float(d.scale);
+  g.scale2 = float(d.scale * 1.4426950408889634074);
+  const auto tiles = [&](const int32_t* offsets, int64_t tokens, int64_t each) {
+    return int(tokens == 0 ? 0 : offsets ? blocks_of(tokens, kRows) + d.sequences : d.sequences * blocks_of(each, kRows));
+  };
+  const int q_tiles = tiles(q_offsets, d.q_tokens, g.q_each), k_tiles = tiles(k_offsets, d.k_tokens, g.k_each);
+  return d.dtype == ACCEPT_F32 ? launch<float>(g, q_tiles, k_tiles, s) : launch<bf16_t>(g, q_tiles, k_tiles, s);
+}
+
+}  // namespace accept

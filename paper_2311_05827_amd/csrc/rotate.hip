@@ -1,0 +1,260 @@
+// Rotation of queries and keys by their position, and the way of new keys and values into a cache of pages.
+#include "attention.hpp"
+
+namespace accept {
+namespace {
+
+// cos and sin of a position's angle.  In turns, in 64 bits: position * frequency is exact there (31 and 24 bits) but for its last ones, and so the part of a
+// turn that is left has 2^-53 of the whole angle's error at most; from there 32 bits do.
+__device__ __forceinline__ void turn_of(int position, float frequency, float* c, float* s) {
+  const double turns = double(position) * double(frequency) * 0.15915494309189533577;
+  sincospif(float(2.0 * (turns - rint(turns))), s, c);
+}
+
+struct RotateArgs {
+  const void* q;      // of append: queries, may be null; of a rotation: the tensor
+  const void* k;
+  const void* v;
+  void* qo;
+  void* k_cache;
+  void* v_cache;
+  const float* frequencies;
+  const int32_t* offsets;
+  const int32_t* lengths;
+  const int32_t* positions;
+  const int32_t* table;
+  int64_t q_stride, k_stride, v_stride, qo_stride;
+  Pages pages;
+  int sequences, tokens, each;
+  int heads, kv_heads, head;  // heads of q: 0 where there are none
+  int half;                   // pairs that turn
+  float sign;                 // of the angle
+  int zeros;                  // what becomes of tokens without a sequence
+  int lanes;                  // items of a head: vectors of pairs, then vectors that are copied
+  int pair_lanes;
+  int per;                    // heads a thread goes through
+  int turning_chunks, chunks; // groups of heads that turn, and all
+};
+
+template <typename T, int N>
+__device__ __forceinline__ void load_n(const T* p, float (&f)[N]) {
+  if constexpr (N == 1) {
+    f[0] = load_one(p);
+  } else {
+    const uint4 w = load16(p);
+    Raw<T, N> r;
+    r.w[0] = w.x, r.w[1] = w.y, r.w[2] = w.z, r.w[3] = w.w;
+    widened(r, f);
+  }
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_n(T* p, const float (&f)[N]) {
+  if constexpr (N == 1) store_some<T, 1>(p, f);
+  else *reinterpret_cast<uint4*>(p) = narrow(f);
+}
+
+// A thread has the same part of some heads of one token: N pairs (their sines once for all of those heads), or 16 bytes that are copied.  Pairs come in
+// vectors of 16 bytes (halves: one of each half; neighbours: two behind each other) where those are whole, else one at a time.
+// CACHE: heads are those of q (if there are any), then of k, into their places; then v's, copied.
+template <typename T, int N, bool NEIGHBOURS, bool CACHE>
+__global__ __launch_bounds__(kBlock) void rotate_kernel(const RotateArgs g) {
+  constexpr int VEC = 16 / int(sizeof(T));
+  const int64_t at = (int64_t(blockIdx.y) * gridDim.x + blockIdx.x) * kBlock + threadIdx.x;
+  const int64_t per_token = int64_t(g.lanes) * g.chunks;
+  const int64_t all = per_token * g.tokens;
+  const bool mine = at < all;
+  const int token = mine ? int(at / per_token) : g.tokens - 1;
+  // the token's sequence: a wavefront's tokens lie next to each other, so the first one's is searched for, and from there on
+  int seq = 0, place = token;
+  bool outside = false;
+  if (!g.offsets) {
+    if (g.each > 0) seq = token / g.each, place = token - seq * g.each;
+  } else if (CACHE || !g.positions || !g.zeros) {
+    int lo = 0, hi = g.sequences;  // the first sequence that ends behind the token
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (g.offsets[mid + 1] > token) hi = mid;
+      else lo = mid + 1;
+    }
+    seq = lo;
+    outside = seq >= g.sequences;
+    if (!outside) place = token - span_of(g.offsets, seq, g.tokens, 0).begin;
+    if (place < 0) outside = true;
+  } else {
+    outside = token >= rest_of(g.offsets, g.sequences, g.tokens);
+  }
+  if (!mine) return;
+  const int in_token = int(at - int64_t(token) * per_token), chunk = in_token / g.lanes, item = in_token - chunk * g.lanes;
+  int length = 0;
+  int64_t row = -1;  // of key head 0 in the caches
+  if (CACHE && !outside) {
+    length = g.lengths[seq] < 0 ? 0 : g.lengths[seq];
+    const int64_t j = int64_t(length) + place;
+    if (has_place(g.pages, j)) {
+      const int page = g.table[int64_t(seq) * g.pages.table_pages + (j >> g.pages.shift)];
+      if (is_page(g.pages, page)) row = cache_row(g.pages, page, j, 0);
+    }
+  }
+  const int64_t head_rows = int64_t(1) << g.pages.shift;
+  if (outside && (!g.zeros || (CACHE && g.heads == 0))) return;
+
+  if (chunk >= g.turning_chunks) {  // v's heads: CACHE only
+    if (outside || row < 0) return;
+    const int first = (chunk - g.turning_chunks) * g.per, end = first + g.per < g.kv_heads ? first + g.per : g.kv_heads;
+    const T* const v = static_cast<const T*>(g.v) + token * g.v_stride;
+    T* const to = static_cast<T*>(g.v_cache);
+    for (int h = first; h < end; ++h)
+      for (int c = item; c < g.head / VEC; c += g.lanes)
+        *reinterpret_cast<uint4*>(to + (row + h * head_rows) * g.head + c * VEC) = load16(v + h * g.head + c * VEC);
+    return;
+  }
+  const int turning = g.heads + (CACHE ? g.kv_heads : 0);
+  const int first = chunk * g.per, end = first + g.per < turning ? first + g.per : turning;
+  const bool pair = item < g.pair_lanes;
+  float c[N], s[N];
+  if (pair && !outside) {
+    const int position = g.positions ? g.positions[token] : length + place;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      turn_of(position, g.frequencies[item * N + i], &c[i], &s[i]);
+      s[i] *= g.sign;
+    }
+  }
+  for (int h = first; h < end; ++h) {
+    const T* from;
+    T* to;
+    if (!CACHE || h < g.heads) {
+      from = static_cast<const T*>(g.q) + token * g.q_stride + h * g.head;
+      to = static_cast<T*>(g.qo) + token * g.qo_stride + h * g.head;
+    } else {
+      if (row < 0) break;  // (keys come last)
+      from = static_cast<const T*>(g.k) + token * g.k_stride + (h - g.heads) * g.head;
+      to = static_cast<T*>(g.k_cache) + (row + (h - g.heads) * head_rows) * g.head;
+    }
+    if (!pair) {
+      const int copied = 2 * g.half + (item - g.pair_lanes) * (N == 1 ? 1 : VEC);
+      if constexpr (N == 1) {
+        store_one(to + copied, outside ? 0.0f : load_one(from + copied));
+      } else {
+        *reinterpret_cast<uint4*>(to + copied) = outside ? make_uint4(0, 0, 0, 0) : load16(from + copied);
+      }
+    } else if constexpr (NEIGHBOURS) {
+      constexpr int V = N == 1 ? 1 : VEC;
+      float f[2 * N];
+#pragma unroll
+      for (int p = 0; p < 2 * N; p += V) {
+        float part[V];
+        load_n<T, V>(from + item * 2 * N + p, part);
+#pragma unroll
+        for (int i = 0; i < V; ++i) f[p + i] = part[i];
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float a = f[2 * i], b = f[2 * i + 1];
+        f[2 * i] = outside ? 0.0f : fmaf(a, c[i], -(b * s[i]));
+        f[2 * i + 1] = outside ? 0.0f : fmaf(a, s[i], b * c[i]);
+      }
+#pragma unroll
+      for (int p = 0; p < 2 * N; p += V) {
+        float part[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) part[i] = f[p + i];
+        store_n<T, V>(to + item * 2 * N + p, part);
+      }
+    } else {
+      float a[N], b[N];
+      load_n<T, N>(from + item * N, a);
+      load_n<T, N>(from + g.half + item * N, b);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float x = a[i], y = b[i];
+        a[i] = outside ? 0.0f : fmaf(x, c[i], -(y * s[i]));
+        b[i] = outside ? 0.0f : fmaf(x, s[i], y * c[i]);
+      }
+      store_n<T, N>(to + item * N, a);
+      store_n<T, N>(to + g.half + item * N, b);
+    }
+  }
+}
+
+template <typename T, bool CACHE>
+hipError_t launch(RotateArgs g, int pairs, hipStream_t s) {
+  constexpr int VEC = 16 / int(sizeof(T));
+  const bool vectors = g.half % VEC == 0;  // then every vector of a head (a multiple of 8) is whole
+  const int n = vectors ? VEC : 1;
+  g.pair_lanes = g.half / n;
+  g.lanes = g.pair_lanes + (g.head - 2 * g.half) / n;
+  const int turning = g.heads + (CACHE ? g.kv_heads : 0);
+  g.per = 1;
+  g.turning_chunks = int(blocks_of(turning, g.per));
+  g.chunks = g.turning_chunks + (CACHE ? int(blocks_of(g.kv_heads, g.per)) : 0);
+  const int64_t groups = blocks_of(int64_t(g.tokens) * g.lanes * g.chunks, kBlock);
+  const dim3 grid(grid_x(groups), grid_rest(groups));
+  if (pairs == ACCEPT_ROTATE_NEIGHBOURS) {
+    if (vectors) rotate_kernel<T, VEC, true, CACHE><<<grid, kBlock, 0, s>>>(g);
+    else rotate_kernel<T, 1, true, CACHE><<<grid, kBlock, 0, s>>>(g);
+  } else {
+    if (vectors) rotate_kernel<T, VEC, false, CACHE><<<grid, kBlock, 0, s>>>(g);
+    else rotate_kernel<T, 1, false, CACHE><<<grid, kBlock, 0, s>>>(g);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rotate(const accept_rotate_desc& d, const void* x, const float* frequencies, const int32_t* offsets,
+                         const int32_t* positions, void* y, hipStream_t s) {
+  RotateArgs g{};
+  const int64_t whole = int64_t(d.heads) * d.head_size;
+  g.q = x;
+  g.qo = y;
+  g.frequencies = frequencies;
+  g.offsets = offsets;
+  g.positions = positions;
+  g.q_stride = d.x_stride ? d.x_stride : whole;
+  g.qo_stride = d.y_stride ? d.y_stride : whole;
+  g.sequences = int(d.sequences);
+  g.tokens = int(d.tokens);
+  g.each = !offsets && !positions && d.sequences > 0 ? int(d.tokens / d.sequences) : 0;
+  g.heads = d.heads;
+  g.head = d.head_size;
+  g.half = d.rotated / 2;
+  g.sign = d.inverse ? -1.0f : 1.0f;
+  g.zeros = d.rest == ACCEPT_REST_ZEROS;
+  return d.dtype == ACCEPT_F32 ? launch<float, false>(g, d.pairs, s) : launch<bf16_t, false>(g, d.pairs, s);
+}
+
+hipError_t launch_cache_append(const accept_cache_desc& d, const void* q, const void* k, const void* v, const float* frequencies,
+                               const int32_t* offsets, const int32_t* lengths, const int32_t* positions, const int32_t* table,
+                               void* qo, void* k_cache, void* v_cache, hipStream_t s) {
+  RotateArgs g{};
+  const int64_t whole = int64_t(d.heads) * d.head_size, kv_whole = int64_t(d.kv_heads) * d.head_size;
+  g.q = q;
+  g.k = k;
+  g.v = v;
+  g.qo = qo;
+  g.k_cache = k_cache;
+  g.v_cache = v_cache;
+  g.frequencies = frequencies;
+  g.offsets = offsets;
+  g.lengths = lengths;
+  g.positions = positions;
+  g.table = table;
+  g.q_stride = d.q_stride ? d.q_stride : whole;
+  g.k_stride = d.k_stride ? d.k_stride : kv_whole;
+  g.v_stride = d.v_stride ? d.v_stride : kv_whole;
+  g.qo_stride = d.qo_stride ? d.qo_stride : whole;
+  g.pages = {int32_t(d.pages), int32_t(d.table_pages), __builtin_ctz(uint32_t(d.page_size)), d.kv_heads};
+  g.sequences = int(d.sequences);
+  g.tokens = int(d.tokens);
+  g.each = offsets || d.sequences == 0 ? 0 : int(d.tokens / d.sequences);
+  g.heads = q ? d.heads : 0;
+  g.kv_heads = d.kv_heads;
+  g.head = d.head_size;
+  g.half = d.rotated / 2;
+  g.sign = 1.0f;
+  g.zeros = d.rest == ACCEPT_REST_ZEROS;
+  return d.dtype == ACCEPT_F32 ? launch<float, true>(g, d.pairs, s) : launch<bf16_t, true>(g, d.pairs, s);
+}
+
+}  // namespace accept
