@@ -5,6 +5,8 @@ Argument marshalling only, as in stage_binding.py: tensors are checked on the ho
 given are allocated, and the kernels run on the current stream of the current device, where the tensors have to be.  Queries, keys, values and
 outputs are (tokens, heads, head_size), their tokens `stride` elements apart, or (tokens, heads * head_size).  What a call allocates
 holds zeros for tokens behind the last sequence, whatever the descriptor's `rest` says; what it is given follows the descriptor.
+csrc/native.cpp makes the same checks and calls without the interpreter; whatever it does not take comes to the code here, which says
+what is wrong.
 """
 from __future__ import annotations
 
@@ -57,6 +59,7 @@ def _declare(lib):
 
 
 lib = _declare(B.lib)
+_native = B._native
 
 
 # ------------------------------------------------------------------------------- descriptors
@@ -121,6 +124,8 @@ def _make_tokens(like, tokens, heads, head, stride, zeros=False):
     whole = heads * head
     if stride in (0, whole):
         return make((tokens, heads, head), dtype=like.dtype, device=like.device)
+    if stride < whole:
+        raise B.AcceptError(B.INVALID_ARG, "tokens of %d values are %d apart" % (whole, stride))
     return make((tokens, stride), dtype=like.dtype, device=like.device)[:, :whole].unflatten(1, (heads, head))
 
 
@@ -148,6 +153,12 @@ def _rest_desc(desc, zeros):
 def accept_rotate(desc, x, frequencies, offsets=None, positions=None, y=None):
     """Enqueue the rotation of x (tokens, heads, head_size) by its tokens' positions on the current stream; returns y, which may be
     given as x.  frequencies (rotated / 2) float32; positions (tokens) int32, or None: a token's place in its sequence."""
+    if type(desc) is RotateDesc:
+        got = _native.rotate(desc, x, frequencies, offsets, positions, y)
+        if type(got) is tuple:
+            return got[0]
+        if got > 0:
+            raise B.AcceptError(got, "accept_rotate")
     where = "accept_rotate"
     S._check_desc(desc, RotateDesc, where)
     if desc.dtype not in (B.F32, B.BF16):
@@ -193,6 +204,12 @@ def _workspace(where, workspace, nbytes, device):
 def accept_attention(desc, q, k, v, q_offsets=None, k_offsets=None, o=None, lse=None, workspace=None):
     """Enqueue attention of q (q_tokens, heads, head_size) over k and v (k_tokens, kv_heads, head_size) on the current stream; returns
     (o, lse), lse (heads, q_tokens) float32 as the backward pass takes it."""
+    if type(desc) is AttentionDesc:
+        got = _native.attention(desc, q, k, v, q_offsets, k_offsets, o, lse, workspace)
+        if type(got) is tuple:
+            return got
+        if got > 0:
+            raise B.AcceptError(got, "accept_attention")
     where = "accept_attention"
     _check_attention(where, desc, q, k, v, q_offsets, k_offsets)
     sizes = (desc.q_tokens, desc.heads, desc.head_size)
@@ -212,6 +229,12 @@ def accept_attention(desc, q, k, v, q_offsets=None, k_offsets=None, o=None, lse=
 
 def accept_attention_backward(desc, do, q, k, v, o, lse, q_offsets=None, k_offsets=None, dq=None, dk=None, dv=None, workspace=None):
     """Gradients of accept_attention from its outputs and that of o: (dq, dk, dv)."""
+    if type(desc) is AttentionDesc:
+        got = _native.attention_backward(desc, do, q, k, v, o, lse, q_offsets, k_offsets, dq, dk, dv, workspace)
+        if type(got) is tuple:
+            return got
+        if got > 0:
+            raise B.AcceptError(got, "accept_attention_backward")
     where = "accept_attention_backward"
     _check_attention(where, desc, q, k, v, q_offsets, k_offsets)
     of_q, of_k = (desc.q_tokens, desc.heads, desc.head_size), (desc.k_tokens, desc.kv_heads, desc.head_size)
@@ -255,6 +278,12 @@ def _check_cache(where, desc, k_cache, v_cache, table, lengths, offsets):
 def accept_cache_append(desc, q, k, v, k_cache, v_cache, table, lengths, offsets=None, positions=None, frequencies=None, q_out=None):
     """Enqueue the way of k (rotated) and v (tokens, kv_heads, head_size) into the places behind their sequences' lengths on the
     current stream; returns q rotated (q_out, which may be q), or None for q None.  positions (tokens) int32, or None: a token's place."""
+    if type(desc) is CacheDesc:
+        got = _native.cache_append(desc, q, k, v, k_cache, v_cache, table, lengths, offsets, positions, frequencies, q_out)
+        if type(got) is tuple:
+            return got[0]
+        if got > 0:
+            raise B.AcceptError(got, "accept_cache_append")
     where = "accept_cache_append"
     _check_cache(where, desc, k_cache, v_cache, table, lengths, offsets)
     dtype = B._DTYPES[desc.dtype]
@@ -284,6 +313,12 @@ def accept_cache_append(desc, q, k, v, k_cache, v_cache, table, lengths, offsets
 def accept_cache_attention(desc, q, k_cache, v_cache, table, lengths, offsets=None, tree=None, o=None, workspace=None):
     """Enqueue attention of q (tokens, heads, head_size) over its sequences' places on the current stream; lengths are those that the
     append of the same tokens took.  tree (tokens, tree_words) int64, the bits of the new tokens that each sees.  Returns o."""
+    if type(desc) is CacheDesc:
+        got = _native.cache_attention(desc, q, k_cache, v_cache, table, lengths, offsets, tree, o, workspace)
+        if type(got) is tuple:
+            return got[0]
+        if got > 0:
+            raise B.AcceptError(got, "accept_cache_attention")
     where = "accept_cache_attention"
     _check_cache(where, desc, k_cache, v_cache, table, lengths, offsets)
     dtype, sizes = B._DTYPES[desc.dtype], (desc.tokens, desc.heads, desc.head_size)

@@ -34,7 +34,7 @@ template <typename T, int DB>
 __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) void attention_kernel(const AttentionArgs g) {
   constexpr int NB = sizeof(T) == 2 ? 2 : 1, BN = 32 * NB;
   constexpr int kTile = BN * Head<T, DB>::kRowBytes;
-  __shared__ __align__(16) uint8_t tiles[4 * kTile];  // keys, values; and the next ones
+  __shared__ __align__(kTileAlign) uint8_t tiles[4 * kTile];  // keys, values; and the next ones
   const int lane = threadIdx.x % kWave, wave = uniform(int(threadIdx.x / kWave));
   const int half = lane / 32, column = lane % 32;
   const HeadTile ht = deal(blockIdx.x, g.heads, g.tiles);
@@ -93,6 +93,7 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
     __syncthreads();
   }
 
+  const Reader<T, DB> lanes(lane);
   v16f_t acc[DB];
   float largest, sum;
   // A second time where a result is not finite, with products that keep away from a row what it does not see: zero times an
@@ -111,12 +112,13 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
       if (key0 >= wave_limit) continue;
       const uint8_t* const kt = tiles + step % 2 * 2 * kTile;
       const uint8_t* const vt = kt + kTile;
+      const Reader<T, DB> reader = lanes.fresh();
       v16f_t s[NB];
       float most = -INFINITY;
       const bool masked = key0 + BN > first_limit;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        s[nb] = rows_product<T, DB>(kt, nb * 32 + column, half, q);
+        s[nb] = rows_product<T, DB>(lds_offset(kt), reader, nb * 32, q);
         if (masked) {
           const int left = limit - key0 - nb * 32;
 #pragma unroll
@@ -148,7 +150,7 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
         } else {
           Weights<T> w;
           set_weights(w, p);
-          weighted_rows<T, DB>(acc, vt, nb * 32, lane, w);
+          weighted_rows<T, DB>(acc, lds_offset(vt), reader, nb * 32, w);
         }
       }
     }

@@ -153,13 +153,53 @@ struct RowParts {
   }
 };
 
-// 32 rows of a tile times 32 rows in registers: result[row of the tile][row of the registers].
+// Where a lane reads in a tile: every other address of a product is this one with some bits turned over, and a constant added.
+// Tiles begin at multiples of kTileAlign.
+constexpr int kTileAlign = 1024;
+typedef const __attribute__((address_space(3))) v4u_t lds_v4u_t;
+typedef const __attribute__((address_space(3))) float lds_float_t;
+typedef short short4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) short4_t lds_short4_t;
+__device__ __forceinline__ uint4 lds_load16(uint32_t at) {
+  const v4u_t v = *reinterpret_cast<lds_v4u_t*>(at);
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
 template <typename T, int DB>
-__device__ __forceinline__ v16f_t rows_product(const uint8_t* tile, int row, int half, const RowParts<T, DB>& b) {
+struct Reader {
+  static constexpr int ROWB = Head<T, DB>::kRowBytes;
+  uint32_t row;      // part lane/32 of row lane%32
+  uint32_t columns;  // of weighted_rows
+  __device__ __forceinline__ explicit Reader(int lane) {
+    const int half = lane / 32, column = lane % 32;
+    row = uint32_t(part_at<ROWB>(column, half));
+    if constexpr (sizeof(T) == 2) columns = uint32_t(part_at<ROWB>(4 * half + lane % 16 / 4, column / 16 * 2 + lane % 4 / 2) + lane % 2 * 8);
+    else columns = uint32_t(part_at<ROWB>(4 * half, column / 4) + lane % 4 * 4);
+  }
+  // Kept as these two: the compiler would keep all of a product's addresses in registers through the loop instead of making them anew.
+  __device__ __forceinline__ Reader fresh() const {
+    Reader r = *this;
+    asm volatile("" : "+v"(r.row), "+v"(r.columns));
+    return r;
+  }
+};
+
+// 32 rows of a tile (from its row n on, a multiple of 32) times 32 rows in registers: result[row of the tile][row of the registers].
+template <typename T, int DB>
+__device__ __forceinline__ v16f_t rows_product(uint32_t tile, const Reader<T, DB>& reader, int n, const RowParts<T, DB>& b) {
   v16f_t c = {};
+  const uint32_t at = tile + reader.row;
+#pragma unroll
+  for (int i = 0; i < Head<T, DB>::kPairs; ++i) c = multiply_parts<T>(lds_load16((at ^ uint32_t(i << 5)) + n * Head<T, DB>::kRowBytes), b.p[i], c);
+  return c;
+}
+// The same with the other operand's 32 rows in shared memory too.
+template <typename T, int DB>
+__device__ __forceinline__ v16f_t rows_product(uint32_t tile, const Reader<T, DB>& reader, uint32_t other) {
+  v16f_t c = {};
+  const uint32_t at = tile + reader.row, other_at = other + reader.row;
 #pragma unroll
   for (int i = 0; i < Head<T, DB>::kPairs; ++i)
-    c = multiply_parts<T>(*reinterpret_cast<const uint4*>(tile + part_at<Head<T, DB>::kRowBytes>(row, 2 * i + half)), b.p[i], c);
+    c = multiply_parts<T>(lds_load16(at ^ uint32_t(i << 5)), lds_load16(other_at ^ uint32_t(i << 5)), c);
   return c;
 }
 
@@ -185,39 +225,35 @@ __device__ __forceinline__ void set_weights(Weights<bf16_t>& o, const float (&f)
                                                      bf16_pair(f[8 * s + 4], f[8 * s + 5]), bf16_pair(f[8 * s + 6], f[8 * s + 7])));
 }
 
-typedef short short4_t __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) short4_t lds_short4_t;
 // 4 rows x 16 columns of 16 bits, transposed: each lane of 16 gives the address of four neighbours, lane i of row i/4 and columns 4*(i%4), and
 // gets column i of the four rows.
-__device__ __forceinline__ short4_t transposed(const uint8_t* p) {
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t*)(p));
+__device__ __forceinline__ short4_t transposed(uint32_t at) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_short4_t*>(at));
 }
 
-// acc[value of a head][lane's column] += sum over 32 rows of a tile, from row0 (a multiple of 32) on, of x[row][value] * w[row][column].
+// acc[value of a head][lane's column] += sum over 32 rows of a tile, from row n (a multiple of 32) on, of x[row][value] * w[row][column].
 template <typename T, int DB>
-__device__ __forceinline__ void weighted_rows(v16f_t (&acc)[DB], const uint8_t* tile, int row0, int lane, const Weights<T>& w) {
+__device__ __forceinline__ void weighted_rows(v16f_t (&acc)[DB], uint32_t tile, const Reader<T, DB>& reader, int n, const Weights<T>& w) {
   constexpr int ROWB = Head<T, DB>::kRowBytes;
-  const int half = lane / 32;
+  const uint32_t at = tile + reader.columns;
   if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const int row = row0 + 16 * s + 4 * half + lane % 16 / 4;
+    for (int s = 0; s < 2; ++s)
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
-        const int part = db * 4 + lane % 32 / 16 * 2 + lane % 4 / 2, in = lane % 2 * 8;
-        const short4_t lo = transposed(tile + part_at<ROWB>(row, part) + in), hi = transposed(tile + part_at<ROWB>(row + 8, part) + in);
+        const uint32_t from = at ^ uint32_t(db << 6);
+        const short4_t lo = transposed(from + (n + 16 * s) * ROWB), hi = transposed((from ^ 32u) + (n + 16 * s + 8) * ROWB);
         typedef short short8_t __attribute__((ext_vector_type(8)));
         const short8_t a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), w.w[s], acc[db], 0, 0, 0);
       }
-    }
   } else {
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const int row = row0 + result_row(r, half);
+      const uint32_t flips = uint32_t(turn<ROWB>(result_row(r, 0))) << 4;
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
-        const float a = *reinterpret_cast<const float*>(tile + part_at<ROWB>(row, db * 8 + lane % 32 / 4) + lane % 4 * 4);
+        const float a = *reinterpret_cast<lds_float_t*>((at ^ flips ^ uint32_t(db << 7)) + (n + result_row(r, 0)) * ROWB);
         acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w.w[r], acc[db], 0, 0, 0);
       }
     }
@@ -312,14 +348,19 @@ __device__ __forceinline__ void load_tile_part(const void* base, uint32_t offset
   base = reinterpret_cast<const void*>(uniform(int64_t(reinterpret_cast<uintptr_t>(base))));  // (the same for all lanes, whatever register it is in)
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(uniform(int(to))), "v"(offset), "s"(base) : "memory");
 }
+// The same with 4 bytes a lane.
+__device__ __forceinline__ void load_tile_word(const void* base, uint32_t offset, uint32_t to) {
+  base = reinterpret_cast<const void*>(uniform(int64_t(reinterpret_cast<uintptr_t>(base))));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(uniform(int(to))), "v"(offset), "s"(base) : "memory");
+}
 
 // Rows of a tensor into a tile, ROWS of them by WAVES wavefronts: 1024 bytes a wavefront and load.  Rows from `end` on give the last one
 // again; they are not used.  Parts behind head_size are not loaded.
 template <typename T, int DB, int ROWS, int WAVES>
 struct TileRows {
   static constexpr int kRowBytes = Head<T, DB>::kRowBytes, kRowParts = Head<T, DB>::kRowParts;
-  static constexpr int kRowsPer = 1024 / kRowBytes, kLoads = ROWS / kRowsPer / WAVES;
-  static_assert(kRowsPer >= 1 && ROWS % (kRowsPer * WAVES) == 0, "whole loads");
+  static constexpr int kRowsPer = 1024 / kRowBytes, kAll = ROWS / kRowsPer, kLoads = (kAll + WAVES - 1) / WAVES;
+  static_assert(kRowsPer >= 1 && ROWS % kRowsPer == 0, "whole loads");
   uint32_t stride;  // bytes
   int wave, lane, parts;
   uint32_t from[kLoads];
@@ -337,6 +378,7 @@ struct TileRows {
     for (int i = 0; i < kLoads; ++i) {
       uint32_t at = from[i];
       if (left < ROWS) at = uint32_t(row(i) < left ? row(i) : left - 1) * stride + uint32_t(part(i)) * 16u;
+      if (kAll % WAVES != 0 && i * WAVES + wave >= kAll) break;
       if (part(i) < parts) load_tile_part(base, at, to + uint32_t(i * WAVES) * 1024u);
     }
   }

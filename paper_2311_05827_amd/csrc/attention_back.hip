@@ -13,7 +13,7 @@ struct BackArgs {
   const void* v;
   const void* o;
   const float* lse;
-  float* along;  // heads x q_tokens: sums of do * o
+  float* stats;  // heads x q_tokens: sums of do * o; and then as many lse, times log2(e)
   void* dq;
   void* dk;
   void* dv;
@@ -58,7 +58,7 @@ template <typename T, int DB>
 __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) void back_queries_kernel(const BackArgs g) {
   constexpr int BN = 32 * (sizeof(T) == 2 && DB <= 4 ? 2 : 1);
   constexpr int kTile = BN * Head<T, DB>::kRowBytes;
-  __shared__ __align__(16) uint8_t tiles[4 * kTile];
+  __shared__ __align__(kTileAlign) uint8_t tiles[4 * kTile];
   const int lane = threadIdx.x % kWave, wave = uniform(int(threadIdx.x / kWave));
   const int half = lane / 32, column = lane % 32;
   const HeadTile ht = deal(blockIdx.x, g.heads, g.tiles);
@@ -99,8 +99,8 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
     }
     along = halves_sum(along);
   }
-  if (is_row && half == 0) g.along[int64_t(head) * g.q_tokens + token] = along;
   const float lse = g.lse[int64_t(head) * g.q_tokens + token] * kLog2e;
+  if (is_row) g.stats[(int64_t(half) * g.heads + head) * g.q_tokens + token] = half ? lse : along;
   q.load(static_cast<const T*>(g.q) + token * g.q_stride + int64_t(head) * g.head, half, parts);
 
   const T* const k0 = static_cast<const T*>(g.k) + ks.begin * g.k_stride + int64_t(head / g.group) * g.head;
@@ -115,6 +115,7 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
     clear_tiles<4 * kTile, kWaves * kWave>(tiles);
     __syncthreads();
   }
+  const Reader<T, DB> lanes(lane);
   v16f_t acc[DB];
   const auto run = [&](auto apart) {  // (see attention_kernel)
 #pragma unroll
@@ -128,11 +129,12 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
       if (key0 >= wave_limit) continue;
       const uint8_t* const kt = tiles + step % 2 * 2 * kTile;
       const uint8_t* const vt = kt + kTile;
+      const Reader<T, DB> reader = lanes.fresh();
       const bool masked = key0 + BN > first_limit;
 #pragma unroll
       for (int n = 0; n < BN; n += 32) {
-        const v16f_t s = rows_product<T, DB>(kt, n + column, half, q);
-        const v16f_t dp = rows_product<T, DB>(vt, n + column, half, dout);
+        const v16f_t s = rows_product<T, DB>(lds_offset(kt), reader, n, q);
+        const v16f_t dp = rows_product<T, DB>(lds_offset(vt), reader, n, dout);
         float ds[16];
 #pragma unroll
         for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], g.scale2, -lse)) * (dp[r] - along);
@@ -146,7 +148,7 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
         } else {
           Weights<T> w;
           set_weights(w, ds);
-          weighted_rows<T, DB>(acc, kt, n, lane, w);
+          weighted_rows<T, DB>(acc, lds_offset(kt), reader, n, w);
         }
       }
     }
@@ -156,14 +158,16 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
   if (is_row) store_column<T, DB>(dq + token * g.dq_stride, acc, half, g.head, g.scale);
 }
 
-// dk and dv: 128 keys of a key head, a lane has a key of its own; tiles of queries and their do come through shared memory, head after head of
-// those that share the key head.
+// dk and dv: 128 keys of a key head, a lane has a key of its own; tiles of 32 queries and their do come through shared memory, head after
+// head of those that share the key head.  Wide heads in bfloat16 leave their values in shared memory: with both gradients' sums and the
+// keys in registers there are two wavefronts a SIMD then, one of which multiplies while the other one exponentiates.
 template <typename T, int DB>
-__global__ __launch_bounds__(kWaves * kWave, DB <= 2 && sizeof(T) == 2 ? 2 : 1) void back_keys_kernel(const BackArgs g) {
-  constexpr int BM = 32 * (sizeof(T) == 2 && DB <= 4 ? 2 : 1);
+__global__ __launch_bounds__(kWaves * kWave, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void back_keys_kernel(const BackArgs g) {
+  constexpr int BM = 32;
   constexpr int kTile = BM * Head<T, DB>::kRowBytes;
-  __shared__ __align__(16) uint8_t tiles[4 * kTile];
-  __shared__ float stats[2][2][BM];  // logarithms, sums of do * o
+  constexpr bool kValuesInLds = sizeof(T) == 2 && (DB == 3 || DB == 4);
+  __shared__ __align__(kTileAlign) uint8_t tiles[4 * kTile + (kValuesInLds ? kRows * Head<T, DB>::kRowBytes : 0)];
+  __shared__ __align__(16) float stats[2][2][BM];
   const int lane = threadIdx.x % kWave, wave = uniform(int(threadIdx.x / kWave));
   const int half = lane / 32, column = lane % 32;
   const HeadTile ht = deal(blockIdx.x, g.kv_heads, g.tiles);
@@ -188,80 +192,94 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 2 && sizeof(T) == 2 ? 2 : 1) 
   const int from = seen_from(is_key ? key : last);
   const int wave_from = seen_from(key0), wave_all = seen_from(key0 + 31);
   const int first = seen_from(piece.tile * kRows) / BM;  // tile of queries
-  const int each = pieces(rows, BM) - first, steps = each > 0 ? each * g.group : 0;
+  const int each = pieces(rows, BM) - first;
 
   const int parts = g.head * int(sizeof(T)) / 16;
   const int64_t token = ks.begin + (is_key ? key : last);
-  RowParts<T, DB> k, v;
-  k.load(static_cast<const T*>(g.k) + token * g.k_stride + int64_t(head) * g.head, half, parts);
-  v.load(static_cast<const T*>(g.v) + token * g.v_stride + int64_t(head) * g.head, half, parts);
-  const TileRows<T, DB, BM, kWaves> q_rows(wave, lane, g.q_stride, parts), o_rows(wave, lane, g.o_stride, parts);
-  const auto fetch = [&](int step) {
-    uint8_t* const to = tiles + step % 2 * 2 * kTile;
-    const int h = head * g.group + step / each, row = (first + step % each) * BM, left = rows - row;
-    const int64_t at = qs.begin + row;
-    q_rows.fetch(static_cast<const T*>(g.q) + at * g.q_stride + int64_t(h) * g.head, left, to);
-    o_rows.fetch(static_cast<const T*>(g.dout) + at * g.o_stride + int64_t(h) * g.head, left, to + kTile);
-  };
-  // rows' statistics: loaded with the tile, stored when it has come
-  const auto statistic = [&](int step) {
-    const int h = head * g.group + step / each, row = (first + step % each) * BM + int(threadIdx.x) % BM;
-    const int64_t at = int64_t(h) * g.q_tokens + qs.begin + (row < rows ? row : rows - 1);
-    return int(threadIdx.x) < BM ? g.lse[at] * kLog2e : int(threadIdx.x) < 2 * BM ? g.along[at] : 0.0f;
-  };
   if (g.head < DB * 32) {
-    clear_tiles<4 * kTile, kWaves * kWave>(tiles);
+    clear_tiles<int(sizeof(tiles)), kWaves * kWave>(tiles);
     __syncthreads();
   }
+  uint8_t* const values = tiles + 4 * kTile;
+  RowParts<T, DB> k, v;
+  if constexpr (kValuesInLds) {
+    const TileRows<T, DB, kRows, kWaves> v_rows(wave, lane, g.v_stride, parts);
+    v_rows.fetch(static_cast<const T*>(g.v) + (ks.begin + int64_t(piece.tile) * kRows) * g.v_stride + int64_t(head) * g.head,
+                 keys - piece.tile * kRows, values);
+  } else {
+    v.load(static_cast<const T*>(g.v) + token * g.v_stride + int64_t(head) * g.head, half, parts);
+  }
+  k.load(static_cast<const T*>(g.k) + token * g.k_stride + int64_t(head) * g.head, half, parts);
+  const TileRows<T, DB, BM, kWaves> q_rows(wave, lane, g.q_stride, parts), o_rows(wave, lane, g.o_stride, parts);
+  const auto fetch = [&](int h, int tile, int b) {
+    uint8_t* const to = tiles + b * 2 * kTile;
+    const int row = tile * BM;
+    const int64_t at = qs.begin + row;
+    q_rows.fetch(static_cast<const T*>(g.q) + at * g.q_stride + int64_t(h) * g.head, rows - row, to);
+    o_rows.fetch(static_cast<const T*>(g.dout) + at * g.o_stride + int64_t(h) * g.head, rows - row, to + kTile);
+    if (wave < 2 && lane < BM)  // the rows' sums of do * o, and their logarithms
+      load_tile_word(g.stats + (int64_t(wave) * g.heads + h) * g.q_tokens + at, uint32_t(lane < rows - row ? lane : rows - row - 1) * 4u, lds_offset(stats[b][wave]));
+  };
+  const Reader<T, DB> lanes(lane);
   v16f_t sum_k[DB], sum_v[DB];
   const auto run = [&](auto apart) {  // (see attention_kernel)
 #pragma unroll
     for (int db = 0; db < DB; ++db) sum_k[db] = v16f_t{}, sum_v[db] = v16f_t{};
-    float mine = 0.0f;
-    if (steps > 0) {
-      mine = statistic(0);
-      fetch(0);
-    }
-    for (int step = 0; step < steps; ++step) {
-      if (int(threadIdx.x) < 2 * BM) stats[step % 2][threadIdx.x / BM][threadIdx.x % BM] = mine;
+    if (each <= 0) return;
+    // from the last queries down: the workgroups of a sequence, which have different first ones, are at the same ones then
+    const int tile_last = first + each - 1;
+    int h = head * g.group, tile = tile_last, b = 0;
+    const int h_end = h + g.group;
+    fetch(h, tile, 0);
+    while (h < h_end) {
       __builtin_amdgcn_s_waitcnt(0);
       __syncthreads();
-      if (step + 1 < steps) {
-        mine = statistic(step + 1);
-        fetch(step + 1);
-      }
-      const int row0 = (first + step % each) * BM;
-      const uint8_t* const qt = tiles + step % 2 * 2 * kTile;
+      const int row0 = tile * BM;
+      const uint8_t* const qt = tiles + b * 2 * kTile;
       const uint8_t* const ot = qt + kTile;
+      const float* const stat = stats[b][0];
+      if (--tile < first) tile = tile_last, ++h;
+      b ^= 1;
+      if (h < h_end) {
+        fetch(h, tile, b);
+      }
+      if (row0 + 31 < wave_from || key0 >= keys) continue;
+      const bool masked = row0 < wave_all || row0 + 32 > rows || key0 + 32 > keys;
+      const Reader<T, DB> reader = lanes.fresh();
+      const v16f_t s = rows_product<T, DB>(lds_offset(qt), reader, 0, k);
+      v16f_t dp;
+      if constexpr (kValuesInLds) dp = rows_product<T, DB>(lds_offset(ot), reader, lds_offset(values) + uint32_t(wave * 32 * Head<T, DB>::kRowBytes));
+      else dp = rows_product<T, DB>(lds_offset(ot), reader, 0, v);
+      float p[16], ds[16];
+      const uint32_t seen = masked ? bits_between(from - row0, rows - row0) : ~0u;
 #pragma unroll
-      for (int n = 0; n < BM; n += 32) {
-        if (row0 + n + 31 < wave_from || row0 + n >= rows || key0 >= keys) continue;
-        const bool masked = row0 + n < wave_all || row0 + n + 32 > rows || key0 + 32 > keys;
-        const v16f_t s = rows_product<T, DB>(qt, n + column, half, k);
-        const v16f_t dp = rows_product<T, DB>(ot, n + column, half, v);
-        float p[16], ds[16];
-        const uint32_t seen = bits_between(from - row0 - n, rows - row0 - n);
+      for (int q = 0; q < 4; ++q) {
+        const float4 sums = *reinterpret_cast<const float4*>(stat + q * 8 + half * 4), logs = *reinterpret_cast<const float4*>(stat + BM + q * 8 + half * 4);
+        const float l[4] = {logs.x, logs.y, logs.z, logs.w}, e[4] = {sums.x, sums.y, sums.z, sums.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int r = 4 * q + j;
+          p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], g.scale2, -l[j]));
+          ds[r] = p[r] * (dp[r] - e[j]);
+        }
+      }
+      if (masked) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const int i = result_row(r, half);
-          p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], g.scale2, -stats[step % 2][0][n + i]));
-          ds[r] = p[r] * (dp[r] - stats[step % 2][1][n + i]);
-          if (masked) {
-            const bool sees = seen >> i & 1;
-            p[r] = sees ? p[r] : 0.0f;
-            ds[r] = sees ? ds[r] : 0.0f;
-          }
+          const bool sees = seen >> result_row(r, half) & 1;
+          p[r] = sees ? p[r] : 0.0f;
+          ds[r] = sees ? ds[r] : 0.0f;
         }
-        if (apart.value && masked) {
-          weighted_rows_apart<T, DB>(sum_v, ot, n, lane, p, seen);
-          weighted_rows_apart<T, DB>(sum_k, qt, n, lane, ds, seen);
-        } else {
-          Weights<T> w;
-          set_weights(w, p);
-          weighted_rows<T, DB>(sum_v, ot, n, lane, w);
-          set_weights(w, ds);
-          weighted_rows<T, DB>(sum_k, qt, n, lane, w);
-        }
+      }
+      if (apart.value && masked) {
+        weighted_rows_apart<T, DB>(sum_v, ot, 0, lane, p, seen);
+        weighted_rows_apart<T, DB>(sum_k, qt, 0, lane, ds, seen);
+      } else {
+        Weights<T> wp, ws;
+        set_weights(wp, p);
+        set_weights(ws, ds);
+        weighted_rows<T, DB>(sum_v, lds_offset(ot), reader, 0, wp);
+        weighted_rows<T, DB>(sum_k, lds_offset(qt), reader, 0, ws);
       }
     }
   };
@@ -297,7 +315,7 @@ hipError_t launch(const BackArgs& g, int q_tiles, int k_tiles, hipStream_t s) {
 }  // namespace
 
 AttentionBackPlan make_attention_back_plan(const accept_attention_desc& d) {
-  return {size_t(up_to(4 * int64_t(d.heads) * d.q_tokens, 256))};
+  return {size_t(up_to(8 * int64_t(d.heads) * d.q_tokens, 256))};
 }
 
 hipError_t launch_attention_backward(const accept_attention_desc& d, const AttentionBackPlan&, const void* dout, const void* q,
@@ -307,7 +325,7 @@ hipError_t launch_attention_backward(const accept_attention_desc& d, const Atten
   const int64_t whole = int64_t(d.heads) * d.head_size, kv_whole = int64_t(d.kv_heads) * d.head_size;
   const auto stride = [](int64_t given, int64_t otherwise) { return given ? given : otherwise; };
   g.dout = dout, g.q = q, g.k = k, g.v = v, g.o = o, g.lse = lse;
-  g.along = static_cast<float*>(ws);
+  g.stats = static_cast<float*>(ws);
   g.dq = dq, g.dk = dk, g.dv = dv;
   g.q_offsets = q_offsets, g.k_offsets = k_offsets;
   g.q_stride = stride(d.q_stride, whole), g.o_stride = stride(d.o_stride, whole), g.dq_stride = stride(d.dq_stride, whole);

@@ -72,7 +72,7 @@ __global__ __launch_bounds__((Shape<T, DB>::kThreads), 1) void cached_kernel(con
   using S = Shape<T, DB>;
   using H = Head<T, DB>;
   constexpr int kWidth = DB * 32, kPad = kItem + 1;
-  __shared__ __align__(16) uint8_t tiles[S::kWaves][4 * S::kTile];
+  __shared__ __align__(kTileAlign) uint8_t tiles[S::kWaves][4 * S::kTile];
   __shared__ float peak[S::kWaves][kItem], total[S::kWaves][kItem];
   const int lane = threadIdx.x % kWave, wave = uniform(int(threadIdx.x / kWave));
   const int half = lane / 32, column = lane % 32;
@@ -170,6 +170,7 @@ __global__ __launch_bounds__((Shape<T, DB>::kThreads), 1) void cached_kernel(con
       return seen;
     };
 
+    const Reader<T, DB> lanes(lane);
     v16f_t acc[DB];
     float largest, sum;
     const int stop = some_see < unit1 * S::kUnit ? some_see : unit1 * S::kUnit;
@@ -188,7 +189,8 @@ __global__ __launch_bounds__((Shape<T, DB>::kThreads), 1) void cached_kernel(con
         if (key0 + S::kUnit < stop) there = fetch(key0 + S::kUnit, b ^ 1);
         const uint8_t* const kt = mine + b * 2 * S::kTile;
         const uint8_t* const vt = kt + S::kTile;
-        v16f_t s = rows_product<T, DB>(kt, column, half, q);
+        const Reader<T, DB> reader = lanes.fresh();
+        v16f_t s = rows_product<T, DB>(lds_offset(kt), reader, 0, q);
         const bool masked = key0 + 32 > all_see || now_there != ~0u;
         uint32_t seen = ~0u;
         if (masked) {
@@ -220,7 +222,7 @@ __global__ __launch_bounds__((Shape<T, DB>::kThreads), 1) void cached_kernel(con
         } else {
           Weights<T> w;
           set_weights(w, p);
-          weighted_rows<T, DB>(acc, vt, 0, lane, w);
+          weighted_rows<T, DB>(acc, lds_offset(vt), reader, 0, w);
         }
       }
     };
@@ -274,11 +276,16 @@ __global__ __launch_bounds__((Shape<T, DB>::kThreads), 1) void cached_kernel(con
   }
 }
 
+constexpr int kMaxParts = 256;  // of a key head's work
+__device__ __forceinline__ int up_to_block(int v) { return (v + kBlock - 1) / kBlock * kBlock; }
+
 // Items in several pieces: their results together; and zeros for tokens behind the last sequence.
 template <typename T, int DB>
 __global__ __launch_bounds__(kBlock) void cached_join_kernel(const CacheArgs g) {
   using S = Shape<T, DB>;
   constexpr int kWidth = DB * 32;
+  __shared__ float factors[kMaxParts][kItem], sums[kMaxParts][kItem], total[kItem];
+  __shared__ v4f_t halves[kBlock];
   const int kv = blockIdx.y;
   const Found f = find_among(g.sequences, blockIdx.x, [&](int s) { return step_of(g, s, S::kUnit).items; });
   const int seq = uniform(f.seq);
@@ -312,20 +319,57 @@ __global__ __launch_bounds__(kBlock) void cached_join_kernel(const CacheArgs g) 
   if (p0 == p1) return;  // its part wrote the result
   const int64_t rows = int64_t(st.span.size()) * g.group, row0 = item * kItem;
   const int count = int(rows - row0 < kItem ? rows - row0 : kItem);
-  for (int i = threadIdx.x; i < count * g.head; i += kBlock) {
-    const int r = i / g.head, d = i % g.head;
-    float top = -INFINITY;
-    for (int p = p0; p <= p1; ++p) top = fmaxf(top, slot_at(g, kv, p, p == p0, kWidth)[kItem * kWidth + r]);
-    float v = 0.0f, l = 0.0f;
-    for (int p = p0; p <= p1; ++p) {
-      const float* const slot = slot_at(g, kv, p, p == p0, kWidth);
-      const float peak = slot[kItem * kWidth + r], factor = peak == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(peak - top);
-      v = fmaf(factor, slot[r * kWidth + d], v);
-      l = fmaf(factor, slot[kItem * kWidth + kItem + r], l);
+  const int pieces_of = p1 - p0 + 1;  // at most kBlock
+  // what every piece counts for in every row
+  for (int i = threadIdx.x; i < count * pieces_of; i += kBlock) {
+    const int r = i % count, p = i / count;
+    const float* const slot = slot_at(g, kv, p0 + p, p == 0, kWidth) + kItem * kWidth;
+    factors[p][r] = slot[r];
+    sums[p][r] = slot[kItem + r];
+  }
+  __syncthreads();
+  if (int(threadIdx.x) < count) {
+    const int r = threadIdx.x;
+    float top = -INFINITY, l = 0.0f;
+    for (int p = 0; p < pieces_of; ++p) top = fmaxf(top, factors[p][r]);
+    for (int p = 0; p < pieces_of; ++p) {
+      const float f = factors[p][r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(factors[p][r] - top);
+      factors[p][r] = f;
+      l = fmaf(f, sums[p][r], l);
     }
-    const int64_t flat = row0 + r;
-    store_one(static_cast<T*>(g.o) + (st.span.begin + flat / g.group) * g.o_stride + (kv * g.group + flat % g.group) * g.head + d,
-              l == 0.0f ? 0.0f : v / l);
+    total[r] = l;
+  }
+  __syncthreads();
+  // four values a thread; where there are few, several threads share the pieces
+  constexpr int kFours = kWidth / 4;
+  const int fours = count * kFours, shares = fours >= kBlock ? 1 : kBlock / fours;
+  for (int i = threadIdx.x; i < up_to_block(fours); i += kBlock) {
+    const int share = shares > 1 ? i / fours : 0, at = shares > 1 ? i % fours : i;
+    const int r = at / kFours, d = at % kFours * 4;
+    v4f_t v = {0, 0, 0, 0};
+    if (at < fours && share < shares) {
+#pragma unroll 4
+      for (int p = share; p < pieces_of; p += shares) {
+        const v4f_t x = *reinterpret_cast<const v4f_t*>(slot_at(g, kv, p0 + p, p == 0, kWidth) + r * kWidth + d);
+        const float f = factors[p][r];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = fmaf(f, x[j], v[j]);
+      }
+    }
+    if (shares > 1) {
+      halves[threadIdx.x] = v;
+      __syncthreads();
+      if (share == 0)
+        for (int o = 1; o < shares; ++o) v += halves[threadIdx.x + o * fours];
+    }
+    if (share == 0 && at < fours && d < g.head) {
+      const int64_t flat = row0 + r;
+      T* const to = static_cast<T*>(g.o) + (st.span.begin + flat / g.group) * g.o_stride + (kv * g.group + flat % g.group) * g.head + d;
+      const float inverse = total[r] == 0.0f ? 0.0f : 1.0f / total[r];
+      const float f[4] = {v[0] * inverse, v[1] * inverse, v[2] * inverse, v[3] * inverse};
+      if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(to) = make_float4(f[0], f[1], f[2], f[3]);
+      else *reinterpret_cast<uint2*>(to) = make_uint2(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3]));
+    }
   }
 }
 
@@ -354,6 +398,7 @@ CachePlan make_cache_plan(const accept_cache_desc& d) {
   // as many workgroups as the chip has room for: one a compute unit, more where shared memory takes more
   constexpr int kUnits = 256;
   p.parts = int((kUnits + d.kv_heads - 1) / d.kv_heads);
+  static_assert(kUnits <= kMaxParts, "what a row's pieces count for is in shared memory");
   const int width = blocks_of_head(d.head_size) * 32;
   p.bytes = size_t(up_to(int64_t(d.kv_heads) * p.parts * 2 * kItem * (width + 2) * 4, 256));
   return p;

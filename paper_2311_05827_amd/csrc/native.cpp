@@ -12,6 +12,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "accept.h"
+#include "accept_attention.h"
 #include "accept_stage.h"
 
 namespace {
@@ -380,10 +381,244 @@ PyObject* block_matmul(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   });
 }
 
+// ---- the attention operators (accept_attention.h) ---------------------------------------------------------------------
+// What a call allocates holds zeros for tokens of no sequence; what it is given follows the descriptor.
+struct Tokens {
+  Checked& c;
+  at::ScalarType type;
+  // (tokens, heads, head) or (tokens, heads * head), tokens `stride` (0: as many) apart, 16-byte aligned
+  void operator()(const at::Tensor* t, int64_t tokens, int64_t heads, int64_t head, int64_t stride) const {
+    if (!c.here(t, type)) return;
+    const int64_t whole = heads * head;
+    const bool three = t->dim() == 3;
+    if (!three && t->dim() != 2) {
+      c.ok = false;
+      return;
+    }
+    c.ok = t->size(0) == tokens && (three ? t->size(1) == heads && t->size(2) == head : t->size(1) == whole);
+    if (!c.ok || tokens == 0) return;
+    c.ok = t->stride(-1) == 1 && (!three || heads == 1 || t->stride(1) == head) && (tokens == 1 || t->stride(0) == (stride ? stride : whole)) &&
+           reinterpret_cast<uintptr_t>(t->data_ptr()) % 16 == 0;
+  }
+};
+void ints(Checked& c, const at::Tensor* t, int64_t size) { c.flat(t, at::kInt, size); }
+bool shared_out(const at::Tensor* offsets, int64_t sequences, int64_t tokens) {
+  return offsets || (sequences > 0 ? tokens % sequences == 0 : tokens == 0);
+}
+at::Tensor make_tokens(const at::Tensor& like, int64_t tokens, int64_t heads, int64_t head, int64_t stride, at::ScalarType type) {
+  const int64_t whole = heads * head;
+  if (stride == 0 || stride == whole) return make(like, {tokens, heads, head}, type);
+  return make(like, {tokens, stride}, type).narrow(1, 0, whole).unflatten(1, {heads, head});
+}
+const int32_t* int_pointer(const at::Tensor* t) { return t ? static_cast<const int32_t*>(t->data_ptr()) : nullptr; }
+
+// rotate(desc, x, frequencies, offsets, positions, y) -> (y,), a status or kNotHere
+PyObject* rotate(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return guarded([&]() -> PyObject* {
+    View<accept_rotate_desc> dv;
+    const accept_rotate_desc* given = nargs == 6 ? dv.get(args[0]) : nullptr;
+    if (!given || (given->dtype != ACCEPT_F32 && given->dtype != ACCEPT_BF16) || given->sequences < 0 || given->tokens < 0 || given->heads < 1 ||
+        given->head_size < 1 || given->y_stride < 0)
+      return PyLong_FromLong(kNotHere);
+    accept_rotate_desc d = *given;
+    Checked c;
+    const at::Tensor *x = c.get(args[1], false), *f = c.get(args[2], d.rotated == 0), *off = c.get(args[3], true), *pos = c.get(args[4], true),
+                     *y = c.get(args[5], true);
+    const Tokens tokens{c, value_type(d.dtype)};
+    tokens(x, d.tokens, d.heads, d.head_size, d.x_stride);
+    if (f) c.flat(f, at::kFloat, d.rotated / 2);
+    if (off) ints(c, off, d.sequences + 1);
+    if (pos) ints(c, pos, d.tokens);
+    if (!pos) c.ok = c.ok && shared_out(off, d.sequences, d.tokens);
+    if (y) tokens(y, d.tokens, d.heads, d.head_size, d.y_stride);
+    if (!c.ok || (d.y_stride && d.y_stride < int64_t(d.heads) * d.head_size)) return PyLong_FromLong(kNotHere);
+    at::Tensor my;
+    if (!y) {
+      my = make_tokens(*x, d.tokens, d.heads, d.head_size, d.y_stride, x->scalar_type()), y = &my;
+      if (off) d.rest = ACCEPT_REST_ZEROS;
+    }
+    void *xp = pointer(x), *fp = pointer(f), *yp = pointer(y);
+    const int32_t *op = int_pointer(off), *pp = int_pointer(pos);
+    const accept_status st = call([&] { return accept_rotate(&d, xp, static_cast<const float*>(fp), op, pp, yp, c.stream); });
+    return st == ACCEPT_OK ? tuple_of({y}) : PyLong_FromLong(st);
+  });
+}
+
+// attention(desc, q, k, v, q_offsets, k_offsets, o, lse, workspace) -> (o, lse), a status or kNotHere
+PyObject* attention(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return guarded([&]() -> PyObject* {
+    View<accept_attention_desc> dv;
+    const accept_attention_desc* given = nargs == 9 ? dv.get(args[0]) : nullptr;
+    size_t wb = 0;
+    if (!given || accept_attention_workspace_size(given, &wb) != ACCEPT_OK) return PyLong_FromLong(kNotHere);
+    accept_attention_desc d = *given;
+    Checked c;
+    const at::Tensor *q = c.get(args[1], false), *k = c.get(args[2], false), *v = c.get(args[3], false), *qo = c.get(args[4], true),
+                     *ko = c.get(args[5], true), *o = c.get(args[6], true), *lse = c.get(args[7], true), *ws = c.get(args[8], true);
+    const Tokens tokens{c, value_type(d.dtype)};
+    tokens(q, d.q_tokens, d.heads, d.head_size, d.q_stride);
+    tokens(k, d.k_tokens, d.kv_heads, d.head_size, d.k_stride);
+    tokens(v, d.k_tokens, d.kv_heads, d.head_size, d.v_stride);
+    if (qo) ints(c, qo, d.sequences + 1);
+    if (ko) ints(c, ko, d.sequences + 1);
+    c.ok = c.ok && shared_out(qo, d.sequences, d.q_tokens) && shared_out(ko, d.sequences, d.k_tokens);
+    if (o) tokens(o, d.q_tokens, d.heads, d.head_size, d.o_stride);
+    if (lse) c.table(lse, at::kFloat, d.heads, d.q_tokens);
+    if (wb && ws) c.ok = c.ok && fits(ws, wb) && ws->get_device() == c.device;
+    if (!c.ok) return PyLong_FromLong(kNotHere);
+    at::Tensor mo, ml, mws;
+    if (!o) {
+      mo = make_tokens(*q, d.q_tokens, d.heads, d.head_size, d.o_stride, q->scalar_type()), o = &mo;
+      if (qo) d.rest = ACCEPT_REST_ZEROS;
+    }
+    if (!lse) ml = make(*q, {d.heads, d.q_tokens}, at::kFloat), lse = &ml;
+    if (wb && !ws) mws = make(*q, {int64_t(wb)}, at::kByte), ws = &mws;
+    void *qp = pointer(q), *kp = pointer(k), *vp = pointer(v), *op = pointer(o), *lp = pointer(lse), *wp = wb ? pointer(ws) : nullptr;
+    const int32_t *qop = int_pointer(qo), *kop = int_pointer(ko);
+    const accept_status st =
+        call([&] { return accept_attention(&d, qp, kp, vp, qop, kop, op, static_cast<float*>(lp), wp, c.stream); });
+    return st == ACCEPT_OK ? tuple_of({o, lse}) : PyLong_FromLong(st);
+  });
+}
+
+// attention_backward(desc, do, q, k, v, o, lse, q_offsets, k_offsets, dq, dk, dv, workspace) -> (dq, dk, dv), a status or kNotHere
+PyObject* attention_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return guarded([&]() -> PyObject* {
+    View<accept_attention_desc> dv;
+    const accept_attention_desc* given = nargs == 13 ? dv.get(args[0]) : nullptr;
+    size_t wb = 0;
+    if (!given || accept_attention_backward_workspace_size(given, &wb) != ACCEPT_OK) return PyLong_FromLong(kNotHere);
+    accept_attention_desc d = *given;
+    // all three gradients made here, or all given: the slow way takes what lies between
+    const int missing = (args[9] == Py_None) + (args[10] == Py_None) + (args[11] == Py_None);
+    if (missing != 0 && missing != 3) return PyLong_FromLong(kNotHere);
+    Checked c;
+    const at::Tensor *dout = c.get(args[1], false), *q = c.get(args[2], false), *k = c.get(args[3], false), *v = c.get(args[4], false),
+                     *o = c.get(args[5], false), *lse = c.get(args[6], false), *qo = c.get(args[7], true), *ko = c.get(args[8], true),
+                     *dq = c.get(args[9], true), *dk = c.get(args[10], true), *dvt = c.get(args[11], true), *ws = c.get(args[12], true);
+    const Tokens tokens{c, value_type(d.dtype)};
+    tokens(q, d.q_tokens, d.heads, d.head_size, d.q_stride);
+    tokens(k, d.k_tokens, d.kv_heads, d.head_size, d.k_stride);
+    tokens(v, d.k_tokens, d.kv_heads, d.head_size, d.v_stride);
+    tokens(o, d.q_tokens, d.heads, d.head_size, d.o_stride);
+    tokens(dout, d.q_tokens, d.heads, d.head_size, d.o_stride);
+    c.table(lse, at::kFloat, d.heads, d.q_tokens);
+    if (qo) ints(c, qo, d.sequences + 1);
+    if (ko) ints(c, ko, d.sequences + 1);
+    c.ok = c.ok && shared_out(qo, d.sequences, d.q_tokens) && shared_out(ko, d.sequences, d.k_tokens);
+    if (!missing) {
+      tokens(dq, d.q_tokens, d.heads, d.head_size, d.dq_stride);
+      tokens(dk, d.k_tokens, d.kv_heads, d.head_size, d.dk_stride);
+      tokens(dvt, d.k_tokens, d.kv_heads, d.head_size, d.dv_stride);
+    }
+    if (wb && ws) c.ok = c.ok && fits(ws, wb) && ws->get_device() == c.device;
+    if (!c.ok) return PyLong_FromLong(kNotHere);
+    at::Tensor mq, mk, mv, mws;
+    if (missing) {
+      mq = make_tokens(*q, d.q_tokens, d.heads, d.head_size, d.dq_stride, q->scalar_type()), dq = &mq;
+      mk = make_tokens(*q, d.k_tokens, d.kv_heads, d.head_size, d.dk_stride, q->scalar_type()), dk = &mk;
+      mv = make_tokens(*q, d.k_tokens, d.kv_heads, d.head_size, d.dv_stride, q->scalar_type()), dvt = &mv;
+      if (qo || ko) d.rest = ACCEPT_REST_ZEROS;
+    }
+    if (wb && !ws) mws = make(*q, {int64_t(wb)}, at::kByte), ws = &mws;
+    void *dp = pointer(dout), *qp = pointer(q), *kp = pointer(k), *vp = pointer(v), *op = pointer(o), *lp = pointer(lse), *dqp = pointer(dq),
+         *dkp = pointer(dk), *dvp = pointer(dvt), *wp = wb ? pointer(ws) : nullptr;
+    const int32_t *qop = int_pointer(qo), *kop = int_pointer(ko);
+    const accept_status st = call([&] {
+      return accept_attention_backward(&d, dp, qp, kp, vp, op, static_cast<const float*>(lp), qop, kop, dqp, dkp, dvp, wp, c.stream);
+    });
+    return st == ACCEPT_OK ? tuple_of({dq, dk, dvt}) : PyLong_FromLong(st);
+  });
+}
+
+// The caches, table, lengths and offsets of a call.
+void check_cache(Checked& c, const accept_cache_desc& d, const at::Tensor* k_cache, const at::Tensor* v_cache, const at::Tensor* table,
+                 const at::Tensor* lengths, const at::Tensor* offsets) {
+  for (const at::Tensor* t : {k_cache, v_cache})
+    if (c.here(t, value_type(d.dtype)))
+      c.ok = t->dim() == 4 && t->size(0) == d.pages && t->size(1) == d.kv_heads && t->size(2) == d.page_size && t->size(3) == d.head_size &&
+             t->is_contiguous() && reinterpret_cast<uintptr_t>(t->data_ptr()) % 16 == 0;
+  c.table(table, at::kInt, d.sequences, d.table_pages);
+  ints(c, lengths, d.sequences);
+  if (offsets) ints(c, offsets, d.sequences + 1);
+  c.ok = c.ok && shared_out(offsets, d.sequences, d.tokens);
+}
+
+// cache_append(desc, q, k, v, k_cache, v_cache, table, lengths, offsets, positions, frequencies, q_out) -> (q_out or None,), a status or kNotHere
+PyObject* cache_append(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return guarded([&]() -> PyObject* {
+    View<accept_cache_desc> dv;
+    const accept_cache_desc* given = nargs == 12 ? dv.get(args[0]) : nullptr;
+    size_t wb = 0;
+    if (!given || accept_cache_workspace_size(given, &wb) != ACCEPT_OK) return PyLong_FromLong(kNotHere);
+    accept_cache_desc d = *given;
+    Checked c;
+    const at::Tensor *q = c.get(args[1], true), *k = c.get(args[2], false), *v = c.get(args[3], false), *kc = c.get(args[4], false),
+                     *vc = c.get(args[5], false), *table = c.get(args[6], false), *lengths = c.get(args[7], false), *off = c.get(args[8], true),
+                     *pos = c.get(args[9], true), *f = c.get(args[10], d.rotated == 0), *out = c.get(args[11], true);
+    if (!c.ok) return PyLong_FromLong(kNotHere);
+    check_cache(c, d, kc, vc, table, lengths, off);
+    const Tokens tokens{c, value_type(d.dtype)};
+    if (q) tokens(q, d.tokens, d.heads, d.head_size, d.q_stride);
+    tokens(k, d.tokens, d.kv_heads, d.head_size, d.k_stride);
+    tokens(v, d.tokens, d.kv_heads, d.head_size, d.v_stride);
+    if (pos) ints(c, pos, d.tokens);
+    if (f) c.flat(f, at::kFloat, d.rotated / 2);
+    if (out) tokens(out, d.tokens, d.heads, d.head_size, d.qo_stride);
+    if (!c.ok || (out && !q)) return PyLong_FromLong(kNotHere);
+    at::Tensor mo;
+    if (q && !out) {
+      mo = make_tokens(*q, d.tokens, d.heads, d.head_size, d.qo_stride, q->scalar_type()), out = &mo;
+      if (off) d.rest = ACCEPT_REST_ZEROS;
+    }
+    void *qp = pointer(q), *kp = pointer(k), *vp = pointer(v), *fp = pointer(f), *op = pointer(out), *kcp = pointer(kc), *vcp = pointer(vc);
+    const int32_t *offp = int_pointer(off), *lp = int_pointer(lengths), *pp = int_pointer(pos), *tp = int_pointer(table);
+    const accept_status st =
+        call([&] { return accept_cache_append(&d, qp, kp, vp, static_cast<const float*>(fp), offp, lp, pp, tp, op, kcp, vcp, c.stream); });
+    return st == ACCEPT_OK ? tuple_of({out}) : PyLong_FromLong(st);
+  });
+}
+
+// cache_attention(desc, q, k_cache, v_cache, table, lengths, offsets, tree, o, workspace) -> (o,), a status or kNotHere
+PyObject* cache_attention(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return guarded([&]() -> PyObject* {
+    View<accept_cache_desc> dv;
+    const accept_cache_desc* given = nargs == 10 ? dv.get(args[0]) : nullptr;
+    size_t wb = 0;
+    if (!given || accept_cache_workspace_size(given, &wb) != ACCEPT_OK) return PyLong_FromLong(kNotHere);
+    accept_cache_desc d = *given;
+    Checked c;
+    const at::Tensor *q = c.get(args[1], false), *kc = c.get(args[2], false), *vc = c.get(args[3], false), *table = c.get(args[4], false),
+                     *lengths = c.get(args[5], false), *off = c.get(args[6], true), *tree = c.get(args[7], d.tree_words == 0),
+                     *o = c.get(args[8], true), *ws = c.get(args[9], true);
+    if (!c.ok || (tree && d.tree_words == 0)) return PyLong_FromLong(kNotHere);
+    check_cache(c, d, kc, vc, table, lengths, off);
+    const Tokens tokens{c, value_type(d.dtype)};
+    tokens(q, d.tokens, d.heads, d.head_size, d.q_stride);
+    if (tree) c.table(tree, at::kLong, d.tokens, d.tree_words);
+    if (o) tokens(o, d.tokens, d.heads, d.head_size, d.o_stride);
+    if (wb && ws) c.ok = c.ok && fits(ws, wb) && ws->get_device() == c.device;
+    if (!c.ok) return PyLong_FromLong(kNotHere);
+    at::Tensor mo, mws;
+    if (!o) {
+      mo = make_tokens(*q, d.tokens, d.heads, d.head_size, d.o_stride, q->scalar_type()), o = &mo;
+      if (off) d.rest = ACCEPT_REST_ZEROS;
+    }
+    if (wb && !ws) mws = make(*q, {int64_t(wb)}, at::kByte), ws = &mws;
+    void *qp = pointer(q), *kcp = pointer(kc), *vcp = pointer(vc), *op = pointer(o), *wp = wb ? pointer(ws) : nullptr, *tp = pointer(tree);
+    const int32_t *offp = int_pointer(off), *lp = int_pointer(lengths), *tabp = int_pointer(table);
+    const accept_status st =
+        call([&] { return accept_cache_attention(&d, qp, kcp, vcp, offp, lp, tabp, static_cast<const uint64_t*>(tp), op, wp, c.stream); });
+    return st == ACCEPT_OK ? tuple_of({o}) : PyLong_FromLong(st);
+  });
+}
+
 #define ACCEPT_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     ACCEPT_METHOD(compress), ACCEPT_METHOD(decompress), ACCEPT_METHOD(layer_norm), ACCEPT_METHOD(layer_norm_quantize),
     ACCEPT_METHOD(layer_norm_backward), ACCEPT_METHOD(block_quantize), ACCEPT_METHOD(block_matmul),
+    ACCEPT_METHOD(rotate), ACCEPT_METHOD(attention), ACCEPT_METHOD(attention_backward), ACCEPT_METHOD(cache_append),
+    ACCEPT_METHOD(cache_attention),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
