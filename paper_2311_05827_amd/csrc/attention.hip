@@ -63,7 +63,7 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
     seq = ht.tile / each;
     tile = ht.tile - seq * each;
   }
-  const Span qs = span_of(g.q_offsets, seq, g.q_tokens, g.q_each), ks = span_of(g.k_offsets, seq, g.k_tokens, g.k_each);
+  const Span qs = uniform_span(g.q_offsets, seq, g.q_tokens, g.q_each), ks = uniform_span(g.k_offsets, seq, g.k_tokens, g.k_each);
   const int rows = qs.size(), keys = ks.size();
   const int more = keys - rows;  // query i sees keys up to i + more
 
@@ -71,7 +71,11 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
   const bool is_row = row < rows;
   const auto seen_by = [&](int i) { return !g.causal ? keys : i + 1 + more < 0 ? 0 : i + 1 + more; };
   const int last = rows - 1;
-  const int limit = seen_by(row < rows ? row : last);         // this lane's query sees keys before it
+  // this lane's query sees keys before it
+  const auto limit = [&] {
+    const int i = row0 + fresh_lane() % 32;
+    return seen_by(i < rows ? i : last);
+  };
   const int first_limit = row0 < rows ? seen_by(row0) : 0;    // all of the wavefront's queries do
   const int wave_limit = row0 < rows ? seen_by(row0 + 31 < last ? row0 + 31 : last) : 0;
   const int end = tile * kRows + kRows - 1;
@@ -80,9 +84,9 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
   const int parts = g.head * int(sizeof(T)) / 16;
   RowParts<T, DB> q;
   q.load(static_cast<const T*>(g.q) + (qs.begin + (is_row ? row : last)) * g.q_stride + int64_t(head) * g.head, half, parts);
-  const T* const k0 = static_cast<const T*>(g.k) + ks.begin * g.k_stride + int64_t(head / g.group) * g.head;
-  const T* const v0 = static_cast<const T*>(g.v) + ks.begin * g.v_stride + int64_t(head / g.group) * g.head;
-  const TileRows<T, DB, BN, kWaves> k_rows(wave, lane, g.k_stride, parts), v_rows(wave, lane, g.v_stride, parts);
+  const T* const k0 = uniform(static_cast<const T*>(g.k) + ks.begin * g.k_stride + int64_t(head / g.group) * g.head);
+  const T* const v0 = uniform(static_cast<const T*>(g.v) + ks.begin * g.v_stride + int64_t(head / g.group) * g.head);
+  const TileRows<T, DB, BN, kWaves> k_rows(wave, g.k_stride, parts), v_rows(wave, g.v_stride, parts);
   const auto fetch = [&](int step) {
     uint8_t* const to = tiles + step % 2 * 2 * kTile;
     k_rows.fetch(k0 + int64_t(step) * BN * g.k_stride, keys - step * BN, to);
@@ -120,9 +124,9 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
       for (int nb = 0; nb < NB; ++nb) {
         s[nb] = rows_product<T, DB>(lds_offset(kt), reader, nb * 32, q);
         if (masked) {
-          const int left = limit - key0 - nb * 32;
+          const int left = limit() - key0 - nb * 32 - fresh_lane() / 32 * 4;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[nb][r] = result_row(r, half) < left ? s[nb][r] : -INFINITY;
+          for (int r = 0; r < 16; ++r) s[nb][r] = result_row(r, 0) < left ? s[nb][r] : -INFINITY;
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) most = fmaxf(most, s[nb][r]);
@@ -146,7 +150,7 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
           sum += p[r];
         }
         if (apart.value && masked) {
-          weighted_rows_apart<T, DB>(acc, vt, nb * 32, lane, p, bits_between(0, limit - key0 - nb * 32));
+          weighted_rows_apart<T, DB>(acc, vt, nb * 32, fresh_lane(), p, bits_between(0, limit() - key0 - nb * 32));
         } else {
           Weights<T> w;
           set_weights(w, p);

@@ -47,6 +47,25 @@ struct Flag {
   static constexpr bool value = B;
 };
 
+// A value that is the same for all lanes, in a scalar register, and with it what is computed from it.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+  return int64_t(uint64_t(uint32_t(uniform(int(v >> 32)))) << 32 | uint32_t(uniform(int(v))));
+}
+
+template <typename P>
+__device__ __forceinline__ P* uniform(P* p) {
+  return reinterpret_cast<P*>(uniform(int64_t(reinterpret_cast<uintptr_t>(p))));
+}
+
+// The lane's number, made anew: what is computed from it in a loop takes no register through the loop.  (Loops here fill the registers, and a value
+// that does not fit and is loaded from memory waits for all loads in front of it, the next tiles' among them.)
+__device__ __forceinline__ int fresh_lane() {
+  int lane;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(lane));
+  return lane;
+}
+
 // ---- sequences ---------------------------------------------------------------------------------
 // First token and end of a sequence; whatever the offsets hold, inside 0 .. tokens.
 struct Span {
@@ -59,6 +78,10 @@ __device__ __forceinline__ Span span_of(const int32_t* offsets, int s, int token
   b = b < 0 ? 0 : b > tokens ? tokens : b;
   e = e < b ? b : e > tokens ? tokens : e;
   return {b, e};
+}
+__device__ __forceinline__ Span uniform_span(const int32_t* offsets, int s, int tokens, int each) {
+  const Span span = span_of(offsets, s, tokens, each);
+  return {uniform(span.begin), uniform(span.end)};
 }
 // The tokens behind the last sequence begin here.
 __device__ __forceinline__ int rest_of(const int32_t* offsets, int sequences, int tokens) {
@@ -94,12 +117,6 @@ __device__ __forceinline__ Found find_among(int sequences, int64_t at, const F& 
   }
   return {-1, before};
 }
-// (both of them uniform values: in scalar registers)
-__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-__device__ __forceinline__ int64_t uniform(int64_t v) {
-  return int64_t(uint64_t(uint32_t(uniform(int(v >> 32)))) << 32 | uint32_t(uniform(int(v))));
-}
-
 // ---- tiles in shared memory, and products of 32 x 32 ---------------------------------------------
 // A tile is rows of ROWB bytes, head_size up to a power of two; a row's 16-byte parts lie in an order of their own, part ^ turn(row), so that
 // 16 rows' parts of one number, and four rows' 64 neighbouring bytes (which a transposing read takes), meet no bank twice.
@@ -345,12 +362,12 @@ __device__ __forceinline__ uint32_t lds_offset(const void* p) {
 // 16 bytes a lane from base + offset to shared memory, `to` on, lane by lane; lanes that are off load and write nothing.  Nothing waits for it but an
 // explicit wait for all loads (the compiler would wait before every read of shared memory).
 __device__ __forceinline__ void load_tile_part(const void* base, uint32_t offset, uint32_t to) {
-  base = reinterpret_cast<const void*>(uniform(int64_t(reinterpret_cast<uintptr_t>(base))));  // (the same for all lanes, whatever register it is in)
+  base = uniform(base);  // (the same for all lanes, whatever register it is in)
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(uniform(int(to))), "v"(offset), "s"(base) : "memory");
 }
 // The same with 4 bytes a lane.
 __device__ __forceinline__ void load_tile_word(const void* base, uint32_t offset, uint32_t to) {
-  base = reinterpret_cast<const void*>(uniform(int64_t(reinterpret_cast<uintptr_t>(base))));
+  base = uniform(base);
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(uniform(int(to))), "v"(offset), "s"(base) : "memory");
 }
 
@@ -361,25 +378,42 @@ struct TileRows {
   static constexpr int kRowBytes = Head<T, DB>::kRowBytes, kRowParts = Head<T, DB>::kRowParts;
   static constexpr int kRowsPer = 1024 / kRowBytes, kAll = ROWS / kRowsPer, kLoads = (kAll + WAVES - 1) / WAVES;
   static_assert(kRowsPer >= 1 && ROWS % kRowsPer == 0, "whole loads");
+  static constexpr int kStep = kRowsPer * WAVES;      // rows from a load to the next
+  static constexpr bool kAlike = kStep % 16 == 0;     // whose parts then lie in the same order
   uint32_t stride;  // bytes
-  int wave, lane, parts;
-  uint32_t from[kLoads];
-  __device__ __forceinline__ TileRows(int wave_, int lane_, int64_t stride_elements, int parts_)
-      : stride(uint32_t(stride_elements) * uint32_t(sizeof(T))), wave(wave_), lane(lane_), parts(parts_) {
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) from[i] = uint32_t(row(i)) * stride + uint32_t(part(i)) * 16u;
-  }
-  __device__ __forceinline__ int row(int i) const { return (i * WAVES + wave) * kRowsPer + lane / kRowParts; }
-  __device__ __forceinline__ int part(int i) const { return lane % kRowParts ^ turn<kRowBytes>(row(i)); }
+  int wave, parts;
+  __device__ __forceinline__ TileRows(int wave_, int64_t stride_elements, int parts_)
+      : stride(uint32_t(stride_elements) * uint32_t(sizeof(T))), wave(wave_), parts(parts_) {}
   // rows first .. first + ROWS - 1 behind `base`, of which there are `left`, at least one
   __device__ __forceinline__ void fetch(const void* base, int left, const uint8_t* tile) const {
     const uint32_t to = lds_offset(tile) + uint32_t(wave) * 1024u;
+    const int lane = fresh_lane();
+    const auto row = [&](int i) { return (i * WAVES + wave) * kRowsPer + lane / kRowParts; };
+    const auto part = [&](int i) { return lane % kRowParts ^ turn<kRowBytes>(row(kAlike ? 0 : i)); };
+    const auto from = [&](int i) { return uint32_t(row(i)) * stride + uint32_t(part(i)) * 16u; };
+    const auto each = [&](const auto& load) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      uint32_t at = from[i];
-      if (left < ROWS) at = uint32_t(row(i) < left ? row(i) : left - 1) * stride + uint32_t(part(i)) * 16u;
-      if (kAll % WAVES != 0 && i * WAVES + wave >= kAll) break;
-      if (part(i) < parts) load_tile_part(base, at, to + uint32_t(i * WAVES) * 1024u);
+      for (int i = 0; i < kLoads; ++i)
+        if (kAll % WAVES == 0 || i * WAVES + wave < kAll) load(i, to + uint32_t(i * WAVES) * 1024u);
+    };
+    const auto whole = [&](int i, uint32_t to_i) {
+      load_tile_part(static_cast<const uint8_t*>(base) + (kAlike ? uint32_t(i * kStep) * uint64_t(stride) : 0), from(kAlike ? 0 : i), to_i);
+    };
+    const auto short_of = [&](int i, uint32_t to_i) {
+      load_tile_part(base, uint32_t(row(i) < left ? row(i) : left - 1) * stride + uint32_t(part(i)) * 16u, to_i);
+    };
+    if constexpr (kAlike) {
+      if (part(0) < parts) {
+        if (left >= ROWS) each(whole);
+        else each(short_of);
+      }
+    } else {
+      each([&](int i, uint32_t to_i) {
+        if (part(i) < parts) {
+          if (left >= ROWS) whole(i, to_i);
+          else short_of(i, to_i);
+        }
+      });
     }
   }
 };

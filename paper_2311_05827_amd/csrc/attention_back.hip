@@ -69,12 +69,15 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
     if (g.zeros) clear_rest(dq, g.dq_stride, g.head, rest_of(g.q_offsets, g.sequences, g.q_tokens), piece.tile, g.q_tokens);
     return;
   }
-  const Span qs = span_of(g.q_offsets, piece.seq, g.q_tokens, g.q_each), ks = span_of(g.k_offsets, piece.seq, g.k_tokens, g.k_each);
+  const Span qs = uniform_span(g.q_offsets, piece.seq, g.q_tokens, g.q_each), ks = uniform_span(g.k_offsets, piece.seq, g.k_tokens, g.k_each);
   const int rows = qs.size(), keys = ks.size(), more = keys - rows, last = rows - 1;
   const int row0 = piece.tile * kRows + wave * 32, row = row0 + column;
   const bool is_row = row < rows;
   const auto seen_by = [&](int i) { return !g.causal ? keys : i + 1 + more < 0 ? 0 : i + 1 + more; };
-  const int limit = seen_by(is_row ? row : last);
+  const auto limit = [&] {
+    const int i = row0 + fresh_lane() % 32;
+    return seen_by(i < rows ? i : last);
+  };
   const int first_limit = row0 < rows ? seen_by(row0) : 0;
   const int wave_limit = row0 < rows ? seen_by(row0 + 31 < last ? row0 + 31 : last) : 0;
   const int end = piece.tile * kRows + kRows - 1;
@@ -103,9 +106,9 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
   if (is_row) g.stats[(int64_t(half) * g.heads + head) * g.q_tokens + token] = half ? lse : along;
   q.load(static_cast<const T*>(g.q) + token * g.q_stride + int64_t(head) * g.head, half, parts);
 
-  const T* const k0 = static_cast<const T*>(g.k) + ks.begin * g.k_stride + int64_t(head / g.group) * g.head;
-  const T* const v0 = static_cast<const T*>(g.v) + ks.begin * g.v_stride + int64_t(head / g.group) * g.head;
-  const TileRows<T, DB, BN, kWaves> k_rows(wave, lane, g.k_stride, parts), v_rows(wave, lane, g.v_stride, parts);
+  const T* const k0 = uniform(static_cast<const T*>(g.k) + ks.begin * g.k_stride + int64_t(head / g.group) * g.head);
+  const T* const v0 = uniform(static_cast<const T*>(g.v) + ks.begin * g.v_stride + int64_t(head / g.group) * g.head);
+  const TileRows<T, DB, BN, kWaves> k_rows(wave, g.k_stride, parts), v_rows(wave, g.v_stride, parts);
   const auto fetch = [&](int step) {
     uint8_t* const to = tiles + step % 2 * 2 * kTile;
     k_rows.fetch(k0 + int64_t(step) * BN * g.k_stride, keys - step * BN, to);
@@ -138,13 +141,13 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
         float ds[16];
 #pragma unroll
         for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], g.scale2, -lse)) * (dp[r] - along);
-        const int left = limit - key0 - n;
         if (masked) {
+          const int left = limit() - key0 - n - fresh_lane() / 32 * 4;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) ds[r] = result_row(r, half) < left ? ds[r] : 0.0f;
+          for (int r = 0; r < 16; ++r) ds[r] = result_row(r, 0) < left ? ds[r] : 0.0f;
         }
         if (apart.value && masked) {
-          weighted_rows_apart<T, DB>(acc, kt, n, lane, ds, bits_between(0, left));
+          weighted_rows_apart<T, DB>(acc, kt, n, fresh_lane(), ds, bits_between(0, limit() - key0 - n));
         } else {
           Weights<T> w;
           set_weights(w, ds);
@@ -183,13 +186,12 @@ __global__ __launch_bounds__(kWaves * kWave, sizeof(T) == 2 && DB <= 4 ? 2 : 1) 
     }
     return;
   }
-  const Span qs = span_of(g.q_offsets, piece.seq, g.q_tokens, g.q_each), ks = span_of(g.k_offsets, piece.seq, g.k_tokens, g.k_each);
+  const Span qs = uniform_span(g.q_offsets, piece.seq, g.q_tokens, g.q_each), ks = uniform_span(g.k_offsets, piece.seq, g.k_tokens, g.k_each);
   const int rows = qs.size(), keys = ks.size(), more = keys - rows, last = keys - 1;
   const int key0 = piece.tile * kRows + wave * 32, key = key0 + column;
   const bool is_key = key < keys;
   // the first query that sees a key
   const auto seen_from = [&](int j) { return !g.causal || j - more < 0 ? 0 : j - more; };
-  const int from = seen_from(is_key ? key : last);
   const int wave_from = seen_from(key0), wave_all = seen_from(key0 + 31);
   const int first = seen_from(piece.tile * kRows) / BM;  // tile of queries
   const int each = pieces(rows, BM) - first;
@@ -203,22 +205,24 @@ __global__ __launch_bounds__(kWaves * kWave, sizeof(T) == 2 && DB <= 4 ? 2 : 1) 
   uint8_t* const values = tiles + 4 * kTile;
   RowParts<T, DB> k, v;
   if constexpr (kValuesInLds) {
-    const TileRows<T, DB, kRows, kWaves> v_rows(wave, lane, g.v_stride, parts);
+    const TileRows<T, DB, kRows, kWaves> v_rows(wave, g.v_stride, parts);
     v_rows.fetch(static_cast<const T*>(g.v) + (ks.begin + int64_t(piece.tile) * kRows) * g.v_stride + int64_t(head) * g.head,
                  keys - piece.tile * kRows, values);
   } else {
     v.load(static_cast<const T*>(g.v) + token * g.v_stride + int64_t(head) * g.head, half, parts);
   }
   k.load(static_cast<const T*>(g.k) + token * g.k_stride + int64_t(head) * g.head, half, parts);
-  const TileRows<T, DB, BM, kWaves> q_rows(wave, lane, g.q_stride, parts), o_rows(wave, lane, g.o_stride, parts);
+  const TileRows<T, DB, BM, kWaves> q_rows(wave, g.q_stride, parts), o_rows(wave, g.o_stride, parts);
   const auto fetch = [&](int h, int tile, int b) {
     uint8_t* const to = tiles + b * 2 * kTile;
     const int row = tile * BM;
     const int64_t at = qs.begin + row;
     q_rows.fetch(static_cast<const T*>(g.q) + at * g.q_stride + int64_t(h) * g.head, rows - row, to);
     o_rows.fetch(static_cast<const T*>(g.dout) + at * g.o_stride + int64_t(h) * g.head, rows - row, to + kTile);
-    if (wave < 2 && lane < BM)  // the rows' sums of do * o, and their logarithms
-      load_tile_word(g.stats + (int64_t(wave) * g.heads + h) * g.q_tokens + at, uint32_t(lane < rows - row ? lane : rows - row - 1) * 4u, lds_offset(stats[b][wave]));
+    const int lane_now = fresh_lane();
+    if (wave < 2 && lane_now < BM)  // the rows' sums of do * o, and their logarithms
+      load_tile_word(g.stats + (int64_t(wave) * g.heads + h) * g.q_tokens + at, uint32_t(lane_now < rows - row ? lane_now : rows - row - 1) * 4u,
+                     lds_offset(stats[b][wave]));
   };
   const Reader<T, DB> lanes(lane);
   v16f_t sum_k[DB], sum_v[DB];
@@ -237,7 +241,7 @@ __global__ __launch_bounds__(kWaves * kWave, sizeof(T) == 2 && DB <= 4 ? 2 : 1) 
       const int row0 = tile * BM;
       const uint8_t* const qt = tiles + b * 2 * kTile;
       const uint8_t* const ot = qt + kTile;
-      const float* const stat = stats[b][0];
+      const float* const stat = stats[b][0] + fresh_lane() / 32 * 4;
       if (--tile < first) tile = tile_last, ++h;
       b ^= 1;
       if (h < h_end) {
@@ -251,10 +255,9 @@ __global__ __launch_bounds__(kWaves * kWave, sizeof(T) == 2 && DB <= 4 ? 2 : 1) 
       if constexpr (kValuesInLds) dp = rows_product<T, DB>(lds_offset(ot), reader, lds_offset(values) + uint32_t(wave * 32 * Head<T, DB>::kRowBytes));
       else dp = rows_product<T, DB>(lds_offset(ot), reader, 0, v);
       float p[16], ds[16];
-      const uint32_t seen = masked ? bits_between(from - row0, rows - row0) : ~0u;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const float4 sums = *reinterpret_cast<const float4*>(stat + q * 8 + half * 4), logs = *reinterpret_cast<const float4*>(stat + BM + q * 8 + half * 4);
+        const float4 sums = *reinterpret_cast<const float4*>(stat + q * 8), logs = *reinterpret_cast<const float4*>(stat + BM + q * 8);
         const float l[4] = {logs.x, logs.y, logs.z, logs.w}, e[4] = {sums.x, sums.y, sums.z, sums.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -263,17 +266,21 @@ __global__ __launch_bounds__(kWaves * kWave, sizeof(T) == 2 && DB <= 4 ? 2 : 1) 
           ds[r] = p[r] * (dp[r] - e[j]);
         }
       }
+      uint32_t seen = ~0u;
       if (masked) {
+        const int lane_now = fresh_lane(), j = key0 + lane_now % 32;
+        seen = bits_between(seen_from(j < keys ? j : last) - row0, rows - row0);
+        const uint32_t here = seen >> (lane_now / 32 * 4);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const bool sees = seen >> result_row(r, half) & 1;
+          const bool sees = here >> result_row(r, 0) & 1;
           p[r] = sees ? p[r] : 0.0f;
           ds[r] = sees ? ds[r] : 0.0f;
         }
       }
       if (apart.value && masked) {
-        weighted_rows_apart<T, DB>(sum_v, ot, 0, lane, p, seen);
-        weighted_rows_apart<T, DB>(sum_k, qt, 0, lane, ds, seen);
+        weighted_rows_apart<T, DB>(sum_v, ot, 0, fresh_lane(), p, seen);
+        weighted_rows_apart<T, DB>(sum_k, qt, 0, fresh_lane(), ds, seen);
       } else {
         Weights<T> wp, ws;
         set_weights(wp, p);

@@ -58,6 +58,10 @@ __device__ __forceinline__ Step step_of(const CacheArgs& g, int seq, int unit) {
   s.units = units > 0 ? units : 1;
   return s;
 }
+__device__ __forceinline__ Step uniform_step(const CacheArgs& g, int seq, int unit) {
+  const Step s = step_of(g, seq, unit);
+  return {{uniform(s.span.begin), uniform(s.span.end)}, uniform(s.length), uniform(s.keys), uniform(s.items), uniform(s.units)};
+}
 // Work of a key head, in units one behind the other, is dealt in equal parts.  A part has at most two pieces of items that are not whole: the end of one that
 // began before it, and the beginning of one that goes on behind it.
 __device__ __forceinline__ int64_t part_begin(int64_t all, int parts, int p) { return all * p / parts; }
@@ -97,7 +101,7 @@ __global__ __launch_bounds__((Shape<T, DB>::kThreads), 1) void cached_kernel(con
   }
 
   while (at < end && seq < g.sequences) {
-    const Step st = step_of(g, seq, S::kUnit);
+    const Step st = uniform_step(g, seq, S::kUnit);
     const int64_t in = at - before;
     if (in >= st.items * st.units) {
       before += st.items * st.units;
@@ -170,7 +174,7 @@ __global__ __launch_bounds__((Shape<T, DB>::kThreads), 1) void cached_kernel(con
       return seen;
     };
 
-    const Reader<T, DB> lanes(lane);
+      const Reader<T, DB> lanes(lane);
     v16f_t acc[DB];
     float largest, sum;
     const int stop = some_see < unit1 * S::kUnit ? some_see : unit1 * S::kUnit;
@@ -300,7 +304,7 @@ __global__ __launch_bounds__(kBlock) void cached_join_kernel(const CacheArgs g) 
     }
     return;
   }
-  const Step st = step_of(g, seq, S::kUnit);
+  const Step st = uniform_step(g, seq, S::kUnit);
   const auto work = [&](int s) {
     const Step each = step_of(g, s, S::kUnit);
     return each.items * each.units;
