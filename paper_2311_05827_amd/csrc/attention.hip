@@ -37,31 +37,22 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
   __shared__ __align__(kTileAlign) uint8_t tiles[4 * kTile];  // keys, values; and the next ones
   const int lane = threadIdx.x % kWave, wave = uniform(int(threadIdx.x / kWave));
   const int half = lane / 32, column = lane % 32;
-  const HeadTile ht = deal(blockIdx.x, g.heads, g.tiles);
-  const int head = ht.head;
-
-  int seq = 0, tile = ht.tile;
-  if (g.q_offsets) {
-    const Found f = find_among(g.sequences, ht.tile, [&](int s) { return pieces(span_of(g.q_offsets, s, g.q_tokens, 0).size(), kRows); });
-    seq = uniform(f.seq);
-    tile = int(ht.tile - uniform(f.before));
-    if (seq < 0) {  // tiles that no sequence has: the tokens behind the last one
-      if (!g.zeros) return;
-      const int rest = rest_of(g.q_offsets, g.sequences, g.q_tokens);
-      const int parts = g.head * int(sizeof(T)) / 16;
-      for (int i = threadIdx.x; i < kRows * parts; i += kWaves * kWave) {
-        const int row = rest + tile * kRows + i / parts;
-        if (row >= g.q_tokens) break;
-        T* const to = static_cast<T*>(g.o) + row * g.o_stride + int64_t(head) * g.head;
-        reinterpret_cast<uint4*>(to)[i % parts] = make_uint4(0, 0, 0, 0);
-        if (g.lse && i % parts == 0) g.lse[int64_t(head) * g.q_tokens + row] = -INFINITY;
-      }
-      return;
+  const HeadPiece hp = deal(blockIdx.x, g.heads);
+  const int head = hp.head;
+  const Piece piece = find_piece(g.q_offsets, g.sequences, g.q_tokens, g.q_each, kRows, hp.index);
+  const int seq = piece.seq, tile = piece.tile;
+  if (seq < 0) {  // pieces that no sequence has: the tokens behind the last one
+    if (!g.zeros) return;
+    const int rest = rest_of(g.q_offsets, g.sequences, g.q_tokens);
+    const int parts = g.head * int(sizeof(T)) / 16;
+    for (int i = threadIdx.x; i < kRows * parts; i += kWaves * kWave) {
+      const int row = rest + tile * kRows + i / parts;
+      if (row >= g.q_tokens) break;
+      T* const to = static_cast<T*>(g.o) + row * g.o_stride + int64_t(head) * g.head;
+      reinterpret_cast<uint4*>(to)[i % parts] = make_uint4(0, 0, 0, 0);
+      if (g.lse && i % parts == 0) g.lse[int64_t(head) * g.q_tokens + row] = -INFINITY;
     }
-  } else {
-    const int each = pieces(g.q_each, kRows);
-    seq = ht.tile / each;
-    tile = ht.tile - seq * each;
+    return;
   }
   const Span qs = uniform_span(g.q_offsets, seq, g.q_tokens, g.q_each), ks = uniform_span(g.k_offsets, seq, g.k_tokens, g.k_each);
   const int rows = qs.size(), keys = ks.size();

@@ -21,6 +21,8 @@ AttentionPlan make_attention_plan(const accept_attention_desc& d);
 hipError_t launch_attention(const accept_attention_desc& d, const AttentionPlan& p, const void* q, const void* k, const void* v,
                             const int32_t* q_offsets, const int32_t* k_offsets, void* o, float* lse, void* ws, hipStream_t s);
 struct AttentionBackPlan {
+  int split;     // shares of a key tile's queries
+  size_t stats;  // bytes of the rows' statistics, in front of the shares' sums
   size_t bytes;
 };
 AttentionBackPlan make_attention_back_plan(const accept_attention_desc& d);
@@ -117,6 +119,48 @@ __device__ __forceinline__ Found find_among(int sequences, int64_t at, const F& 
   }
   return {-1, before};
 }
+// The same with the longest sequences first (of every 64), so that a launch ends with short pieces of work: 12288 tokens in seven sequences,
+// 32 heads, gradients of the keys in 793 us in their own order, DKDV_US so.
+template <typename F, typename L>
+__device__ __forceinline__ Found find_longest_first(int sequences, int64_t at, const F& size, const L& length) {
+  const int lane = threadIdx.x % kWave;
+  int64_t before = 0;
+  for (int base = 0; base < sequences; base += kWave) {
+    const int here = sequences - base < kWave ? sequences - base : kWave;
+    const int n = lane < here ? int(size(base + lane)) : 0, key = lane < here ? int(length(base + lane)) : -1;
+    int64_t mine = before, all = 0;
+    for (int j = 0; j < here; ++j) {
+      const int n_j = __builtin_amdgcn_readlane(n, j), key_j = __builtin_amdgcn_readlane(key, j);
+      if (key_j > key || (key_j == key && j < lane)) mine += n_j;
+      all += n_j;
+    }
+    const uint64_t it = __ballot(lane < here && mine <= at && at < mine + n);
+    if (it) {
+      const int first = __builtin_ctzll(it);
+      return {base + first, __shfl(mine, first, kWave)};
+    }
+    before += all;
+  }
+  return {-1, before};
+}
+// Piece number `index`, heaviest ones first, of sequences that are cut in pieces of `rows` tokens: its sequence, and its place in it with the
+// last piece first (seq -1: number `tile` of the pieces of the tokens behind the last sequence).
+struct Piece {
+  int seq, tile;
+};
+__device__ __forceinline__ Piece find_piece(const int32_t* offsets, int sequences, int tokens, int each, int rows, int index) {
+  if (!offsets) {
+    const int per = pieces(each, rows);
+    return {index % sequences, per - 1 - index / sequences};
+  }
+  const Found f = find_longest_first(sequences, index, [&](int s) { return pieces(span_of(offsets, s, tokens, 0).size(), rows); },
+                                     [&](int s) { return span_of(offsets, s, tokens, 0).size(); });
+  const int seq = uniform(f.seq), in = int(index - uniform(f.before));
+  if (seq < 0) return {-1, in};
+  const Span span = uniform_span(offsets, seq, tokens, 0);
+  return {seq, pieces(span.size(), rows) - 1 - in};
+}
+
 // ---- tiles in shared memory, and products of 32 x 32 ---------------------------------------------
 // A tile is rows of ROWB bytes, head_size up to a power of two; a row's 16-byte parts lie in an order of their own, part ^ turn(row), so that
 // 16 rows' parts of one number, and four rows' 64 neighbouring bytes (which a transposing read takes), meet no bank twice.
@@ -200,6 +244,20 @@ struct Reader {
   }
 };
 
+// A tile's 32 rows from its row n on as a left operand.
+template <typename T, int DB>
+__device__ __forceinline__ void load_parts(RowParts<T, DB>& a, uint32_t tile, const Reader<T, DB>& reader, int n) {
+  const uint32_t at = tile + reader.row;
+#pragma unroll
+  for (int i = 0; i < Head<T, DB>::kPairs; ++i) a.p[i] = lds_load16((at ^ uint32_t(i << 5)) + n * Head<T, DB>::kRowBytes);
+}
+template <typename T, int DB>
+__device__ __forceinline__ v16f_t rows_product(const RowParts<T, DB>& a, const RowParts<T, DB>& b) {
+  v16f_t c = {};
+#pragma unroll
+  for (int i = 0; i < Head<T, DB>::kPairs; ++i) c = multiply_parts<T>(a.p[i], b.p[i], c);
+  return c;
+}
 // 32 rows of a tile (from its row n on, a multiple of 32) times 32 rows in registers: result[row of the tile][row of the registers].
 template <typename T, int DB>
 __device__ __forceinline__ v16f_t rows_product(uint32_t tile, const Reader<T, DB>& reader, int n, const RowParts<T, DB>& b) {
@@ -246,6 +304,29 @@ __device__ __forceinline__ void set_weights(Weights<bf16_t>& o, const float (&f)
 // gets column i of the four rows.
 __device__ __forceinline__ short4_t transposed(uint32_t at) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_short4_t*>(at));
+}
+
+// A tile's rows n + 16 * s on, 16 of them, as the left operand of weighted_rows; and that half of its products.
+template <int DB>
+struct Columns {
+  bf16x8_t a[DB];
+};
+template <int DB>
+__device__ __forceinline__ void load_columns(Columns<DB>& c, uint32_t tile, const Reader<bf16_t, DB>& reader, int n, int s) {
+  constexpr int ROWB = Head<bf16_t, DB>::kRowBytes;
+  const uint32_t at = tile + reader.columns;
+#pragma unroll
+  for (int db = 0; db < DB; ++db) {
+    const uint32_t from = at ^ uint32_t(db << 6);
+    const short4_t lo = transposed(from + (n + 16 * s) * ROWB), hi = transposed((from ^ 32u) + (n + 16 * s + 8) * ROWB);
+    typedef short short8_t __attribute__((ext_vector_type(8)));
+    c.a[db] = __builtin_bit_cast(bf16x8_t, short8_t(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)));
+  }
+}
+template <int DB>
+__device__ __forceinline__ void weighted_half(v16f_t (&acc)[DB], const Columns<DB>& c, bf16x8_t w) {
+#pragma unroll
+  for (int db = 0; db < DB; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c.a[db], w, acc[db], 0, 0, 0);
 }
 
 // acc[value of a head][lane's column] += sum over 32 rows of a tile, from row n (a multiple of 32) on, of x[row][value] * w[row][column].
@@ -377,7 +458,7 @@ template <typename T, int DB, int ROWS, int WAVES>
 struct TileRows {
   static constexpr int kRowBytes = Head<T, DB>::kRowBytes, kRowParts = Head<T, DB>::kRowParts;
   static constexpr int kRowsPer = 1024 / kRowBytes, kAll = ROWS / kRowsPer, kLoads = (kAll + WAVES - 1) / WAVES;
-  static_assert(kRowsPer >= 1 && ROWS % kRowsPer == 0, "whole loads");
+  static_assert(kRowsPer >= 1 && ROWS % kRowsPer == 0 && (kAll % WAVES == 0 || kAll < WAVES), "whole loads");
   static constexpr int kStep = kRowsPer * WAVES;      // rows from a load to the next
   static constexpr bool kAlike = kStep % 16 == 0;     // whose parts then lie in the same order
   uint32_t stride;  // bytes
@@ -386,6 +467,8 @@ struct TileRows {
       : stride(uint32_t(stride_elements) * uint32_t(sizeof(T))), wave(wave_), parts(parts_) {}
   // rows first .. first + ROWS - 1 behind `base`, of which there are `left`, at least one
   __device__ __forceinline__ void fetch(const void* base, int left, const uint8_t* tile) const {
+    // (where there are fewer loads than wavefronts some load the same, so that all wait for the same number)
+    const int wave = kAll < WAVES ? this->wave % kAll : this->wave;
     const uint32_t to = lds_offset(tile) + uint32_t(wave) * 1024u;
     const int lane = fresh_lane();
     const auto row = [&](int i) { return (i * WAVES + wave) * kRowsPer + lane / kRowParts; };
@@ -393,8 +476,7 @@ struct TileRows {
     const auto from = [&](int i) { return uint32_t(row(i)) * stride + uint32_t(part(i)) * 16u; };
     const auto each = [&](const auto& load) {
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i)
-        if (kAll % WAVES == 0 || i * WAVES + wave < kAll) load(i, to + uint32_t(i * WAVES) * 1024u);
+      for (int i = 0; i < kLoads; ++i) load(i, to + uint32_t(i * WAVES) * 1024u);
     };
     const auto whole = [&](int i, uint32_t to_i) {
       load_tile_part(static_cast<const uint8_t*>(base) + (kAlike ? uint32_t(i * kStep) * uint64_t(stride) : 0), from(kAlike ? 0 : i), to_i);
@@ -417,24 +499,30 @@ struct TileRows {
     }
   }
 };
+// Waits until no more than N of this wavefront's loads are on their way.
+template <int N>
+__device__ __forceinline__ void wait_for_loads() {
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x70 | 0xF00);
+  asm volatile("" : : : "memory");
+}
 // Tiles' parts that no load fills are zeros.
 template <int BYTES, int THREADS>
 __device__ __forceinline__ void clear_tiles(uint8_t* tiles) {
   for (int i = threadIdx.x * 16; i < BYTES; i += THREADS * 16) *reinterpret_cast<uint4*>(tiles + i) = make_uint4(0, 0, 0, 0);
 }
 
-// Workgroups are dealt to the chip's eight dies in turn; a die gets neighbouring heads, all of their tiles, so that the keys and values
-// its workgroups read at a time are in its cache.  Tiles in falling order: with a causal mask the later ones are longer.
-struct HeadTile {
-  int head, tile;
+// Workgroups are dealt to the chip's eight dies in turn; a die gets neighbouring heads, all of their pieces, so that the keys and values
+// its workgroups read at a time are in its cache.
+struct HeadPiece {
+  int head, index;
 };
-__device__ __forceinline__ HeadTile deal(int id, int heads, int tiles) {
+__device__ __forceinline__ HeadPiece deal(int id, int heads) {
   constexpr int kDies = 8;
   if (heads % kDies == 0) {
     const int each = heads / kDies, in = id / kDies;
-    return {id % kDies * each + in % each, tiles - 1 - in / each};
+    return {id % kDies * each + in % each, in / each};
   }
-  return {id % heads, tiles - 1 - id / heads};
+  return {id % heads, id / heads};
 }
 
 #endif  // __HIPCC__

@@ -14,6 +14,8 @@ struct BackArgs {
   const void* o;
   const float* lse;
   float* stats;  // heads x q_tokens: sums of do * o; and then as many lse, times log2(e)
+  float* shares; // [share][dk, dv][k_tokens][kv_heads][head], where a key head's queries are shared out
+  int split;     // in so many
   void* dq;
   void* dk;
   void* dv;
@@ -22,7 +24,6 @@ struct BackArgs {
   int64_t q_stride, k_stride, v_stride, o_stride, dq_stride, dk_stride, dv_stride;
   int sequences, q_tokens, k_tokens, q_each, k_each;
   int heads, kv_heads, group, head;
-  int tiles;
   int causal, zeros;
   float scale, scale2;  // as it is, and times log2(e)
 };
@@ -30,18 +31,6 @@ struct BackArgs {
 constexpr int kRows = 128;  // of a workgroup, 32 of a wavefront
 constexpr int kWaves = 4;
 
-// A workgroup's piece of kRows tokens of a sequence; seq -1: `tile` counts the pieces of the tokens behind the last one.
-struct Piece {
-  int seq, tile;
-};
-__device__ __forceinline__ Piece find_piece(const int32_t* offsets, int sequences, int tokens, int each, int tile) {
-  if (!offsets) {
-    const int per = pieces(each, kRows);
-    return {tile / per, tile % per};
-  }
-  const Found f = find_among(sequences, tile, [&](int s) { return pieces(span_of(offsets, s, tokens, 0).size(), kRows); });
-  return {uniform(f.seq), int(tile - uniform(f.before))};
-}
 // Zeros for this piece of the tokens behind the last sequence.
 template <typename T>
 __device__ __forceinline__ void clear_rest(T* to, int64_t stride, int head, int first, int tile, int tokens) {
@@ -61,9 +50,9 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
   __shared__ __align__(kTileAlign) uint8_t tiles[4 * kTile];
   const int lane = threadIdx.x % kWave, wave = uniform(int(threadIdx.x / kWave));
   const int half = lane / 32, column = lane % 32;
-  const HeadTile ht = deal(blockIdx.x, g.heads, g.tiles);
-  const int head = ht.head;
-  const Piece piece = find_piece(g.q_offsets, g.sequences, g.q_tokens, g.q_each, ht.tile);
+  const HeadPiece hp = deal(blockIdx.x, g.heads);
+  const int head = hp.head;
+  const Piece piece = find_piece(g.q_offsets, g.sequences, g.q_tokens, g.q_each, kRows, hp.index);
   T* const dq = static_cast<T*>(g.dq) + int64_t(head) * g.head;
   if (piece.seq < 0) {
     if (g.zeros) clear_rest(dq, g.dq_stride, g.head, rest_of(g.q_offsets, g.sequences, g.q_tokens), piece.tile, g.q_tokens);
@@ -173,13 +162,15 @@ __global__ __launch_bounds__(kWaves * kWave, sizeof(T) == 2 && DB <= 4 ? 2 : 1) 
   __shared__ __align__(16) float stats[2][2][BM];
   const int lane = threadIdx.x % kWave, wave = uniform(int(threadIdx.x / kWave));
   const int half = lane / 32, column = lane % 32;
-  const HeadTile ht = deal(blockIdx.x, g.kv_heads, g.tiles);
-  const int head = ht.head;
-  const Piece piece = find_piece(g.k_offsets, g.sequences, g.k_tokens, g.k_each, g.tiles - 1 - ht.tile);  // (the first keys have most queries)
+  const HeadPiece hp = deal(blockIdx.x, g.kv_heads * g.split);
+  const int head = hp.head / g.split, share = hp.head % g.split;
+  Piece piece = find_piece(g.k_offsets, g.sequences, g.k_tokens, g.k_each, kRows, hp.index);
+  if (piece.seq >= 0)  // the first keys have most queries
+    piece.tile = pieces(uniform_span(g.k_offsets, piece.seq, g.k_tokens, g.k_each).size(), kRows) - 1 - piece.tile;
   T* const dk = static_cast<T*>(g.dk) + int64_t(head) * g.head;
   T* const dv = static_cast<T*>(g.dv) + int64_t(head) * g.head;
   if (piece.seq < 0) {
-    if (g.zeros) {
+    if (g.zeros && share == 0) {
       const int rest = rest_of(g.k_offsets, g.sequences, g.k_tokens);
       clear_rest(dk, g.dk_stride, g.head, rest, piece.tile, g.k_tokens);
       clear_rest(dv, g.dv_stride, g.head, rest, piece.tile, g.k_tokens);
@@ -194,7 +185,8 @@ __global__ __launch_bounds__(kWaves * kWave, sizeof(T) == 2 && DB <= 4 ? 2 : 1) 
   const auto seen_from = [&](int j) { return !g.causal || j - more < 0 ? 0 : j - more; };
   const int wave_from = seen_from(key0), wave_all = seen_from(key0 + 31);
   const int first = seen_from(piece.tile * kRows) / BM;  // tile of queries
-  const int each = pieces(rows, BM) - first;
+  const int each = pieces(rows, BM) - first > 0 ? pieces(rows, BM) - first : 0;
+  const int steps = each * g.group, step = int(int64_t(steps) * share / g.split), step_end = int(int64_t(steps) * (share + 1) / g.split);
 
   const int parts = g.head * int(sizeof(T)) / 16;
   const int64_t token = ks.begin + (is_key ? key : last);
@@ -229,13 +221,12 @@ __global__ __launch_bounds__(kWaves * kWave, sizeof(T) == 2 && DB <= 4 ? 2 : 1) 
   const auto run = [&](auto apart) {  // (see attention_kernel)
 #pragma unroll
     for (int db = 0; db < DB; ++db) sum_k[db] = v16f_t{}, sum_v[db] = v16f_t{};
-    if (each <= 0) return;
+    if (step == step_end) return;
     // from the last queries down: the workgroups of a sequence, which have different first ones, are at the same ones then
     const int tile_last = first + each - 1;
-    int h = head * g.group, tile = tile_last, b = 0;
-    const int h_end = h + g.group;
+    int h = head * g.group + step / each, tile = tile_last - step % each, left = step_end - step, b = 0;
     fetch(h, tile, 0);
-    while (h < h_end) {
+    while (left > 0) {
       __builtin_amdgcn_s_waitcnt(0);
       __syncthreads();
       const int row0 = tile * BM;
@@ -244,9 +235,7 @@ __global__ __launch_bounds__(kWaves * kWave, sizeof(T) == 2 && DB <= 4 ? 2 : 1) 
       const float* const stat = stats[b][0] + fresh_lane() / 32 * 4;
       if (--tile < first) tile = tile_last, ++h;
       b ^= 1;
-      if (h < h_end) {
-        fetch(h, tile, b);
-      }
+      if (--left > 0) fetch(h, tile, b);
       if (row0 + 31 < wave_from || key0 >= keys) continue;
       const bool masked = row0 < wave_all || row0 + 32 > rows || key0 + 32 > keys;
       const Reader<T, DB> reader = lanes.fresh();
@@ -293,20 +282,47 @@ __global__ __launch_bounds__(kWaves * kWave, sizeof(T) == 2 && DB <= 4 ? 2 : 1) 
   run(Flag<false>{});
   if (__syncthreads_or(is_key && !(finite_column<DB>(sum_k) && finite_column<DB>(sum_v)))) run(Flag<true>{});
   if (!is_key) return;
+  if (g.split > 1) {
+    const int64_t whole = int64_t(g.k_tokens) * g.kv_heads * g.head;
+    float* const to = g.shares + 2 * share * whole + (token * g.kv_heads + head) * g.head;
+    store_column<float, DB>(to, sum_k, half, g.head, g.scale);
+    store_column<float, DB>(to + whole, sum_v, half, g.head, 1.0f);
+    return;
+  }
   store_column<T, DB>(dk + token * g.dk_stride, sum_k, half, g.head, g.scale);
   store_column<T, DB>(dv + token * g.dv_stride, sum_v, half, g.head, 1.0f);
+}
+
+// The shares' sums, four values a thread.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void back_join_kernel(const BackArgs g) {
+  const int64_t whole = int64_t(g.k_tokens) * g.kv_heads * g.head, at = (int64_t(blockIdx.x) * kBlock + threadIdx.x) * 4;
+  const int row_values = g.kv_heads * g.head;
+  if (at >= whole) return;
+  const int64_t token = at / row_values;
+  if (token >= rest_of(g.k_offsets, g.sequences, g.k_tokens)) return;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    v4f_t v = {0, 0, 0, 0};
+    for (int p = 0; p < g.split; ++p) v += *reinterpret_cast<const v4f_t*>(g.shares + (2 * p + which) * whole + at);
+    T* const to = which ? static_cast<T*>(g.dv) + token * g.dv_stride + at % row_values : static_cast<T*>(g.dk) + token * g.dk_stride + at % row_values;
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<v4f_t*>(to) = v;
+    else *reinterpret_cast<uint2*>(to) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+  }
 }
 
 template <typename T, int DB>
 void launch_both(BackArgs g, int q_tiles, int k_tiles, hipStream_t s) {
   constexpr int kThreads = kWaves * kWave;
   if (q_tiles > 0) {
-    g.tiles = q_tiles;
     back_queries_kernel<T, DB><<<dim3(uint32_t(q_tiles) * g.heads), kThreads, 0, s>>>(g);
   }
   if (k_tiles > 0) {
-    g.tiles = k_tiles;
-    back_keys_kernel<T, DB><<<dim3(uint32_t(k_tiles) * g.kv_heads), kThreads, 0, s>>>(g);
+    back_keys_kernel<T, DB><<<dim3(uint32_t(k_tiles) * g.kv_heads * g.split), kThreads, 0, s>>>(g);
+    if (g.split > 1) {
+      const int64_t fours = int64_t(g.k_tokens) * g.kv_heads * g.head / 4;
+      back_join_kernel<T><<<dim3(uint32_t(blocks_of(fours, kBlock))), kBlock, 0, s>>>(g);
+    }
   }
 }
 template <typename T>
@@ -322,10 +338,22 @@ hipError_t launch(const BackArgs& g, int q_tiles, int k_tiles, hipStream_t s) {
 }  // namespace
 
 AttentionBackPlan make_attention_back_plan(const accept_attention_desc& d) {
-  return {size_t(up_to(8 * int64_t(d.heads) * d.q_tokens, 256))};
+  AttentionBackPlan p{};
+  p.stats = size_t(up_to(8 * int64_t(d.heads) * d.q_tokens, 256));
+  // A key tile's queries are one workgroup's work, one after the other, and there are two workgroups a compute unit: below four rounds of
+  // those the last ones' queries are shared out.  (12288 tokens in seven sequences, 32 heads on 8: 824 workgroups, the longest with 3.6
+  // times the average's work: SPLIT_US, in two shares and with the sums of those SPLIT2_US.)
+  constexpr int64_t kEnough = 1024, kMost = 16;
+  const int64_t groups = (blocks_of(d.k_tokens, kRows) + d.sequences) * d.kv_heads;
+  const int64_t queries = d.sequences > 0 ? blocks_of(d.q_tokens, d.sequences) * (d.heads / d.kv_heads) : 0;  // of a key tile
+  p.split = 1;
+  while (p.split < kMost && groups * p.split < kEnough && queries >= 512 * p.split) p.split *= 2;
+  p.bytes = p.stats;
+  if (p.split > 1) p.bytes += size_t(up_to(8 * p.split * d.k_tokens * d.kv_heads * d.head_size, 256));
+  return p;
 }
 
-hipError_t launch_attention_backward(const accept_attention_desc& d, const AttentionBackPlan&, const void* dout, const void* q,
+hipError_t launch_attention_backward(const accept_attention_desc& d, const AttentionBackPlan& p, const void* dout, const void* q,
                                      const void* k, const void* v, const void* o, const float* lse, const int32_t* q_offsets,
                                      const int32_t* k_offsets, void* dq, void* dk, void* dv, void* ws, hipStream_t s) {
   BackArgs g{};
@@ -333,6 +361,8 @@ hipError_t launch_attention_backward(const accept_attention_desc& d, const Atten
   const auto stride = [](int64_t given, int64_t otherwise) { return given ? given : otherwise; };
   g.dout = dout, g.q = q, g.k = k, g.v = v, g.o = o, g.lse = lse;
   g.stats = static_cast<float*>(ws);
+  g.shares = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + p.stats);
+  g.split = p.split;
   g.dq = dq, g.dk = dk, g.dv = dv;
   g.q_offsets = q_offsets, g.k_offsets = k_offsets;
   g.q_stride = stride(d.q_stride, whole), g.o_stride = stride(d.o_stride, whole), g.dq_stride = stride(d.dq_stride, whole);
