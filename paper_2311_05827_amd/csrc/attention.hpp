@@ -463,39 +463,27 @@ struct TileRows {
   static constexpr bool kAlike = kStep % 16 == 0;     // whose parts then lie in the same order
   uint32_t stride;  // bytes
   int wave, parts;
+  // (where there are fewer loads than wavefronts some load the same, so that all wait for the same number)
   __device__ __forceinline__ TileRows(int wave_, int64_t stride_elements, int parts_)
-      : stride(uint32_t(stride_elements) * uint32_t(sizeof(T))), wave(wave_), parts(parts_) {}
+      : stride(uint32_t(stride_elements) * uint32_t(sizeof(T))), wave(kAll < WAVES ? wave_ % kAll : wave_), parts(parts_) {}
+  __device__ __forceinline__ int row(int i, int lane) const { return (i * WAVES + wave) * kRowsPer + lane / kRowParts; }
+  __device__ __forceinline__ int part(int i, int lane) const { return lane % kRowParts ^ turn<kRowBytes>(row(kAlike ? 0 : i, lane)); }
   // rows first .. first + ROWS - 1 behind `base`, of which there are `left`, at least one
   __device__ __forceinline__ void fetch(const void* base, int left, const uint8_t* tile) const {
-    // (where there are fewer loads than wavefronts some load the same, so that all wait for the same number)
-    const int wave = kAll < WAVES ? this->wave % kAll : this->wave;
     const uint32_t to = lds_offset(tile) + uint32_t(wave) * 1024u;
     const int lane = fresh_lane();
-    const auto row = [&](int i) { return (i * WAVES + wave) * kRowsPer + lane / kRowParts; };
-    const auto part = [&](int i) { return lane % kRowParts ^ turn<kRowBytes>(row(kAlike ? 0 : i)); };
-    const auto from = [&](int i) { return uint32_t(row(i)) * stride + uint32_t(part(i)) * 16u; };
-    const auto each = [&](const auto& load) {
+    if (kAlike && left >= ROWS && parts == kRowParts) {
+      const uint32_t from = uint32_t(row(0, lane)) * stride + uint32_t(part(0, lane)) * 16u;
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) load(i, to + uint32_t(i * WAVES) * 1024u);
-    };
-    const auto whole = [&](int i, uint32_t to_i) {
-      load_tile_part(static_cast<const uint8_t*>(base) + (kAlike ? uint32_t(i * kStep) * uint64_t(stride) : 0), from(kAlike ? 0 : i), to_i);
-    };
-    const auto short_of = [&](int i, uint32_t to_i) {
-      load_tile_part(base, uint32_t(row(i) < left ? row(i) : left - 1) * stride + uint32_t(part(i)) * 16u, to_i);
-    };
-    if constexpr (kAlike) {
-      if (part(0) < parts) {
-        if (left >= ROWS) each(whole);
-        else each(short_of);
-      }
-    } else {
-      each([&](int i, uint32_t to_i) {
-        if (part(i) < parts) {
-          if (left >= ROWS) whole(i, to_i);
-          else short_of(i, to_i);
-        }
-      });
+      for (int i = 0; i < kLoads; ++i)
+        load_tile_part(static_cast<const uint8_t*>(base) + uint32_t(i * kStep) * uint64_t(stride), from, to + uint32_t(i * WAVES) * 1024u);
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = row(i, lane);
+      if (part(i, lane) < parts)
+        load_tile_part(base, uint32_t(r < left ? r : left - 1) * stride + uint32_t(part(i, lane)) * 16u, to + uint32_t(i * WAVES) * 1024u);
     }
   }
 };
