@@ -31,7 +31,8 @@ hipError_t launch_attention_backward(const accept_attention_desc& d, const Atten
                                      const int32_t* k_offsets, void* dq, void* dk, void* dv, void* ws, hipStream_t s);
 
 struct CachePlan {
-  int64_t items;  // at most so many pieces of 32 rows
+  bool rows;      // many rows a sequence: items of 128 (see cached_rows_kernel), else of 32
+  int64_t items;  // at most so many
   int parts;      // of the work of a key head
   size_t bytes;   // workspace
 };
@@ -119,6 +120,51 @@ __device__ __forceinline__ Found find_among(int sequences, int64_t at, const F& 
   }
   return {-1, before};
 }
+// find_among for several questions: up to 64 sequences are counted once.
+template <typename F>
+struct Index {
+  int sequences;
+  const F& size;
+  int64_t incl, total;
+  __device__ __forceinline__ Index(int sequences_, const F& size_) : sequences(sequences_), size(size_) {
+    if (sequences <= kWave) {
+      const int lane = threadIdx.x % kWave;
+      incl = lane < sequences ? int64_t(size(lane)) : 0;
+      if (sequences > 1) {
+#pragma unroll
+        for (int d = 1; d < kWave; d *= 2) {
+          const int64_t up = __shfl_up(incl, d, kWave);
+          if (lane >= d) incl += up;
+        }
+        total = uniform(__shfl(incl, kWave - 1, kWave));
+      } else {
+        total = uniform(incl);  // lane 0's
+      }
+    } else {
+      total = uniform(find_among(sequences, INT64_MAX, size).before);
+    }
+  }
+  // what lies in front of a sequence
+  __device__ __forceinline__ int64_t before(int seq) const {
+    if (sequences > kWave) return uniform(find_among(seq, INT64_MAX, size).before);
+    return seq == 0 ? 0 : uniform(__shfl(incl, seq - 1, kWave));
+  }
+  __device__ __forceinline__ Found find(int64_t at) const {
+    if (sequences > kWave) {
+      const Found f = find_among(sequences, at, size);
+      return {uniform(f.seq), uniform(f.before)};
+    }
+    if (at >= total) return {-1, total};
+    const int seq = sequences > 1 ? __builtin_ctzll(__ballot(incl > at)) : 0;
+    return {seq, before(seq)};
+  }
+};
+// a / b for a >= 0, b > 0, the same for all lanes; most often short ones
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  if (((a | b) >> 32) == 0) return int64_t(uniform(int(uint32_t(a) / uint32_t(b))));
+  return uniform(a / b);
+}
+
 // The same with the longest sequences first (of every 64), so that a launch ends with short pieces of work: 12288 tokens in seven sequences,
 // 32 heads, gradients of the keys in 793 us in their own order, DKDV_US so.
 template <typename F, typename L>
@@ -442,9 +488,12 @@ __device__ __forceinline__ uint32_t lds_offset(const void* p) {
 }
 // 16 bytes a lane from base + offset to shared memory, `to` on, lane by lane; lanes that are off load and write nothing.  Nothing waits for it but an
 // explicit wait for all loads (the compiler would wait before every read of shared memory).
+// ONCE: what no other workgroup reads; it does not stay in the caches.
+template <bool ONCE = false>
 __device__ __forceinline__ void load_tile_part(const void* base, uint32_t offset, uint32_t to) {
   base = uniform(base);  // (the same for all lanes, whatever register it is in)
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(uniform(int(to))), "v"(offset), "s"(base) : "memory");
+  if constexpr (ONCE) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" : : "s"(uniform(int(to))), "v"(offset), "s"(base) : "memory");
+  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(uniform(int(to))), "v"(offset), "s"(base) : "memory");
 }
 // The same with 4 bytes a lane.
 __device__ __forceinline__ void load_tile_word(const void* base, uint32_t offset, uint32_t to) {

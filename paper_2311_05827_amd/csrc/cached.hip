@@ -24,19 +24,26 @@ struct CacheArgs {
   float scale;     // times log2(e)
 };
 
-// An item is 32 rows of a key head: its query heads for one token after the other.  Rows are columns of the products, as in attention_kernel.
-constexpr int kItem = 32;
-
-// What a wavefront goes through at a time is 32 keys; it keeps the next 32 coming, in shared memory of its own, and waits for nobody.  A
-// unit of work is 32 keys for each wavefront of a workgroup.
+// Rows are columns of the products, as in attention_kernel: a key head's query heads for one token after the other.  An item is so many rows of a
+// sequence as a workgroup has at a time, a unit of work so many keys for an item.
+//
+// Few rows (cached_keys_kernel): an item is 32 rows.  What a wavefront goes through at a time is 32 keys; it keeps the next 32 coming, in shared
+// memory of its own, and waits for nobody; in the end the wavefronts' results are put together.
 template <typename T, int DB>
-struct Shape {
+struct KeysShape {
   static constexpr int kTile = 32 * Head<T, DB>::kRowBytes;
   static constexpr int kWaves = 4 * kTile * 4 <= 131072 ? 4 : 131072 / (4 * kTile);
-  static constexpr int kUnit = 32 * kWaves;
-  static constexpr int kThreads = kWaves * kWave;
+  static constexpr int kItem = 32, kUnit = 32 * kWaves, kThreads = kWaves * kWave;
   static constexpr int kSum = DB * 32 * (kItem + 1);  // floats of a wavefront's results, transposed without meeting banks
   static_assert(kSum * 4 <= 4 * kTile, "results take the tiles' place");
+};
+// Many rows (cached_rows_kernel): an item is 32 rows of each wavefront, 256 where registers allow eight wavefronts, and all of them take the same
+// keys, which come into shared memory once, several tiles ahead.
+template <typename T, int DB>
+struct RowsShape {
+  static constexpr int kTile = 32 * Head<T, DB>::kRowBytes;
+  static constexpr int kWaves = DB * int(sizeof(T)) <= 8 ? 8 : 4, kItem = 32 * kWaves, kUnit = 128, kThreads = kWaves * kWave;
+  static constexpr int kRing = 65536 / kTile < 8 ? 65536 / kTile : 8;  // tiles of keys and of values that are there or on their way
 };
 // A sequence of the step.
 struct Step {
@@ -45,7 +52,8 @@ struct Step {
   int keys;    // places that its tokens may see
   int64_t items, units;  // units of every item
 };
-__device__ __forceinline__ Step step_of(const CacheArgs& g, int seq, int unit) {
+template <typename S>
+__device__ __forceinline__ Step step_of(const CacheArgs& g, int seq) {
   Step s;
   s.span = span_of(g.offsets, seq, g.tokens, g.each);
   const int64_t capacity = g.pages.count > 0 ? int64_t(g.pages.table_pages) << g.pages.shift : 0;
@@ -53,203 +61,283 @@ __device__ __forceinline__ Step step_of(const CacheArgs& g, int seq, int unit) {
   s.length = given < 0 ? 0 : given;
   const int64_t all = int64_t(s.length) + n;
   s.keys = int(all < capacity ? all : capacity);
-  s.items = (int64_t(n) * g.group + kItem - 1) / kItem;
-  const int64_t units = (int64_t(s.keys) + unit - 1) / unit;
+  s.items = (int64_t(n) * g.group + S::kItem - 1) / S::kItem;
+  const int64_t units = (int64_t(s.keys) + S::kUnit - 1) / S::kUnit;
   s.units = units > 0 ? units : 1;
   return s;
 }
-__device__ __forceinline__ Step uniform_step(const CacheArgs& g, int seq, int unit) {
-  const Step s = step_of(g, seq, unit);
+template <typename S>
+__device__ __forceinline__ Step uniform_step(const CacheArgs& g, int seq) {
+  const Step s = step_of<S>(g, seq);
   return {{uniform(s.span.begin), uniform(s.span.end)}, uniform(s.length), uniform(s.keys), uniform(s.items), uniform(s.units)};
 }
 // Work of a key head, in units one behind the other, is dealt in equal parts.  A part has at most two pieces of items that are not whole: the end of one that
 // began before it, and the beginning of one that goes on behind it.
-__device__ __forceinline__ int64_t part_begin(int64_t all, int parts, int p) { return all * p / parts; }
+__device__ __forceinline__ int64_t part_begin(int64_t all, int parts, int p) { return quotient(all * p, parts); }
 __device__ __forceinline__ int used_parts(int64_t all, int parts) { return all < parts ? int(all) : parts; }
-// Floats of a piece's results: 32 rows of sums, their maxima, their sums of weights.
+// Floats of a piece's results: rows of sums, their maxima, their sums of weights.
+template <typename S>
 __device__ __forceinline__ float* slot_at(const CacheArgs& g, int kv, int part, bool begins, int width) {
+  constexpr int kItem = S::kItem;
   return g.parts_at + (int64_t(kv) * g.parts + part) * 2 * kItem * (width + 2) + (begins ? kItem * (width + 2) : 0);
 }
 
-template <typename T, int DB>
-__global__ __launch_bounds__((Shape<T, DB>::kThreads), 1) void cached_kernel(const CacheArgs g) {
-  using S = Shape<T, DB>;
+// Where a part of the work is: the pieces of items that it has, one after the other.
+struct Walk {
+  int64_t at, end, before;  // units; `before` the sequence's first
+  int seq;
+};
+template <typename S>
+__device__ __forceinline__ Walk begin_walk(const CacheArgs& g, int part) {
+  const auto work = [&](int s) {
+    const Step st = step_of<S>(g, s);
+    return st.items * st.units;
+  };
+  const Index<decltype(work)> index(g.sequences, work);
+  const int parts = used_parts(index.total, g.parts);
+  if (part >= parts) return {0, 0, 0, 0};
+  const int64_t at = part_begin(index.total, parts, part);
+  const Found found = index.find(at);
+  return {at, part_begin(index.total, parts, part + 1), found.before, found.seq};
+}
+struct Stretch {
+  Step st;
+  int64_t item;
+  int unit0, unit1;
+};
+template <typename S>
+__device__ __forceinline__ bool next_stretch(const CacheArgs& g, Walk& w, Stretch& s) {
+  while (w.at < w.end && w.seq < g.sequences) {
+    s.st = uniform_step<S>(g, w.seq);
+    const int64_t in = w.at - w.before, all = s.st.items * s.st.units;
+    if (in >= all) {
+      w.before += all;
+      ++w.seq;
+      continue;
+    }
+    s.item = quotient(in, s.st.units);
+    s.unit0 = int(in - s.item * s.st.units);
+    s.unit1 = int(s.st.units - s.unit0 < w.end - w.at ? s.st.units : s.unit0 + (w.end - w.at));
+    w.at += s.unit1 - s.unit0;
+    return true;
+  }
+  return false;
+}
+
+// What rows row0 .. row0 + count - 1 of a sequence see: a row its token's places, of which all see the first ones and none those from `some` on.
+struct Sight {
+  int all, some;
+};
+__device__ __forceinline__ Sight sight_of(const CacheArgs& g, const Step& st, int row0, int count) {
+  const int64_t first = int64_t(st.length) + (g.tree_words ? 0 : row0 / g.group + 1);
+  const int64_t last = int64_t(st.length) + (row0 + count - 1) / g.group + 1;
+  return {uniform(int(first < st.keys ? first : st.keys)), uniform(g.tree_words || last > st.keys ? st.keys : int(last))};
+}
+// Which of the 32 places from key0 on a token sees: its number in its sequence's new ones, and in all.
+__device__ __forceinline__ uint32_t seen_among(const CacheArgs& g, const Step& st, int of_step, int token, int key0) {
+  const int64_t sees = int64_t(st.length) + of_step + 1;
+  const int limit = g.tree_words ? st.keys : int(sees < st.keys ? sees : st.keys);
+  uint32_t seen = bits_between(0, limit - key0);
+  if (g.tree_words && key0 + 32 > st.length) {
+    const int first = key0 - st.length;  // the node that bit 0 is; below 0: cached
+    const uint64_t* const words = g.tree + int64_t(token) * g.tree_words;
+    const auto word = [&](int i) { return i < g.tree_words ? words[i] : 0; };
+    uint32_t nodes;
+    if (first < 0) {
+      nodes = uint32_t(word(0)) << -first | ((1u << -first) - 1u);
+    } else {
+      const int by = first % 64;
+      uint64_t w = word(first / 64) >> by;
+      if (by > 32) w |= word(first / 64 + 1) << (64 - by);
+      nodes = uint32_t(w);
+    }
+    seen &= nodes;
+  }
+  return seen;
+}
+
+// The pages of a sequence, 128 of them at a time in two registers of the wavefront: a tile's page is then there at once, and not a trip to memory
+// away.
+struct Window {
+  const int32_t* table;  // of the sequence
+  int first, last;       // in the registers; of all
+  int low, high;
+  __device__ __forceinline__ Window(const CacheArgs& g, const Step& st, int seq)
+      : table(g.table + int64_t(seq) * g.pages.table_pages), first(-kReach), last((st.keys - 1) >> g.pages.shift) {}
+  static constexpr int kReach = 2 * kWave;
+  __device__ __forceinline__ void load(int from) {
+    first = from;
+    const int lane = fresh_lane(), a = first + lane, b = a + kWave;
+    low = table[a < last ? a : last];
+    high = table[b < last ? b : last];
+    asm volatile("" : "+v"(low), "+v"(high));  // they are waited for here, and not, with all tiles on their way, wherever they are used
+  }
+  __device__ __forceinline__ int at(int i) const {
+    const int in = uniform(i - first);
+    return in < kWave ? __builtin_amdgcn_readlane(low, in) : __builtin_amdgcn_readlane(high, in - kWave);
+  }
+};
+// The pages of the 32 places from key0 (a multiple of 32) on, of which the first exists: two at most, a page has 16 places or more.
+struct TwoPages {
+  int page[2];
+};
+__device__ __forceinline__ TwoPages pages_of(const CacheArgs& g, const Step& st, Window& window, int key0) {
+  const int i = key0 >> g.pages.shift, j = (key0 + 16 < st.keys ? key0 + 16 : st.keys - 1) >> g.pages.shift;
+  if (j >= window.first + Window::kReach || i < window.first) window.load(i);
+  return {window.at(i), window.at(j)};
+}
+// Those keys and values into tiles, by WAVES wavefronts; places behind the last one give that one again.  Returns which of the places exist.
+template <typename T, int DB, int WAVES, bool ONCE>
+__device__ __forceinline__ uint32_t fetch_places(const CacheArgs& g, const Step& st, const TwoPages& two, int kv, int key0, int wave, uint32_t k_to,
+                                                 uint32_t v_to) {
   using H = Head<T, DB>;
-  constexpr int kWidth = DB * 32, kPad = kItem + 1;
+  constexpr int kPer = 1024 / H::kRowBytes, kAll = 32 / kPer, kLoads = (kAll + WAVES - 1) / WAVES;
+  const int row_bytes = g.head * int(sizeof(T)), parts = row_bytes / 16;
+  const auto place = [&](int half) { return key0 + 16 * half < st.keys ? key0 + 16 * half : st.keys - 1; };
+  uint32_t there = 0;
+  int64_t first[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int page = uniform(two.page[h]);
+    const bool is = is_page(g.pages, page);
+    there |= is ? 0xFFFFu << (16 * h) : 0u;
+    first[h] = cache_row(g.pages, is ? page : 0, place(h), kv) * row_bytes;
+  }
+  const int lane = fresh_lane();
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int load = WAVES == 1 ? i : (i * WAVES + wave) % kAll, row = load * kPer, h = row >= 16;
+    const int r = row + lane / H::kRowParts, p = lane % H::kRowParts ^ turn<H::kRowBytes>(r);
+    const int j = key0 + r < st.keys ? key0 + r : st.keys - 1;
+    const uint32_t offset = uint32_t(j - place(h)) * uint32_t(row_bytes) + uint32_t(p) * 16u;
+    if (p < parts) {
+      load_tile_part<ONCE>(static_cast<const uint8_t*>(g.k) + first[h], offset, k_to + load * 1024);
+      load_tile_part<ONCE>(static_cast<const uint8_t*>(g.v) + first[h], offset, v_to + load * 1024);
+    }
+  }
+  return there;
+}
+
+// The running softmax of 32 rows (a lane's column each) over one tile of 32 keys after the other.
+template <typename T, int DB>
+struct Rows {
+  RowParts<T, DB> q;
+  v16f_t acc[DB];
+  float largest, sum;
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int db = 0; db < DB; ++db) acc[db] = v16f_t{};
+    largest = -INFINITY;
+    sum = 0.0f;
+  }
+  // seen: for columns that do not see all of the tile (then `masked`)
+  template <typename Apart, typename Seen>
+  __device__ __forceinline__ void take(const uint8_t* kt, const uint8_t* vt, const Reader<T, DB>& reader, float scale, bool masked, const Seen& seen_of, Apart) {
+    v16f_t s = rows_product<T, DB>(lds_offset(kt), reader, 0, q);
+    uint32_t seen = ~0u;
+    if (masked) {
+      seen = seen_of();
+      const uint32_t here = seen >> (fresh_lane() / 32 * 4);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = here >> result_row(r, 0) & 1 ? s[r] : -INFINITY;
+    }
+    float most = s[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) most = fmaxf(most, s[r]);
+    most = halves_max(most) * scale;
+    if (__any(most > largest + 8.0f)) {  // (see kBehind of attention_kernel)
+      const float now = fmaxf(largest, most);
+      const float factor = largest == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(largest - now);
+      largest = now;
+      sum *= factor;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) acc[db] *= factor;
+    }
+    const float base = largest == -INFINITY ? 0.0f : -largest;
+    float p[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale, base));
+      sum += p[r];
+    }
+    if (Apart::value && masked) {
+      weighted_rows_apart<T, DB>(acc, vt, 0, fresh_lane(), p, seen);
+    } else {
+      Weights<T> w;
+      set_weights(w, p);
+      weighted_rows<T, DB>(acc, lds_offset(vt), reader, 0, w);
+    }
+  }
+};
+
+template <typename T, int DB>
+__global__ __launch_bounds__((KeysShape<T, DB>::kThreads), 1) void cached_keys_kernel(const CacheArgs g) {
+  using S = KeysShape<T, DB>;
+  constexpr int kItem = S::kItem, kWidth = DB * 32, kPad = kItem + 1;
   __shared__ __align__(kTileAlign) uint8_t tiles[S::kWaves][4 * S::kTile];
   __shared__ float peak[S::kWaves][kItem], total[S::kWaves][kItem];
   const int lane = threadIdx.x % kWave, wave = uniform(int(threadIdx.x / kWave));
   const int half = lane / 32, column = lane % 32;
   const int kv = blockIdx.y, part = blockIdx.x;
-  const int parts_of_row = g.head * int(sizeof(T)) / 16;
   uint8_t* const mine = tiles[wave];
-
-  const auto work = [&](int s) {
-    const Step st = step_of(g, s, S::kUnit);
-    return st.items * st.units;
-  };
-  const int64_t all = uniform(find_among(g.sequences, INT64_MAX, work).before);
-  const int parts = used_parts(all, g.parts);
-  if (part >= parts) return;
-  int64_t at = part_begin(all, parts, part);
-  const int64_t end = part_begin(all, parts, part + 1);
-  const Found found = find_among(g.sequences, at, work);
-  int seq = uniform(found.seq);
-  int64_t before = uniform(found.before);
-  if (g.head < kWidth) {
+  const auto clear_mine = [&] {
     for (int i = lane * 16; i < 4 * S::kTile; i += kWave * 16) *reinterpret_cast<uint4*>(mine + i) = make_uint4(0, 0, 0, 0);
-  }
-
-  while (at < end && seq < g.sequences) {
-    const Step st = uniform_step(g, seq, S::kUnit);
-    const int64_t in = at - before;
-    if (in >= st.items * st.units) {
-      before += st.items * st.units;
-      ++seq;
-      continue;
-    }
-    const int64_t item = in / st.units;
-    const int unit0 = int(in - item * st.units);
-    const int unit1 = int(st.units - unit0 < end - at ? st.units : unit0 + (end - at));
-    at += unit1 - unit0;
-
-    const int64_t rows = int64_t(st.span.size()) * g.group, row0 = item * kItem;
-    const int count = int(rows - row0 < kItem ? rows - row0 : kItem);
-    const int64_t row = row0 + (column < count ? column : count - 1);
-    const int of_step = int(row / g.group), token = st.span.begin + of_step, head = kv * g.group + int(row % g.group);
-    const int64_t sees = int64_t(st.length) + of_step + 1;
-    const int limit = g.tree_words ? st.keys : int(sees < st.keys ? sees : st.keys);
-    const int64_t first_sees = int64_t(st.length) + (g.tree_words ? 0 : row0 / g.group + 1);
-    const int all_see = int(first_sees < st.keys ? first_sees : st.keys);       // every row sees keys before it
-    const int64_t last_sees = int64_t(st.length) + (row0 + count - 1) / g.group + 1;
-    const int some_see = g.tree_words || last_sees > st.keys ? st.keys : int(last_sees);
-    RowParts<T, DB> q;
-    q.load(static_cast<const T*>(g.q) + token * g.q_stride + int64_t(head) * g.head, half, parts_of_row);
-
-    // 32 keys from key0 on, into buffer b; which of them exist
-    typedef const __attribute__((address_space(4))) int32_t constant_int;
-    const auto page_of = [&](int j) {
-      return uniform(int(((constant_int*)(g.table))[int64_t(seq) * g.pages.table_pages + (j >> g.pages.shift)]));
-    };
-    const auto fetch = [&](int key0, int b) {
-      constexpr int kPer = 1024 / H::kRowBytes, kLoads = 32 / kPer;
-      const bool one_page = g.pages.shift >= 5;
-      uint32_t there = 0;
-      int page = 0;
-      const uint32_t to = lds_offset(mine) + uint32_t(b) * 2u * S::kTile;
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const int j = key0 + i * kPer < st.keys ? key0 + i * kPer : st.keys - 1;
-        if (i == 0 || !one_page) page = page_of(j);
-        const bool is = is_page(g.pages, page);
-        there |= is ? (kPer == 32 ? ~0u : ((1u << (kPer % 32)) - 1u)) << (i * kPer) : 0u;
-        const int64_t first = cache_row(g.pages, is ? page : 0, j, kv) * g.head * int(sizeof(T));
-        const int r = lane / H::kRowParts, p = lane % H::kRowParts ^ turn<H::kRowBytes>(i * kPer + r);
-        const int left = st.keys - 1 - j;  // rows behind j
-        const uint32_t offset = uint32_t(r < left ? r : left) * uint32_t(g.head * int(sizeof(T))) + uint32_t(p) * 16u;
-        if (p < parts_of_row) {
-          load_tile_part(static_cast<const uint8_t*>(g.k) + first, offset, to + i * 1024);
-          load_tile_part(static_cast<const uint8_t*>(g.v) + first, offset, to + S::kTile + i * 1024);
-        }
-      }
-      return there;
-    };
-    const auto seen_among = [&](int key0, uint32_t there) {
-      uint32_t seen = bits_between(0, limit - key0) & there;
-      if (g.tree_words && key0 + 32 > st.length) {
-        const int first = key0 - st.length;  // the node that bit 0 is; below 0: cached
-        const uint64_t* const words = g.tree + int64_t(token) * g.tree_words;
-        const auto word = [&](int i) { return i < g.tree_words ? words[i] : 0; };
-        uint32_t nodes;
-        if (first < 0) {
-          nodes = uint32_t(word(0)) << -first | ((1u << -first) - 1u);
-        } else {
-          const int by = first % 64;
-          uint64_t w = word(first / 64) >> by;
-          if (by > 32) w |= word(first / 64 + 1) << (64 - by);
-          nodes = uint32_t(w);
-        }
-        seen &= nodes;
-      }
-      return seen;
-    };
-
-      const Reader<T, DB> lanes(lane);
-    v16f_t acc[DB];
-    float largest, sum;
-    const int stop = some_see < unit1 * S::kUnit ? some_see : unit1 * S::kUnit;
+  };
+  const Reader<T, DB> lanes(lane);
+  Rows<T, DB> rows;
+  Walk walk = begin_walk<S>(g, part);
+  Stretch now;
+  if (g.head < kWidth) clear_mine();
+  while (next_stretch<S>(g, walk, now)) {
+    const Step& st = now.st;
+    // (rows of a sequence: fewer than 2^28, see the check of the descriptor)
+    const int row0 = int(now.item) * kItem, left = st.span.size() * g.group - row0;
+    const int count = left < kItem ? left : kItem;
+    const int row = row0 + (column < count ? column : count - 1);
+    const int of_step = row / g.group, token = st.span.begin + of_step, head = kv * g.group + row % g.group;
+    const Sight sight = sight_of(g, st, row0, count);
+    rows.q.load(static_cast<const T*>(g.q) + token * g.q_stride + int64_t(head) * g.head, half, g.head * int(sizeof(T)) / 16);
+    const int stop = sight.some < now.unit1 * S::kUnit ? sight.some : now.unit1 * S::kUnit;
     const auto run = [&](auto apart) {
-#pragma unroll
-      for (int db = 0; db < DB; ++db) acc[db] = v16f_t{};
-      largest = -INFINITY;
-      sum = 0.0f;
-      int key0 = unit0 * S::kUnit + wave * 32, b = 0;
+      rows.clear();
+      Window window(g, st, walk.seq);
+      const auto fetch = [&](int key0, int b) {
+        const uint32_t to = lds_offset(mine) + uint32_t(b) * 2u * S::kTile;
+        return fetch_places<T, DB, 1, true>(g, st, pages_of(g, st, window, key0), kv, key0, 0, to, to + S::kTile);
+      };
+      int key0 = now.unit0 * S::kUnit + wave * 32, b = 0;
       uint32_t there = 0;
       if (key0 < stop) there = fetch(key0, 0);
       for (; key0 < stop; key0 += S::kUnit, b ^= 1) {
-        __builtin_amdgcn_s_waitcnt(0);
-        asm volatile("" : : : "memory");
+        wait_for_loads<0>();
         const uint32_t now_there = there;
         if (key0 + S::kUnit < stop) there = fetch(key0 + S::kUnit, b ^ 1);
         const uint8_t* const kt = mine + b * 2 * S::kTile;
-        const uint8_t* const vt = kt + S::kTile;
-        const Reader<T, DB> reader = lanes.fresh();
-        v16f_t s = rows_product<T, DB>(lds_offset(kt), reader, 0, q);
-        const bool masked = key0 + 32 > all_see || now_there != ~0u;
-        uint32_t seen = ~0u;
-        if (masked) {
-          seen = seen_among(key0, now_there);
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = seen >> result_row(r, half) & 1 ? s[r] : -INFINITY;
-        }
-        float most = -INFINITY;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) most = fmaxf(most, s[r]);
-        most = halves_max(most) * g.scale;
-        if (__any(most > largest + 8.0f)) {  // (see kBehind of attention_kernel)
-          const float now = fmaxf(largest, most);
-          const float factor = largest == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(largest - now);
-          largest = now;
-          sum *= factor;
-#pragma unroll
-          for (int db = 0; db < DB; ++db) acc[db] *= factor;
-        }
-        const float base = largest == -INFINITY ? 0.0f : -largest;
-        float p[16];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], g.scale, base));
-          sum += p[r];
-        }
-        if (apart.value && masked) {
-          weighted_rows_apart<T, DB>(acc, vt, 0, lane, p, seen);
-        } else {
-          Weights<T> w;
-          set_weights(w, p);
-          weighted_rows<T, DB>(acc, lds_offset(vt), reader, 0, w);
-        }
+        rows.take(kt, kt + S::kTile, lanes.fresh(), g.scale, key0 + 32 > sight.all || now_there != ~0u,
+                  [&] { return seen_among(g, st, of_step, token, key0) & now_there; }, apart);
       }
     };
     run(Flag<false>{});
-    if (__any(column < count && !finite_column<DB>(acc))) run(Flag<true>{});
-    sum = halves_sum(sum);
+    if (__any(column < count && !finite_column<DB>(rows.acc))) run(Flag<true>{});
+    const float sum = halves_sum(rows.sum);
 
     // the wavefronts' results together, relative to the largest of their maxima
-    if (half == 0) peak[wave][column] = largest;
+    if (half == 0) peak[wave][column] = rows.largest;
     __syncthreads();
     float top = -INFINITY;
 #pragma unroll
     for (int w = 0; w < S::kWaves; ++w) top = fmaxf(top, peak[w][column]);
-    const float factor = largest == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(largest - top);
+    const float factor = rows.largest == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(rows.largest - top);
     if (half == 0) total[wave][column] = sum * factor;
     float* const out = reinterpret_cast<float*>(mine);
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) out[(db * 32 + result_row(r, half)) * kPad + column] = largest == -INFINITY ? 0.0f : acc[db][r] * factor;
+      for (int r = 0; r < 16; ++r)
+        out[(db * 32 + result_row(r, half)) * kPad + column] = rows.largest == -INFINITY ? 0.0f : rows.acc[db][r] * factor;
     __syncthreads();
-    const bool begins = unit0 == 0, ends = unit1 == st.units;
-    float* const slot = slot_at(g, kv, part, begins, kWidth);
+    const bool begins = now.unit0 == 0, ends = now.unit1 == st.units;
+    float* const slot = slot_at<S>(g, kv, part, begins, kWidth);
     for (int i = threadIdx.x; i < count * kWidth; i += S::kThreads) {
       const int r = i / kWidth, d = i % kWidth;
       float v = 0.0f, l = 0.0f;
@@ -259,7 +347,7 @@ __global__ __launch_bounds__((Shape<T, DB>::kThreads), 1) void cached_kernel(con
         l += total[w][r];
       }
       if (begins && ends) {
-        const int64_t flat = row0 + r;
+        const int flat = row0 + r;
         if (d < g.head)
           store_one(static_cast<T*>(g.o) + (st.span.begin + flat / g.group) * g.o_stride + (kv * g.group + flat % g.group) * g.head + d,
                     l == 0.0f ? 0.0f : v / l);
@@ -275,8 +363,90 @@ __global__ __launch_bounds__((Shape<T, DB>::kThreads), 1) void cached_kernel(con
       }
     }
     __syncthreads();
-    if (g.head < kWidth && at < end)  // the results went where the tiles have zeros
-      for (int i = lane * 16; i < 4 * S::kTile; i += kWave * 16) *reinterpret_cast<uint4*>(mine + i) = make_uint4(0, 0, 0, 0);
+    if (g.head < kWidth && walk.at < walk.end) clear_mine();  // the results went where the tiles have zeros
+  }
+}
+
+template <typename T, int DB>
+__global__ __launch_bounds__((RowsShape<T, DB>::kThreads), 1) void cached_rows_kernel(const CacheArgs g) {
+  using S = RowsShape<T, DB>;
+  constexpr int kItem = S::kItem, kWidth = DB * 32, kRing = S::kRing;
+  __shared__ __align__(kTileAlign) uint8_t tiles[2 * kRing * S::kTile];
+  const int lane = threadIdx.x % kWave, wave = uniform(int(threadIdx.x / kWave));
+  const int half = lane / 32, column = lane % 32;
+  const int kv = blockIdx.y, part = blockIdx.x;
+  const Reader<T, DB> lanes(lane);
+  Rows<T, DB> rows;
+  Walk walk = begin_walk<S>(g, part);
+  Stretch now;
+  if (g.head < kWidth) {
+    clear_tiles<2 * kRing * S::kTile, S::kThreads>(tiles);
+    __syncthreads();
+  }
+  while (next_stretch<S>(g, walk, now)) {
+    const Step& st = now.st;
+    const int item0 = int(now.item) * kItem, row0 = item0 + wave * 32, left = st.span.size() * g.group - row0;
+    const int count = left < 0 ? 0 : left < 32 ? left : 32;
+    const int item_rows = st.span.size() * g.group - item0, item_count = item_rows < kItem ? item_rows : kItem;
+    // (a wavefront without rows of its own takes part with the item's last one)
+    const auto row_of = [&](int c) { return count > 0 ? row0 + (c < count ? c : count - 1) : item0 + item_count - 1; };
+    const int row = row_of(column);
+    const int token = st.span.begin + row / g.group, head = kv * g.group + row % g.group;
+    const Sight of_item = sight_of(g, st, item0, item_count);
+    const Sight sight = count > 0 ? sight_of(g, st, row0, count) : Sight{0, 0};
+    rows.q.load(static_cast<const T*>(g.q) + token * g.q_stride + int64_t(head) * g.head, half, g.head * int(sizeof(T)) / 16);
+    const int begin = now.unit0 * S::kUnit, stop = of_item.some < now.unit1 * S::kUnit ? of_item.some : now.unit1 * S::kUnit;
+    const int steps = begin < stop ? pieces(stop - begin, 32) : 0;
+    constexpr int kLoads = 2 * ((32 * Head<T, DB>::kRowBytes / 1024 + S::kWaves - 1) / S::kWaves);  // of a wavefront and step
+    const auto run = [&](auto apart) {
+      rows.clear();
+      uint32_t there[kRing];
+      Window window(g, st, walk.seq);
+      const auto fetch = [&](int step, uint32_t& exists) {
+        exists = 0;
+        if (step >= steps) return;
+        const uint32_t to = lds_offset(tiles) + uint32_t(step % kRing) * 2u * S::kTile;
+        const int key0 = begin + step * 32;
+        exists = fetch_places<T, DB, S::kWaves, false>(g, st, pages_of(g, st, window, key0), kv, key0, wave, to, to + S::kTile);
+      };
+#pragma unroll
+      for (int i = 0; i < kRing - 1; ++i) fetch(i, there[i]);
+      for (int step = 0; step < steps; ++step) {
+        if (step + kRing - 1 <= steps) wait_for_loads<(kRing - 2) * kLoads>();
+        else wait_for_loads<0>();
+        __syncthreads();
+        fetch(step + kRing - 1, there[kRing - 1]);
+        const int key0 = begin + step * 32;
+        const uint32_t now_there = there[0];
+#pragma unroll
+        for (int i = 0; i + 1 < kRing; ++i) there[i] = there[i + 1];
+        if (key0 >= sight.some) continue;
+        const uint8_t* const kt = tiles + step % kRing * 2 * S::kTile;
+        rows.take(kt, kt + S::kTile, lanes.fresh(), g.scale, key0 + 32 > sight.all || now_there != ~0u,
+                  [&] {
+                    const int of_step = row_of(fresh_lane() % 32) / g.group;
+                    return seen_among(g, st, of_step, st.span.begin + of_step, key0) & now_there;
+                  },
+                  apart);
+      }
+      __syncthreads();  // the tiles are free for the next stretch
+    };
+    run(Flag<false>{});
+    if (__syncthreads_or(column < count && !finite_column<DB>(rows.acc))) run(Flag<true>{});
+    const float sum = halves_sum(rows.sum);
+    if (column >= count) continue;
+    const bool begins = now.unit0 == 0, ends = now.unit1 == st.units;
+    if (begins && ends) {
+      store_column<T, DB>(static_cast<T*>(g.o) + token * g.o_stride + int64_t(head) * g.head, rows.acc, half, g.head, sum == 0.0f ? 0.0f : 1.0f / sum);
+    } else {
+      float* const slot = slot_at<S>(g, kv, part, begins, kWidth);
+      const int r = wave * 32 + column;
+      store_column<float, DB>(slot + r * kWidth, rows.acc, half, kWidth, 1.0f);
+      if (half == 0) {
+        slot[kItem * kWidth + r] = rows.largest;
+        slot[kItem * kWidth + kItem + r] = sum;
+      }
+    }
   }
 }
 
@@ -284,50 +454,51 @@ constexpr int kMaxParts = 256;  // of a key head's work
 __device__ __forceinline__ int up_to_block(int v) { return (v + kBlock - 1) / kBlock * kBlock; }
 
 // Items in several pieces: their results together; and zeros for tokens behind the last sequence.
-template <typename T, int DB>
+template <typename T, int DB, typename S>
 __global__ __launch_bounds__(kBlock) void cached_join_kernel(const CacheArgs g) {
-  using S = Shape<T, DB>;
-  constexpr int kWidth = DB * 32;
-  __shared__ float factors[kMaxParts][kItem], sums[kMaxParts][kItem], total[kItem];
+  constexpr int kWidth = DB * 32, kItem = S::kItem, kRows = 32;
+  __shared__ float factors[kMaxParts][kRows], sums[kMaxParts][kRows], total[kRows];
   __shared__ v4f_t halves[kBlock];
-  const int kv = blockIdx.y;
-  const Found f = find_among(g.sequences, blockIdx.x, [&](int s) { return step_of(g, s, S::kUnit).items; });
-  const int seq = uniform(f.seq);
-  const int64_t item = int64_t(blockIdx.x) - uniform(f.before);
+  const int kv = blockIdx.y, row_in = int(blockIdx.z) * kRows;  // of the item
+  const auto items = [&](int s) { return step_of<S>(g, s).items; };
+  const Found f = Index<decltype(items)>(g.sequences, items).find(blockIdx.x);
+  const int seq = f.seq;
+  const int64_t item = int64_t(blockIdx.x) - f.before;
   if (seq < 0) {
     if (!g.zeros) return;
     const int rest = rest_of(g.offsets, g.sequences, g.tokens);
-    for (int i = threadIdx.x; i < kItem * g.head; i += kBlock) {
-      const int64_t flat = item * kItem + i / g.head, token = rest + flat / g.group;
+    for (int i = threadIdx.x; i < kRows * g.head; i += kBlock) {
+      const int64_t flat = item * kItem + row_in + i / g.head, token = rest + flat / g.group;
       if (token >= g.tokens) break;
       store_one(static_cast<T*>(g.o) + token * g.o_stride + (kv * g.group + flat % g.group) * g.head + i % g.head, 0.0f);
     }
     return;
   }
-  const Step st = uniform_step(g, seq, S::kUnit);
+  const Step st = uniform_step<S>(g, seq);
   const auto work = [&](int s) {
-    const Step each = step_of(g, s, S::kUnit);
+    const Step each = step_of<S>(g, s);
     return each.items * each.units;
   };
-  const int64_t all = uniform(find_among(g.sequences, INT64_MAX, work).before);
-  const int64_t before = uniform(find_among(seq, INT64_MAX, work).before);
+  const Index<decltype(work)> index(g.sequences, work);
+  const int64_t all = index.total, before = index.before(seq);
   const int parts = used_parts(all, g.parts);
   const int64_t first = before + item * st.units, last = first + st.units - 1;
   const auto part_of = [&](int64_t unit) {
-    int p = int(unit * parts / all);
+    int p = int(quotient(unit * parts, all));
     while (p + 1 < parts && part_begin(all, parts, p + 1) <= unit) ++p;
     while (p > 0 && part_begin(all, parts, p) > unit) --p;
     return p;
   };
   const int p0 = part_of(first), p1 = part_of(last);
   if (p0 == p1) return;  // its part wrote the result
-  const int64_t rows = int64_t(st.span.size()) * g.group, row0 = item * kItem;
-  const int count = int(rows - row0 < kItem ? rows - row0 : kItem);
+  const int row0 = int(item) * kItem + row_in, left = st.span.size() * g.group - row0;
+  const int count = left < kRows ? left : kRows;
+  if (count <= 0) return;
   const int pieces_of = p1 - p0 + 1;  // at most kBlock
   // what every piece counts for in every row
   for (int i = threadIdx.x; i < count * pieces_of; i += kBlock) {
     const int r = i % count, p = i / count;
-    const float* const slot = slot_at(g, kv, p0 + p, p == 0, kWidth) + kItem * kWidth;
+    const float* const slot = slot_at<S>(g, kv, p0 + p, p == 0, kWidth) + kItem * kWidth + row_in;
     factors[p][r] = slot[r];
     sums[p][r] = slot[kItem + r];
   }
@@ -354,7 +525,7 @@ __global__ __launch_bounds__(kBlock) void cached_join_kernel(const CacheArgs g) 
     if (at < fours && share < shares) {
 #pragma unroll 4
       for (int p = share; p < pieces_of; p += shares) {
-        const v4f_t x = *reinterpret_cast<const v4f_t*>(slot_at(g, kv, p0 + p, p == 0, kWidth) + r * kWidth + d);
+        const v4f_t x = *reinterpret_cast<const v4f_t*>(slot_at<S>(g, kv, p0 + p, p == 0, kWidth) + (row_in + r) * kWidth + d);
         const float f = factors[p][r];
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] = fmaf(f, x[j], v[j]);
@@ -367,7 +538,7 @@ __global__ __launch_bounds__(kBlock) void cached_join_kernel(const CacheArgs g) 
         for (int o = 1; o < shares; ++o) v += halves[threadIdx.x + o * fours];
     }
     if (share == 0 && at < fours && d < g.head) {
-      const int64_t flat = row0 + r;
+      const int flat = row0 + r;
       T* const to = static_cast<T*>(g.o) + (st.span.begin + flat / g.group) * g.o_stride + (kv * g.group + flat % g.group) * g.head + d;
       const float inverse = total[r] == 0.0f ? 0.0f : 1.0f / total[r];
       const float f[4] = {v[0] * inverse, v[1] * inverse, v[2] * inverse, v[3] * inverse};
@@ -378,17 +549,25 @@ __global__ __launch_bounds__(kBlock) void cached_join_kernel(const CacheArgs g) 
 }
 
 template <typename T, int DB>
-void launch_both(const CacheArgs& g, int64_t items, int kv_heads, hipStream_t s) {
-  cached_kernel<T, DB><<<dim3(g.parts, kv_heads), Shape<T, DB>::kThreads, 0, s>>>(g);
-  cached_join_kernel<T, DB><<<dim3(uint32_t(items), kv_heads), kBlock, 0, s>>>(g);
+void launch_both(const CacheArgs& g, const CachePlan& p, int kv_heads, hipStream_t s) {
+  const dim3 grid(uint32_t(g.parts), uint32_t(kv_heads));
+  if (p.rows) {
+    using S = RowsShape<T, DB>;
+    cached_rows_kernel<T, DB><<<grid, S::kThreads, 0, s>>>(g);
+    cached_join_kernel<T, DB, S><<<dim3(uint32_t(p.items), kv_heads, S::kItem / 32), kBlock, 0, s>>>(g);
+  } else {
+    using S = KeysShape<T, DB>;
+    cached_keys_kernel<T, DB><<<grid, S::kThreads, 0, s>>>(g);
+    cached_join_kernel<T, DB, S><<<dim3(uint32_t(p.items), kv_heads), kBlock, 0, s>>>(g);
+  }
 }
 template <typename T>
-hipError_t launch(const CacheArgs& g, int64_t items, int kv_heads, hipStream_t s) {
-  if (g.head <= 32) launch_both<T, 1>(g, items, kv_heads, s);
-  else if (g.head <= 64) launch_both<T, 2>(g, items, kv_heads, s);
-  else if (g.head <= 96) launch_both<T, 3>(g, items, kv_heads, s);
-  else if (g.head <= 128) launch_both<T, 4>(g, items, kv_heads, s);
-  else launch_both<T, 8>(g, items, kv_heads, s);
+hipError_t launch(const CacheArgs& g, const CachePlan& p, int kv_heads, hipStream_t s) {
+  if (g.head <= 32) launch_both<T, 1>(g, p, kv_heads, s);
+  else if (g.head <= 64) launch_both<T, 2>(g, p, kv_heads, s);
+  else if (g.head <= 96) launch_both<T, 3>(g, p, kv_heads, s);
+  else if (g.head <= 128) launch_both<T, 4>(g, p, kv_heads, s);
+  else launch_both<T, 8>(g, p, kv_heads, s);
   return hipGetLastError();
 }
 
@@ -398,13 +577,15 @@ int blocks_of_head(int head) { return head <= 32 ? 1 : head <= 64 ? 2 : head <= 
 
 CachePlan make_cache_plan(const accept_cache_desc& d) {
   CachePlan p{};
-  p.items = d.tokens * (d.heads / d.kv_heads) / kItem + d.sequences + 1;
-  // as many workgroups as the chip has room for: one a compute unit, more where shared memory takes more
-  constexpr int kUnits = 256;
-  p.parts = int((kUnits + d.kv_heads - 1) / d.kv_heads);
-  static_assert(kUnits <= kMaxParts, "what a row's pieces count for is in shared memory");
-  const int width = blocks_of_head(d.head_size) * 32;
-  p.bytes = size_t(up_to(int64_t(d.kv_heads) * p.parts * 2 * kItem * (width + 2) * 4, 256));
+  const int64_t rows = d.tokens * (d.heads / d.kv_heads);
+  p.rows = rows > 32 * d.sequences;  // more than one wavefront's, of a sequence on average
+  const int blocks = blocks_of_head(d.head_size), width = blocks * 32;
+  const int item = !p.rows ? 32 : blocks * (d.dtype == ACCEPT_F32 ? 4 : 2) <= 8 ? 256 : 128;  // (as in RowsShape)
+  p.items = rows / item + d.sequences + 1;
+  // as many workgroups as the chip has room for: one a compute unit, two where few rows of short heads leave room in shared memory
+  const int64_t groups = !p.rows && d.dtype == ACCEPT_BF16 && d.head_size <= 64 ? 512 : 256;
+  p.parts = int(blocks_of(groups, d.kv_heads) < kMaxParts ? blocks_of(groups, d.kv_heads) : kMaxParts);
+  p.bytes = size_t(up_to(int64_t(d.kv_heads) * p.parts * 2 * item * (width + 2) * 4, 256));
   return p;
 }
 
@@ -429,7 +610,7 @@ hipError_t launch_cache_attention(const accept_cache_desc& d, const CachePlan& p
   g.tree_words = d.tree_words;
   g.zeros = d.rest == ACCEPT_REST_ZEROS;
   g.scale = float(d.scale * 1.4426950408889634074);
-  return d.dtype == ACCEPT_F32 ? launch<float>(g, p.items, d.kv_heads, s) : launch<bf16_t>(g, p.items, d.kv_heads, s);
+  return d.dtype == ACCEPT_F32 ? launch<float>(g, p, d.kv_heads, s) : launch<bf16_t>(g, p, d.kv_heads, s);
 }
 
 }  // namespace accept
