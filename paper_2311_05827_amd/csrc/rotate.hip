@@ -32,8 +32,13 @@ struct RotateArgs {
   int zeros;                  // what becomes of tokens without a sequence
   int lanes;                  // items of a head: vectors of pairs, then vectors that are copied
   int pair_lanes;
-  int per;                    // heads a thread goes through
+  int per;                    // heads of a thread: some times kBatch, or 1 where that leaves too few threads
   int turning_chunks, chunks; // groups of heads that turn, and all
+};
+
+template <int N>
+struct Number {
+  static constexpr int value = N;
 };
 
 template <typename T, int N>
@@ -53,17 +58,18 @@ __device__ __forceinline__ void store_n(T* p, const float (&f)[N]) {
   else *reinterpret_cast<uint4*>(p) = narrow(f);
 }
 
-// A thread has the same part of some heads of one token: N pairs (their sines once for all of those heads), or 16 bytes that are copied.  Pairs come in
+constexpr int kBatch = 4;
+// A thread has the same part of some heads of one token: N pairs (their sines once for all of those heads, whose loads go out together), or 16 bytes that are copied.  Pairs come in
 // vectors of 16 bytes (halves: one of each half; neighbours: two behind each other) where those are whole, else one at a time.
 // CACHE: heads are those of q (if there are any), then of k, into their places; then v's, copied.
 template <typename T, int N, bool NEIGHBOURS, bool CACHE>
 __global__ __launch_bounds__(kBlock) void rotate_kernel(const RotateArgs g) {
   constexpr int VEC = 16 / int(sizeof(T));
   const int64_t at = (int64_t(blockIdx.y) * gridDim.x + blockIdx.x) * kBlock + threadIdx.x;
-  const int64_t per_token = int64_t(g.lanes) * g.chunks;
-  const int64_t all = per_token * g.tokens;
+  const uint32_t per_token = uint32_t(g.lanes) * uint32_t(g.chunks);
+  const int64_t all = int64_t(per_token) * g.tokens;
   const bool mine = at < all;
-  const int token = mine ? int(at / per_token) : g.tokens - 1;
+  const int token = !mine ? g.tokens - 1 : all >> 32 == 0 ? int(uint32_t(at) / per_token) : int(at / per_token);
   // the token's sequence: a wavefront's tokens lie next to each other, so the first one's is searched for, and from there on
   int seq = 0, place = token;
   bool outside = false;
@@ -84,7 +90,8 @@ __global__ __launch_bounds__(kBlock) void rotate_kernel(const RotateArgs g) {
     outside = token >= rest_of(g.offsets, g.sequences, g.tokens);
   }
   if (!mine) return;
-  const int in_token = int(at - int64_t(token) * per_token), chunk = in_token / g.lanes, item = in_token - chunk * g.lanes;
+  const uint32_t in_token = uint32_t(at - int64_t(token) * per_token);
+  const int chunk = int(in_token / uint32_t(g.lanes)), item = int(in_token) - chunk * g.lanes;
   int length = 0;
   int64_t row = -1;  // of key head 0 in the caches
   if (CACHE && !outside) {
@@ -103,9 +110,16 @@ __global__ __launch_bounds__(kBlock) void rotate_kernel(const RotateArgs g) {
     const int first = (chunk - g.turning_chunks) * g.per, end = first + g.per < g.kv_heads ? first + g.per : g.kv_heads;
     const T* const v = static_cast<const T*>(g.v) + token * g.v_stride;
     T* const to = static_cast<T*>(g.v_cache);
-    for (int h = first; h < end; ++h)
-      for (int c = item; c < g.head / VEC; c += g.lanes)
-        *reinterpret_cast<uint4*>(to + (row + h * head_rows) * g.head + c * VEC) = load16(v + h * g.head + c * VEC);
+    for (int h = first; h < end; h += kBatch)
+      for (int c = item; c < g.head / VEC; c += g.lanes) {
+        uint4 part[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i)
+          if (h + i < end) part[i] = load16(v + (h + i) * g.head + c * VEC);
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i)
+          if (h + i < end) *reinterpret_cast<uint4*>(to + (row + (h + i) * head_rows) * g.head + c * VEC) = part[i];
+      }
     return;
   }
   const int turning = g.heads + (CACHE ? g.kv_heads : 0);
@@ -120,61 +134,69 @@ __global__ __launch_bounds__(kBlock) void rotate_kernel(const RotateArgs g) {
       s[i] *= g.sign;
     }
   }
-  for (int h = first; h < end; ++h) {
-    const T* from;
-    T* to;
-    if (!CACHE || h < g.heads) {
-      from = static_cast<const T*>(g.q) + token * g.q_stride + h * g.head;
-      to = static_cast<T*>(g.qo) + token * g.qo_stride + h * g.head;
-    } else {
-      if (row < 0) break;  // (keys come last)
-      from = static_cast<const T*>(g.k) + token * g.k_stride + (h - g.heads) * g.head;
-      to = static_cast<T*>(g.k_cache) + (row + (h - g.heads) * head_rows) * g.head;
+  // BATCH heads at a time: what they read is asked for before any of it is used
+  const auto go = [&](auto batch, int first) {
+    constexpr int kHeads = decltype(batch)::value;
+    const T* from[kHeads];
+    T* to[kHeads];
+    bool here[kHeads];
+#pragma unroll
+    for (int i = 0; i < kHeads; ++i) {
+      const int h = first + i;
+      if (!CACHE || h < g.heads) {
+        from[i] = static_cast<const T*>(g.q) + token * g.q_stride + h * g.head;
+        to[i] = static_cast<T*>(g.qo) + token * g.qo_stride + h * g.head;
+        here[i] = h < end;
+      } else {
+        from[i] = static_cast<const T*>(g.k) + token * g.k_stride + (h - g.heads) * g.head;
+        to[i] = static_cast<T*>(g.k_cache) + (row + (h - g.heads) * head_rows) * g.head;
+        here[i] = h < end && row >= 0;
+      }
     }
     if (!pair) {
       const int copied = 2 * g.half + (item - g.pair_lanes) * (N == 1 ? 1 : VEC);
-      if constexpr (N == 1) {
-        store_one(to + copied, outside ? 0.0f : load_one(from + copied));
-      } else {
-        *reinterpret_cast<uint4*>(to + copied) = outside ? make_uint4(0, 0, 0, 0) : load16(from + copied);
-      }
-    } else if constexpr (NEIGHBOURS) {
-      constexpr int V = N == 1 ? 1 : VEC;
-      float f[2 * N];
+      uint4 v[kHeads];
 #pragma unroll
-      for (int p = 0; p < 2 * N; p += V) {
-        float part[V];
-        load_n<T, V>(from + item * 2 * N + p, part);
-#pragma unroll
-        for (int i = 0; i < V; ++i) f[p + i] = part[i];
+      for (int i = 0; i < kHeads; ++i) {
+        if constexpr (N == 1) v[i].x = here[i] && !outside ? f32_as_u32(load_one(from[i] + copied)) : 0u;
+        else v[i] = here[i] && !outside ? load16(from[i] + copied) : make_uint4(0, 0, 0, 0);
       }
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float a = f[2 * i], b = f[2 * i + 1];
-        f[2 * i] = outside ? 0.0f : fmaf(a, c[i], -(b * s[i]));
-        f[2 * i + 1] = outside ? 0.0f : fmaf(a, s[i], b * c[i]);
+      for (int i = 0; i < kHeads; ++i) {
+        if (!here[i]) continue;
+        if constexpr (N == 1) store_one(to[i] + copied, u32_as_f32(v[i].x));
+        else *reinterpret_cast<uint4*>(to[i] + copied) = v[i];
       }
-#pragma unroll
-      for (int p = 0; p < 2 * N; p += V) {
-        float part[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) part[i] = f[p + i];
-        store_n<T, V>(to + item * 2 * N + p, part);
-      }
-    } else {
-      float a[N], b[N];
-      load_n<T, N>(from + item * N, a);
-      load_n<T, N>(from + g.half + item * N, b);
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float x = a[i], y = b[i];
-        a[i] = outside ? 0.0f : fmaf(x, c[i], -(y * s[i]));
-        b[i] = outside ? 0.0f : fmaf(x, s[i], y * c[i]);
-      }
-      store_n<T, N>(to + item * N, a);
-      store_n<T, N>(to + g.half + item * N, b);
+      return;
     }
-  }
+    // a pair's first values and its second ones: of halves, or neighbours (N = 1: one pair; else a vector's N / 2, and the next one's)
+    const int at_a = NEIGHBOURS ? item * 2 * N : item * N, at_b = NEIGHBOURS ? at_a + N : g.half + item * N;
+    float a[kHeads][N], b[kHeads][N];
+#pragma unroll
+    for (int i = 0; i < kHeads; ++i) {
+      if (!here[i]) continue;
+      load_n<T, N>(from[i] + at_a, a[i]);
+      load_n<T, N>(from[i] + at_b, b[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kHeads; ++i) {
+      if (!here[i]) continue;
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        // values j of the two vectors; neighbours: pairs lie inside a vector, and the second vector has the second half of them
+        float& x = !NEIGHBOURS || N == 1 ? a[i][j] : j < N / 2 ? a[i][2 * j] : b[i][2 * j - N];
+        float& y = !NEIGHBOURS || N == 1 ? b[i][j] : j < N / 2 ? a[i][2 * j + 1] : b[i][2 * j - N + 1];
+        const float p = x, q = y;
+        x = outside ? 0.0f : fmaf(p, c[j], -(q * s[j]));
+        y = outside ? 0.0f : fmaf(p, s[j], q * c[j]);
+      }
+      store_n<T, N>(to[i] + at_a, a[i]);
+      store_n<T, N>(to[i] + at_b, b[i]);
+    }
+  };
+  if (g.per == 1) go(Number<1>{}, first);
+  else
+    for (int h = first; h < end; h += kBatch) go(Number<kBatch>{}, h);
 }
 
 template <typename T, bool CACHE>
@@ -185,7 +207,11 @@ hipError_t launch(RotateArgs g, int pairs, hipStream_t s) {
   g.pair_lanes = g.half / n;
   g.lanes = g.pair_lanes + (g.head - 2 * g.half) / n;
   const int turning = g.heads + (CACHE ? g.kv_heads : 0);
-  g.per = 1;
+  // As many threads as keep every compute unit busy, and beyond that kBatch heads each, twice that for a cache, where a thread begins with a trip
+  // to memory each for its sequence, its length and its page: 8144 tokens x 16 heads x 64 in bfloat16 10.9 us with a head a thread, 7.2 with four;
+  // 16332 tokens x 48 heads x 128 into pages 114 with one, 97 with four, 92 with eight (tensors without a cache: 159 and 162 us for 819 MB).
+  const int64_t threads = int64_t(g.tokens) * g.lanes * turning;
+  g.per = threads < 65536 * kBatch ? 1 : CACHE && threads >= 8 * 65536 * kBatch ? 2 * kBatch : kBatch;
   g.turning_chunks = int(blocks_of(turning, g.per));
   g.chunks = g.turning_chunks + (CACHE ? int(blocks_of(g.kv_heads, g.per)) : 0);
   const int64_t groups = blocks_of(int64_t(g.tokens) * g.lanes * g.chunks, kBlock);
