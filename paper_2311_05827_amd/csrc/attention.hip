@@ -15,7 +15,8 @@ struct AttentionArgs {
   int64_t q_stride, k_stride, v_stride, o_stride;
   int sequences, q_tokens, k_tokens, q_each, k_each;
   int heads, group, head;
-  int tiles;      // of a head: at most so many
+  float* shares;  // [share][heads][q_tokens][width + 2]: sums of values, maximum, sum of weights, where a row's keys are shared out
+  int split;      // in so many
   int causal, zeros;
   float scale;    // times log2(e)
 };
@@ -30,19 +31,20 @@ constexpr float kBehind = 8.0f;
 // A workgroup has 128 queries of a head, a wavefront 32 of them: as columns, so that a lane has a query of its own (its
 // maximum, sum and factor are the lane's, two lanes' together) and the weights come out of the first product in the registers that the second one
 // takes them from.  Tiles of keys and values come into shared memory one ahead.
-template <typename T, int DB>
+template <typename T, int DB, bool SPLIT>
 __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) void attention_kernel(const AttentionArgs g) {
   constexpr int NB = sizeof(T) == 2 ? 2 : 1, BN = 32 * NB;
   constexpr int kTile = BN * Head<T, DB>::kRowBytes;
   __shared__ __align__(kTileAlign) uint8_t tiles[4 * kTile];  // keys, values; and the next ones
   const int lane = threadIdx.x % kWave, wave = uniform(int(threadIdx.x / kWave));
   const int half = lane / 32, column = lane % 32;
-  const HeadPiece hp = deal(blockIdx.x, g.heads);
-  const int head = hp.head;
+  const int split = SPLIT ? g.split : 1;
+  const HeadPiece hp = deal(blockIdx.x, g.heads * split);
+  const int head = SPLIT ? hp.head / split : hp.head, share = SPLIT ? hp.head % split : 0;
   const Piece piece = find_piece(g.q_offsets, g.sequences, g.q_tokens, g.q_each, kRows, hp.index);
   const int seq = piece.seq, tile = piece.tile;
   if (seq < 0) {  // pieces that no sequence has: the tokens behind the last one
-    if (!g.zeros) return;
+    if (!g.zeros || share > 0) return;
     const int rest = rest_of(g.q_offsets, g.sequences, g.q_tokens);
     const int parts = g.head * int(sizeof(T)) / 16;
     for (int i = threadIdx.x; i < kRows * parts; i += kWaves * kWave) {
@@ -70,7 +72,8 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
   const int first_limit = row0 < rows ? seen_by(row0) : 0;    // all of the wavefront's queries do
   const int wave_limit = row0 < rows ? seen_by(row0 + 31 < last ? row0 + 31 : last) : 0;
   const int end = tile * kRows + kRows - 1;
-  const int steps = pieces(seen_by(end < last ? end : last), BN);
+  const int all_steps = pieces(seen_by(end < last ? end : last), BN);
+  const int step0 = SPLIT ? int(int64_t(all_steps) * share / split) : 0, steps = SPLIT ? int(int64_t(all_steps) * (share + 1) / split) : all_steps;
 
   const int parts = g.head * int(sizeof(T)) / 16;
   RowParts<T, DB> q;
@@ -98,8 +101,8 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
     for (int db = 0; db < DB; ++db) acc[db] = v16f_t{};
     largest = -INFINITY;
     sum = 0.0f;
-    if (steps > 0) fetch(0);
-    for (int step = 0; step < steps; ++step) {
+    if (step0 < steps) fetch(step0);
+    for (int step = step0; step < steps; ++step) {
       __builtin_amdgcn_s_waitcnt(0);
       __syncthreads();
       if (step + 1 < steps) fetch(step + 1);
@@ -155,30 +158,80 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
   sum = halves_sum(sum);
   if (!is_row) return;
   const int64_t token = qs.begin + row;
+  if constexpr (SPLIT) {
+    float* const to = g.shares + ((int64_t(share) * g.heads + head) * g.q_tokens + token) * (DB * 32 + 2);
+    store_pairs<DB>(to, acc, half);
+    if (half == 0) *reinterpret_cast<float2*>(to + DB * 32) = make_float2(largest, sum);
+    return;
+  }
   store_column<T, DB>(static_cast<T*>(g.o) + token * g.o_stride + int64_t(head) * g.head, acc, half, g.head, sum == 0.0f ? 0.0f : 1.0f / sum);
   if (g.lse && half == 0)
     g.lse[int64_t(head) * g.q_tokens + token] = sum == 0.0f ? -INFINITY : (largest + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
+// A row's shares together, relative to the largest of their maxima: four values a thread.
+template <typename T, int DB>
+__global__ __launch_bounds__(kBlock) void attention_join_kernel(const AttentionArgs g) {
+  constexpr int kWidth = DB * 32, kFours = kWidth / 4;
+  const int64_t at = int64_t(blockIdx.x) * kBlock + threadIdx.x, row = at / kFours;  // head, token
+  const int d = int(at % kFours) * 4;
+  if (row >= int64_t(g.heads) * g.q_tokens) return;
+  const int head = int(row / g.q_tokens), token = int(row % g.q_tokens);
+  if (token >= rest_of(g.q_offsets, g.sequences, g.q_tokens)) return;
+  const int64_t apart = int64_t(g.heads) * g.q_tokens * (kWidth + 2);
+  const float* const from = g.shares + row * (kWidth + 2);
+  float top = -INFINITY;
+  for (int p = 0; p < g.split; ++p) top = fmaxf(top, from[p * apart + kWidth]);
+  float v[4] = {0, 0, 0, 0}, sum = 0.0f;
+  for (int p = 0; p < g.split; ++p) {
+    const float peak = from[p * apart + kWidth], factor = peak == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(peak - top);
+    sum = fmaf(factor, from[p * apart + kWidth + 1], sum);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = fmaf(factor, from[p * apart + d + j], v[j]);
+  }
+  if (g.lse && d == 0) g.lse[row] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+  if (d >= g.head) return;
+  const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
+  T* const to = static_cast<T*>(g.o) + token * g.o_stride + int64_t(head) * g.head + d;
+  if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(to) = make_float4(v[0] * inverse, v[1] * inverse, v[2] * inverse, v[3] * inverse);
+  else *reinterpret_cast<uint2*>(to) = make_uint2(bf16_pair(v[0] * inverse, v[1] * inverse), bf16_pair(v[2] * inverse, v[3] * inverse));
+}
+
+template <typename T, int DB>
+void launch_head(const AttentionArgs& g, uint32_t groups, hipStream_t s) {
+  if (g.split == 1) return attention_kernel<T, DB, false><<<dim3(groups), kWaves * kWave, 0, s>>>(g);
+  attention_kernel<T, DB, true><<<dim3(groups * uint32_t(g.split)), kWaves * kWave, 0, s>>>(g);
+  attention_join_kernel<T, DB><<<dim3(uint32_t(blocks_of(int64_t(g.heads) * g.q_tokens * DB * 8, kBlock))), kBlock, 0, s>>>(g);
+}
 template <typename T>
-hipError_t launch(const AttentionArgs& g, hipStream_t s) {
-  const int64_t groups = int64_t(g.heads) * g.tiles;
-  const dim3 grid(static_cast<uint32_t>(groups));
-  constexpr int kThreads = kWaves * kWave;
-  if (g.head <= 32) attention_kernel<T, 1><<<grid, kThreads, 0, s>>>(g);
-  else if (g.head <= 64) attention_kernel<T, 2><<<grid, kThreads, 0, s>>>(g);
-  else if (g.head <= 96) attention_kernel<T, 3><<<grid, kThreads, 0, s>>>(g);
-  else if (g.head <= 128) attention_kernel<T, 4><<<grid, kThreads, 0, s>>>(g);
-  else attention_kernel<T, 8><<<grid, kThreads, 0, s>>>(g);
+hipError_t launch(const AttentionArgs& g, int64_t tiles, hipStream_t s) {
+  const uint32_t groups = uint32_t(g.heads * tiles);
+  if (g.head <= 32) launch_head<T, 1>(g, groups, s);
+  else if (g.head <= 64) launch_head<T, 2>(g, groups, s);
+  else if (g.head <= 96) launch_head<T, 3>(g, groups, s);
+  else if (g.head <= 128) launch_head<T, 4>(g, groups, s);
+  else launch_head<T, 8>(g, groups, s);
   return hipGetLastError();
 }
 
+int64_t tiles_of(const accept_attention_desc& d) { return blocks_of(d.q_tokens, kRows) + d.sequences; }  // of a head: at most so many
+
 }  // namespace
 
-AttentionPlan make_attention_plan(const accept_attention_desc&) { return {0}; }
+AttentionPlan make_attention_plan(const accept_attention_desc& d) {
+  AttentionPlan p{1, 0};
+  // A piece's keys are one workgroup's work, one tile after the other, and there are two workgroups a compute unit: where there are fewer, the
+  // keys are shared out, as long as a share has some.
+  constexpr int64_t kEnough = 512, kMost = 16, kKeys = 512;
+  const int64_t groups = (tiles_of(d) - (d.sequences > 0)) * d.heads, keys = d.sequences > 0 ? blocks_of(d.k_tokens, d.sequences) : 0;
+  while (p.split < kMost && groups * p.split * 2 <= kEnough && keys >= kKeys * 2 * p.split) p.split *= 2;
+  const int64_t width = d.head_size <= 32 ? 32 : d.head_size <= 64 ? 64 : d.head_size <= 96 ? 96 : d.head_size <= 128 ? 128 : 256;
+  if (p.split > 1) p.bytes = size_t(up_to(4 * int64_t(p.split) * d.heads * d.q_tokens * (width + 2), 256));
+  return p;
+}
 
-hipError_t launch_attention(const accept_attention_desc& d, const AttentionPlan&, const void* q, const void* k, const void* v,
-                            const int32_t* q_offsets, const int32_t* k_offsets, void* o, float* lse, void*, hipStream_t s) {
+hipError_t launch_attention(const accept_attention_desc& d, const AttentionPlan& p, const void* q, const void* k, const void* v,
+                            const int32_t* q_offsets, const int32_t* k_offsets, void* o, float* lse, void* ws, hipStream_t s) {
   AttentionArgs g{};
   const int64_t whole = int64_t(d.heads) * d.head_size, kv_whole = int64_t(d.kv_heads) * d.head_size;
   g.q = q;
@@ -186,6 +239,8 @@ hipError_t launch_attention(const accept_attention_desc& d, const AttentionPlan&
   g.v = v;
   g.o = o;
   g.lse = lse;
+  g.shares = static_cast<float*>(ws);
+  g.split = p.split;
   g.q_offsets = q_offsets;
   g.k_offsets = k_offsets;
   g.q_stride = d.q_stride ? d.q_stride : whole;
@@ -200,11 +255,11 @@ hipError_t launch_attention(const accept_attention_desc& d, const AttentionPlan&
   g.heads = d.heads;
   g.group = d.heads / d.kv_heads;
   g.head = d.head_size;
-  g.tiles = int(q_offsets ? blocks_of(d.q_tokens, kRows) + d.sequences : d.sequences * blocks_of(g.q_each, kRows));
+  const int64_t tiles = q_offsets ? tiles_of(d) : d.sequences * blocks_of(g.q_each, kRows);
   g.causal = d.causal;
   g.zeros = d.rest == ACCEPT_REST_ZEROS;
   g.scale = float(d.scale * 1.4426950408889634074);
-  return d.dtype == ACCEPT_F32 ? launch<float>(g, s) : launch<bf16_t>(g, s);
+  return d.dtype == ACCEPT_F32 ? launch<float>(g, tiles, s) : launch<bf16_t>(g, tiles, s);
 }
 
 }  // namespace accept

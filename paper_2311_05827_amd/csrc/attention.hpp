@@ -15,7 +15,8 @@ hipError_t launch_cache_append(const accept_cache_desc& d, const void* q, const 
                                const int32_t* offsets, const int32_t* lengths, const int32_t* positions, const int32_t* table,
                                void* qo, void* k_cache, void* v_cache, hipStream_t s);
 struct AttentionPlan {
-  size_t bytes;  // workspace
+  int split;     // shares of a row's keys
+  size_t bytes;  // workspace: the shares' results
 };
 AttentionPlan make_attention_plan(const accept_attention_desc& d);
 hipError_t launch_attention(const accept_attention_desc& d, const AttentionPlan& p, const void* q, const void* k, const void* v,
@@ -447,6 +448,14 @@ __device__ __forceinline__ void store_column(T* row, const v16f_t (&acc)[DB], in
         *reinterpret_cast<uint2*>(row + value) = make_uint2(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3]));
       }
     }
+}
+// The same as floats, from an address that is a multiple of 8 bytes.
+template <int DB>
+__device__ __forceinline__ void store_pairs(float* row, const v16f_t (&acc)[DB], int half) {
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) *reinterpret_cast<float2*>(row + db * 32 + result_row(r, half)) = make_float2(acc[db][r], acc[db][r + 1]);
 }
 // Not finite anywhere in the values that are stored?
 template <int DB>

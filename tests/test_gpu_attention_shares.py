@@ -1,0 +1,102 @@
+"""Attention whose keys, or whose keys' queries, are shared out among workgroups because there are few: against the oracle in 64 bits, and what a
+share does not see or has none of."""
+import numpy as np
+import pytest
+
+from attention_util import ints
+from stage_util import f64, torch_mod
+from test_gpu_attention import Case
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def A():
+    torch = torch_mod()
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    import paper_2311_05827_amd as pkg
+    return pkg
+
+
+# lengths of queries and keys, heads, key heads, head size, shares expected at least (forward, backward)
+SIZES = [
+    ([1], [5000], 1, 1, 64, 4, 1),
+    ([3, 1], [1100, 3000], 2, 1, 128, 2, 1),
+    ([1500], [1500], 2, 1, 128, 2, 4),
+    ([2100, 0, 40], [2100, 7, 40], 2, 2, 80, 1, 2),
+    ([2000], [300], 4, 1, 64, 1, 8),            # most rows see no key
+    ([1200], [1200], 1, 1, 256, 2, 2),
+]
+
+
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("q_lengths,k_lengths,heads,kv_heads,head,forward,backward", SIZES)
+def test_both_passes(A, name, causal, q_lengths, k_lengths, heads, kv_heads, head, forward, backward):
+    c = Case(A, 1, name, q_lengths, k_lengths, heads, kv_heads, head, causal)
+    one = 4 * heads * c.nq * head
+    assert A.accept_attention_workspace_size(c.desc) >= (forward * one if forward > 1 else 0)
+    assert A.accept_attention_backward_workspace_size(c.desc) >= (8 * backward * c.nk * kv_heads * head if backward > 1 else 0)
+    c.forward()
+    c.check_forward()
+    c.check_backward(c.backward())
+
+
+def test_rows_behind_the_last_sequence(A):
+    torch = torch_mod()
+    c = Case(A, 2, "bf16", [1100, 900], [1100, 900], 2, 1, 64, behind=70)
+    assert A.accept_attention_backward_workspace_size(c.desc) > 8 * 2 * c.nq + 256
+    c.forward()
+    made = c.backward()
+    assert torch.all(c.o[2000:] == 0) and torch.all(c.lse[:, 2000:] == -float("inf")) and all(torch.all(g[2000:] == 0) for g in made)
+    o, lse, grads = torch.full_like(c.o, 7.0), torch.full_like(c.lse, 7.0), [torch.full_like(g, 7.0) for g in made]
+    first = c.o.clone()
+    c.forward(o=o, lse=lse)
+    c.backward(dq=grads[0], dk=grads[1], dv=grads[2])
+    assert torch.all(o[2000:] == 7) and torch.all(lse[:, 2000:] == 7) and all(torch.all(g[2000:] == 7) for g in grads)
+    assert torch.equal(o[:2000], first[:2000]) and all(torch.equal(g[:2000], m[:2000]) for g, m in zip(grads, made))
+
+
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+def test_what_is_not_seen_has_no_effect(A, name):
+    """A value that is NaN is seen by the rows from its own on, in one share only."""
+    def spoil(values):
+        values["v"][1300, 0, 5] = np.nan
+    c = Case(A, 3, name, [1500], [1500], 1, 1, 64, change=spoil)
+    assert A.accept_attention_workspace_size(c.desc) > 0
+    o = f64(c.forward()[0])
+    assert np.isfinite(o[:1300]).all() and np.isnan(o[1300:, 0, 5]).all() and np.isfinite(np.delete(o, 5, axis=2)).all()
+    c.check_forward()
+
+
+def test_the_same_bits_and_workspaces(A):
+    """Again, with a workspace that holds NaN, on another stream and captured."""
+    torch = torch_mod()
+    c = Case(A, 4, "bf16", [1600], [1600], 2, 1, 64)
+    fw = torch.full((A.accept_attention_workspace_size(c.desc) // 4,), float("nan"), device="cuda")
+    bw = torch.full((A.accept_attention_backward_workspace_size(c.desc) // 4,), float("nan"), device="cuda")
+    want = [*c.forward(), *c.backward()]
+    assert fw.numel() > 0
+    for _ in range(2):
+        got = [*c.forward(workspace=fw.view(torch.uint8)), *c.backward(workspace=bw.view(torch.uint8))]
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = [*c.forward(), *c.backward()]
+    for _ in range(3):
+        c.t["q"].normal_()
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = [*c.forward(), *c.backward()]
+        assert all(torch.equal(a, b) for a, b in zip(held, eager))
+    with pytest.raises(A.AcceptError):
+        c.forward(workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
+
+
+def test_without_offsets(A):
+    c = Case(A, 5, "bf16", [1100, 1100], [1100, 1100], 1, 1, 128, packed=False)
+    assert A.accept_attention_workspace_size(c.desc) > 0
+    c.forward()
+    c.check_forward()
+    c.check_backward(c.backward())
