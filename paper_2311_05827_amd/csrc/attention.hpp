@@ -22,8 +22,10 @@ AttentionPlan make_attention_plan(const accept_attention_desc& d);
 hipError_t launch_attention(const accept_attention_desc& d, const AttentionPlan& p, const void* q, const void* k, const void* v,
                             const int32_t* q_offsets, const int32_t* k_offsets, void* o, float* lse, void* ws, hipStream_t s);
 struct AttentionBackPlan {
-  int split;     // shares of a key tile's queries
-  size_t stats;  // bytes of the rows' statistics, in front of the shares' sums
+  int split;        // shares of a key tile's queries
+  int q_split;      // shares of a query tile's keys
+  size_t stats;     // bytes of the rows' statistics, in front of the shares' sums
+  size_t q_shares;  // where those of the queries are
   size_t bytes;
 };
 AttentionBackPlan make_attention_back_plan(const accept_attention_desc& d);

@@ -16,6 +16,8 @@ struct BackArgs {
   float* stats;  // heads x q_tokens: sums of do * o; and then as many lse, times log2(e)
   float* shares; // [share][dk, dv][k_tokens][kv_heads][head], where a key head's queries are shared out
   int split;     // in so many
+  float* q_shares;  // [share][q_tokens][heads][head]: dq, where a query's keys are shared out
+  int q_split;
   void* dq;
   void* dk;
   void* dv;
@@ -50,12 +52,12 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
   __shared__ __align__(kTileAlign) uint8_t tiles[4 * kTile];
   const int lane = threadIdx.x % kWave, wave = uniform(int(threadIdx.x / kWave));
   const int half = lane / 32, column = lane % 32;
-  const HeadPiece hp = deal(blockIdx.x, g.heads);
-  const int head = hp.head;
+  const HeadPiece hp = deal(blockIdx.x, g.heads * g.q_split);
+  const int head = hp.head / g.q_split, share = hp.head % g.q_split;
   const Piece piece = find_piece(g.q_offsets, g.sequences, g.q_tokens, g.q_each, kRows, hp.index);
   T* const dq = static_cast<T*>(g.dq) + int64_t(head) * g.head;
   if (piece.seq < 0) {
-    if (g.zeros) clear_rest(dq, g.dq_stride, g.head, rest_of(g.q_offsets, g.sequences, g.q_tokens), piece.tile, g.q_tokens);
+    if (g.zeros && share == 0) clear_rest(dq, g.dq_stride, g.head, rest_of(g.q_offsets, g.sequences, g.q_tokens), piece.tile, g.q_tokens);
     return;
   }
   const Span qs = uniform_span(g.q_offsets, piece.seq, g.q_tokens, g.q_each), ks = uniform_span(g.k_offsets, piece.seq, g.k_tokens, g.k_each);
@@ -70,7 +72,8 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
   const int first_limit = row0 < rows ? seen_by(row0) : 0;
   const int wave_limit = row0 < rows ? seen_by(row0 + 31 < last ? row0 + 31 : last) : 0;
   const int end = piece.tile * kRows + kRows - 1;
-  const int steps = pieces(seen_by(end < last ? end : last), BN);
+  const int all_steps = pieces(seen_by(end < last ? end : last), BN);
+  const int step0 = int(int64_t(all_steps) * share / g.q_split), steps = int(int64_t(all_steps) * (share + 1) / g.q_split);
 
   const int parts = g.head * int(sizeof(T)) / 16;
   const int64_t token = qs.begin + (is_row ? row : last);
@@ -92,7 +95,7 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
     along = halves_sum(along);
   }
   const float lse = g.lse[int64_t(head) * g.q_tokens + token] * kLog2e;
-  if (is_row) g.stats[(int64_t(half) * g.heads + head) * g.q_tokens + token] = half ? lse : along;
+  if (is_row && share == 0) g.stats[(int64_t(half) * g.heads + head) * g.q_tokens + token] = half ? lse : along;
   q.load(static_cast<const T*>(g.q) + token * g.q_stride + int64_t(head) * g.head, half, parts);
 
   const T* const k0 = uniform(static_cast<const T*>(g.k) + ks.begin * g.k_stride + int64_t(head / g.group) * g.head);
@@ -112,8 +115,8 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
   const auto run = [&](auto apart) {  // (see attention_kernel)
 #pragma unroll
     for (int db = 0; db < DB; ++db) acc[db] = v16f_t{};
-    if (steps > 0) fetch(0);
-    for (int step = 0; step < steps; ++step) {
+    if (step0 < steps) fetch(step0);
+    for (int step = step0; step < steps; ++step) {
       __builtin_amdgcn_s_waitcnt(0);
       __syncthreads();
       if (step + 1 < steps) fetch(step + 1);
@@ -147,7 +150,11 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
   };
   run(Flag<false>{});
   if (__syncthreads_or(is_row && !finite_column<DB>(acc))) run(Flag<true>{});
-  if (is_row) store_column<T, DB>(dq + token * g.dq_stride, acc, half, g.head, g.scale);
+  if (!is_row) return;
+  if (g.q_split > 1)
+    store_column<float, DB>(g.q_shares + ((int64_t(share) * g.q_tokens + token) * g.heads + head) * g.head, acc, half, g.head, g.scale);
+  else
+    store_column<T, DB>(dq + token * g.dq_stride, acc, half, g.head, g.scale);
 }
 
 // dk and dv: 128 keys of a key head, a lane has a key of its own; tiles of 32 queries and their do come through shared memory, head after
@@ -293,29 +300,40 @@ __global__ __launch_bounds__(kWaves * kWave, sizeof(T) == 2 && DB <= 4 ? 2 : 1) 
   store_column<T, DB>(dv + token * g.dv_stride, sum_v, half, g.head, 1.0f);
 }
 
-// The shares' sums, four values a thread.
+// The shares' sums, four values a thread, of `tokens` (those of a sequence) of `row_values` each.
+template <typename T>
+__device__ __forceinline__ void join(const float* shares, int split, int64_t apart, int64_t at, int row_values, T* to, int64_t stride) {
+  v4f_t v = {0, 0, 0, 0};
+  for (int p = 0; p < split; ++p) v += *reinterpret_cast<const v4f_t*>(shares + p * apart + at);
+  to += at / row_values * stride + at % row_values;
+  if constexpr (sizeof(T) == 4) *reinterpret_cast<v4f_t*>(to) = v;
+  else *reinterpret_cast<uint2*>(to) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+}
 template <typename T>
 __global__ __launch_bounds__(kBlock) void back_join_kernel(const BackArgs g) {
-  const int64_t whole = int64_t(g.k_tokens) * g.kv_heads * g.head, at = (int64_t(blockIdx.x) * kBlock + threadIdx.x) * 4;
   const int row_values = g.kv_heads * g.head;
-  if (at >= whole) return;
-  const int64_t token = at / row_values;
-  if (token >= rest_of(g.k_offsets, g.sequences, g.k_tokens)) return;
-#pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    v4f_t v = {0, 0, 0, 0};
-    for (int p = 0; p < g.split; ++p) v += *reinterpret_cast<const v4f_t*>(g.shares + (2 * p + which) * whole + at);
-    T* const to = which ? static_cast<T*>(g.dv) + token * g.dv_stride + at % row_values : static_cast<T*>(g.dk) + token * g.dk_stride + at % row_values;
-    if constexpr (sizeof(T) == 4) *reinterpret_cast<v4f_t*>(to) = v;
-    else *reinterpret_cast<uint2*>(to) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
-  }
+  const int64_t whole = int64_t(g.k_tokens) * row_values, at = (int64_t(blockIdx.x) * kBlock + threadIdx.x) * 4;
+  if (at >= whole || at / row_values >= rest_of(g.k_offsets, g.sequences, g.k_tokens)) return;
+  join(g.shares, g.split, 2 * whole, at, row_values, static_cast<T*>(g.dk), g.dk_stride);
+  join(g.shares + whole, g.split, 2 * whole, at, row_values, static_cast<T*>(g.dv), g.dv_stride);
+}
+template <typename T>
+__global__ __launch_bounds__(kBlock) void back_join_queries_kernel(const BackArgs g) {
+  const int row_values = g.heads * g.head;
+  const int64_t whole = int64_t(g.q_tokens) * row_values, at = (int64_t(blockIdx.x) * kBlock + threadIdx.x) * 4;
+  if (at >= whole || at / row_values >= rest_of(g.q_offsets, g.sequences, g.q_tokens)) return;
+  join(g.q_shares, g.q_split, whole, at, row_values, static_cast<T*>(g.dq), g.dq_stride);
 }
 
 template <typename T, int DB>
 void launch_both(BackArgs g, int q_tiles, int k_tiles, hipStream_t s) {
   constexpr int kThreads = kWaves * kWave;
   if (q_tiles > 0) {
-    back_queries_kernel<T, DB><<<dim3(uint32_t(q_tiles) * g.heads), kThreads, 0, s>>>(g);
+    back_queries_kernel<T, DB><<<dim3(uint32_t(q_tiles) * g.heads * g.q_split), kThreads, 0, s>>>(g);
+    if (g.q_split > 1) {
+      const int64_t fours = int64_t(g.q_tokens) * g.heads * g.head / 4;
+      back_join_queries_kernel<T><<<dim3(uint32_t(blocks_of(fours, kBlock))), kBlock, 0, s>>>(g);
+    }
   }
   if (k_tiles > 0) {
     back_keys_kernel<T, DB><<<dim3(uint32_t(k_tiles) * g.kv_heads * g.split), kThreads, 0, s>>>(g);
@@ -350,6 +368,13 @@ AttentionBackPlan make_attention_back_plan(const accept_attention_desc& d) {
   while (p.split < kMost && groups * p.split < kEnough && queries >= 512 * p.split) p.split *= 2;
   p.bytes = p.stats;
   if (p.split > 1) p.bytes += size_t(up_to(8 * p.split * d.k_tokens * d.kv_heads * d.head_size, 256));
+  // The same for the queries' gradients and their keys, below one round of workgroups.  (One sequence of 4096 tokens, 4 heads, all gradients
+  // 181 us, and 122 so; a query over 8192 keys, 8 heads, 223 and 44.)
+  const int64_t q_groups = blocks_of(d.q_tokens, kRows) * d.heads, keys = d.sequences > 0 ? blocks_of(d.k_tokens, d.sequences) : 0;
+  p.q_split = 1;
+  while (p.q_split < kMost && q_groups * p.q_split * 2 <= kEnough / 2 && keys >= 1024 * p.q_split) p.q_split *= 2;
+  p.q_shares = p.bytes;
+  if (p.q_split > 1) p.bytes += size_t(up_to(4 * p.q_split * d.q_tokens * d.heads * d.head_size, 256));
   return p;
 }
 
@@ -363,6 +388,8 @@ hipError_t launch_attention_backward(const accept_attention_desc& d, const Atten
   g.stats = static_cast<float*>(ws);
   g.shares = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + p.stats);
   g.split = p.split;
+  g.q_shares = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + p.q_shares);
+  g.q_split = p.q_split;
   g.dq = dq, g.dk = dk, g.dv = dv;
   g.q_offsets = q_offsets, g.k_offsets = k_offsets;
   g.q_stride = stride(d.q_stride, whole), g.o_stride = stride(d.o_stride, whole), g.dq_stride = stride(d.dq_stride, whole);
