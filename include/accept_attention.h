@@ -71,7 +71,9 @@ accept_status accept_rotate(const accept_rotate_desc* desc, const void* x_dev, c
  *            the last key, and where there are more queries than keys the first ones see none.
  *  q_tokens, k_tokens, sequences  >= 0, below 2^31; tokens * stride <= 2^40.
  *  o_stride  of o and do;  dq_stride, dk_stride, dv_stride of the gradients.
- *  scale     of the products; finite, > 0.
+ *  scale     of the products, 2^-100 to 2^100.
+ *
+ * heads * (larger of q_tokens and k_tokens / 32 + 2 * sequences + 2) is at most 2^23 (else ACCEPT_ERR_UNSUPPORTED): a launch's workgroups.
  */
 typedef struct {
   int32_t dtype;
@@ -135,6 +137,9 @@ accept_status accept_attention_backward(const accept_attention_desc* desc, const
  *  tree_words  0: new token i of a sequence sees the cached ones and new tokens 0 .. i.  Otherwise it sees the cached ones
  *              and new token j where bit j % 64 of word tree_dev[token * tree_words + j / 64] is set (its own bit is no exception).  0 to 64.
  *  q_stride    of q (accept_cache_append: of its input);  qo_stride of its rotated output.  o_stride of o.
+ *  scale       as in accept_attention_desc.
+ *
+ * tokens * heads / 32 + kv_heads * (sequences + 1) is at most 2^23 (else ACCEPT_ERR_UNSUPPORTED).
  */
 typedef struct {
   int32_t dtype;

@@ -1,6 +1,4 @@
 // C ABI of the attention operators: argument validation and sizes, before anything is launched.
-#include <math.h>
-
 #include "attention.hpp"
 
 using namespace accept;
@@ -14,6 +12,8 @@ constexpr int64_t kMaxGroups = int64_t(1) << 23;  // workgroups of a launch: few
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 bool is_dtype(int32_t d) { return d == ACCEPT_F32 || d == ACCEPT_BF16; }
+// float32 holds it times log2(e), and what it multiplies by that: masked products are minus infinity, whose multiple by 0 would be NaN
+bool is_scale(double s) { return s >= 0x1p-100 && s <= 0x1p100; }
 bool is_flag(int32_t v) { return v == 0 || v == 1; }
 bool is_count(int64_t v) { return v >= 0 && v <= kMaxCount; }
 bool are_heads(int32_t heads, int32_t kv_heads, int32_t head_size) {
@@ -49,7 +49,7 @@ accept_status check_rotate(const accept_rotate_desc* d) {
 accept_status check_attention(const accept_attention_desc* d) {
   if (!d || !is_dtype(d->dtype) || !are_heads(d->heads, d->kv_heads, d->head_size) || !is_flag(d->causal) || !is_flag(d->rest))
     return ACCEPT_ERR_INVALID_ARG;
-  if (!is_count(d->sequences) || !is_count(d->q_tokens) || !is_count(d->k_tokens) || !isfinite(d->scale) || !(d->scale > 0))
+  if (!is_count(d->sequences) || !is_count(d->q_tokens) || !is_count(d->k_tokens) || !is_scale(d->scale))
     return ACCEPT_ERR_INVALID_ARG;
   for (const int64_t stride : {d->q_stride, d->o_stride, d->dq_stride})
     if (!are_tokens(d->q_tokens, d->heads, d->head_size, stride, d->dtype)) return ACCEPT_ERR_INVALID_ARG;
@@ -67,7 +67,7 @@ accept_status check_cache(const accept_cache_desc* d) {
     return ACCEPT_ERR_INVALID_ARG;
   if (d->page_size < 16 || d->page_size > 65536 || (d->page_size & (d->page_size - 1)) != 0) return ACCEPT_ERR_INVALID_ARG;
   if (!is_count(d->sequences) || !is_count(d->tokens) || !is_count(d->pages) || !is_count(d->table_pages) ||
-      d->table_pages * d->page_size > kMaxCount || !isfinite(d->scale) || !(d->scale > 0))
+      d->table_pages * d->page_size > kMaxCount || !is_scale(d->scale))
     return ACCEPT_ERR_INVALID_ARG;
   if (d->pages > kMaxElems / (int64_t(d->kv_heads) * d->page_size * d->head_size)) return ACCEPT_ERR_INVALID_ARG;
   for (const int64_t stride : {d->q_stride, d->o_stride, d->qo_stride})

@@ -44,7 +44,9 @@ __device__ __forceinline__ void clear_rest(T* to, int64_t stride, int head, int 
   }
 }
 
-// dq: 128 queries of a head, a lane has a query of its own as in the forward pass.
+// dq: 128 queries of a head, a lane has a query of its own as in the forward pass; the sums of do * o, which both kernels need, are made on the way.
+// Bound as the forward pass is, with three products of tiles for its two.  12288 tokens in 7 sequences, 32 heads on 8 of 128, bfloat16: 385 to
+// 400 us, 860 TFLOP/s of these products.
 template <typename T, int DB>
 __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) void back_queries_kernel(const BackArgs g) {
   constexpr int BN = 32 * (sizeof(T) == 2 && DB <= 4 ? 2 : 1);
@@ -159,7 +161,8 @@ __global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) 
 
 // dk and dv: 128 keys of a key head, a lane has a key of its own; tiles of 32 queries and their do come through shared memory, head after
 // head of those that share the key head.  Wide heads in bfloat16 leave their values in shared memory: with both gradients' sums and the
-// keys in registers there are two wavefronts a SIMD then, one of which multiplies while the other one exponentiates.
+// keys in registers there are two wavefronts a SIMD then, one of which multiplies while the other one exponentiates.  (12288 tokens in 7 sequences, 32
+// heads on 8 of 128, bfloat16: 505 to 528 us, four products of tiles at 870 TFLOP/s; with the values in registers and one wavefront a SIMD 875.)
 template <typename T, int DB>
 __global__ __launch_bounds__(kWaves * kWave, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void back_keys_kernel(const BackArgs g) {
   constexpr int BM = 32;

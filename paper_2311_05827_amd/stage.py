@@ -184,13 +184,23 @@ class NormLinear(torch.nn.Module):
 # ---- attention --------------------------------------------------------------------------------
 def _tokens(t):
     """(tokens, heads, head) of (batch, n, heads, head) or (tokens, heads, head), with a stride and an alignment that the operators take."""
-    t = t.reshape(-1, *t.shape[-2:])
+    if t.dim() not in (3, 4):
+        raise ValueError("%s is neither (batch, n, heads, head) nor (tokens, heads, head)" % (tuple(t.shape),))
+    t = t.flatten(0, -3)
     heads, head = t.shape[1:]
     if t.stride(2) == 1 and (heads == 1 or t.stride(1) == head) and heads * head <= t.stride(0) <= T.MAX_TOKEN_STRIDE:
         if t.stride(0) * t.element_size() % 16 == 0 and t.data_ptr() % 16 == 0:
             return t
     t = t.contiguous()
-    return t if t.data_ptr() % 16 == 0 else t.clone()
+    if t.data_ptr() % 16:
+        t = t.clone()
+    return t.as_strided(t.shape, (heads * head, head, 1))  # one token has any stride, and is contiguous
+
+
+def _same_batch(offsets, *tensors):
+    """Without offsets the tensors' sequences are those of one batch."""
+    if offsets is None and len({t.shape[0] if t.dim() == 4 else None for t in tensors}) > 1:
+        raise ValueError("batches of %s" % ", ".join(str(tuple(t.shape)) for t in tensors))
 
 
 def _sequences(x, offsets):
@@ -248,6 +258,7 @@ def attention(q, k, v, offsets=None, k_offsets=None, causal=True, scale=None):
     """q (batch, n, heads, head) over k and v (batch, m, kv_heads, head), or tokens of packed sequences (tokens, heads, head) with their
     offsets (sequences + 1 int32 device values; k_offsets None: q's).  float32 or bfloat16; heads / kv_heads query heads share a key head.
     With a causal mask a sequence's last query sees its last key.  Tokens behind the last sequence give and get zeros."""
+    _same_batch(offsets if k_offsets is None else k_offsets, q, k, v)
     return _Attention.apply(q, k, v, offsets, offsets if k_offsets is None else k_offsets, bool(causal), scale)
 
 
@@ -307,6 +318,9 @@ class Cache:
         accepted, so `advance` is no for trees if nothing is said."""
         if tree is not None and frequencies is not None and positions is None:
             raise ValueError("tokens of a tree need positions")
+        _same_batch(offsets, q, k, v)
+        if offsets is None and q.dim() == 4 and q.shape[0] != self.table.shape[0]:
+            raise ValueError("a batch of %d for %d sequences" % (q.shape[0], self.table.shape[0]))
         q, k, v = _tokens(q), _tokens(k), _tokens(v)
         n, heads, head = q.shape
         pages, kv, page_size, _ = self.k.shape
@@ -319,7 +333,7 @@ class Cache:
         q = out if turned else q
         o = T.accept_cache_attention(_cache_desc(*sizes, q_stride=q.stride(0), **kind), q, self.k, self.v, self.table, self.lengths, offsets, tree)
         if tree is None if advance is None else advance:
-            self.lengths += n // self.table.shape[0] if offsets is None else offsets[1:] - offsets[:-1]
+            self.lengths += n // max(self.table.shape[0], 1) if offsets is None else offsets[1:] - offsets[:-1]
         return o
 
 
@@ -356,6 +370,8 @@ class SelfAttention(torch.nn.Module):
         else:
             if torch.is_grad_enabled() and qkv.requires_grad:
                 raise ValueError("a cache holds no gradients: call it without them")
+            if offsets is None and x.dim() == 3 and x.shape[0] != cache.table.shape[0]:
+                raise ValueError("a batch of %d for %d sequences" % (x.shape[0], cache.table.shape[0]))
             q, k, v = qkv.split([self.heads, self.kv_heads, self.kv_heads], 1)
             o = cache.step(q, k, v, offsets, self.frequencies, positions, tree, self.pairs == T.ROTATE_NEIGHBOURS, advance=advance)
         return self.out(o.view(*x.shape[:-1], self.heads * self.head_size))

@@ -200,6 +200,33 @@ def test_tensors_on_the_host_are_refused(A):
         assert err.value.status == INVALID
 
 
+@pytest.mark.parametrize("scale", [2.0 ** -101, 1e-300, 2.0 ** 101, 1e300])
+def test_scales_that_float32_does_not_carry(A, lib, scale):
+    n = ctypes.c_size_t(7)
+    a, c = A.make_attention_desc(6, 6, 4, 2, 64, scale=scale), A.make_cache_desc(6, 3, 4, 2, 64, 16, 10, 4, scale=scale)
+    assert lib.accept_attention_workspace_size(ctypes.byref(a), ctypes.byref(n)) == INVALID
+    assert lib.accept_cache_workspace_size(ctypes.byref(c), ctypes.byref(n)) == INVALID and n.value == 7
+    a.scale, c.scale = 2.0 ** -100, 2.0 ** 100
+    assert lib.accept_attention_workspace_size(ctypes.byref(a), ctypes.byref(n)) == 0
+    assert lib.accept_cache_workspace_size(ctypes.byref(c), ctypes.byref(n)) == 0
+
+
+def test_shapes_that_a_stage_refuses(A):
+    """Each of these would otherwise be taken for something else: a head for a token, a batch for another one."""
+    import torch
+    x = torch.zeros
+    f = x(32)
+    for bad in (lambda: A.stage.rotate(x(6, 64), f), lambda: A.stage.rotate(x(1, 2, 3, 2, 64), f),
+                lambda: A.stage.attention(x(6, 64), x(6, 64), x(6, 64)),
+                lambda: A.stage.attention(x(2, 6, 2, 64), x(4, 6, 2, 64), x(4, 6, 2, 64)),
+                lambda: A.stage.attention(x(2, 6, 2, 64), x(12, 2, 64), x(12, 2, 64)),
+                lambda: A.stage.attention(x(2, 6, 2, 64), x(2, 6, 2, 64), x(3, 4, 2, 64)),
+                lambda: A.stage.Cache(4, 16, 2, 64, device="cpu", dtype=torch.float32).step(x(2, 2, 2, 64), x(2, 2, 2, 64), x(2, 2, 2, 64)),
+                lambda: A.stage.Cache(2, 16, 2, 64, device="cpu", dtype=torch.float32).step(x(2, 2, 2, 64), x(4, 2, 64), x(4, 2, 64))):
+        with pytest.raises(ValueError):
+            bad()
+
+
 def test_oracle_against_sums_by_hand():
     """Three keys, two queries, one channel."""
     q, k, v = np.array([[1.0], [2.0]]), np.array([[0.5], [-1.0], [3.0]]), np.array([[1.0], [10.0], [100.0]])

@@ -207,6 +207,43 @@ def test_two_passes_of_a_stage_captured(A):
         assert all(torch.equal(a, b) for a, b in zip(held, grads())), turn
 
 
+def test_one_token_of_any_stride(A):
+    """A single token's stride says nothing: 13 values here, which no operator takes."""
+    torch = torch_mod()
+    x = torch.randn(3, 2, 13, device="cuda")[:1, :, :8].transpose(0, 1)[1:2]   # (1, 1, 8), not whole vectors apart
+    y = torch.randn(5, 24, device="cuda")[2:3, None, :8]
+    f = frequencies(8)
+    for t in (x, y):
+        whole = t.clone(memory_format=torch.contiguous_format)
+        assert torch.equal(A.stage.rotate(t, f), A.stage.rotate(whole, f))
+        assert torch.equal(A.stage.attention(t, t, t), A.stage.attention(whole, whole, whole))
+        one, other = (A.stage.Cache(1, 16, 1, 8, 16, torch.float32) for _ in range(2))
+        assert torch.equal(one.step(t, t, t, frequencies=f), other.step(whole, whole, whole, frequencies=f))
+
+
+@pytest.mark.parametrize("shape", [(0, 2, 64), (0, 5, 2, 64), (3, 0, 2, 64)])
+def test_nothing_there(A, shape):
+    torch = torch_mod()
+    x = torch.zeros(shape, device="cuda", requires_grad=True)
+    y = A.stage.attention(*(A.stage.rotate(x, frequencies(64)) for _ in range(2)), x)
+    y.sum().backward()
+    assert y.shape == shape and x.grad.shape == shape
+    cache = A.stage.Cache(0, 16, 2, 64, 16, torch.float32)
+    assert cache.step(x[:0].detach(), x[:0].detach(), x[:0].detach()).numel() == 0
+
+
+def test_gradients_that_are_one_number(A):
+    """The gradient of a sum has no strides: it is taken as what it stands for."""
+    torch = torch_mod()
+    torch.manual_seed(4)
+    x = torch.randn(2, 9, 4, 64, device="cuda", requires_grad=True)
+    got = []
+    for of in (lambda y: y.sum(), lambda y: (y * torch.ones_like(y)).sum()):
+        y = A.stage.attention(A.stage.rotate(x, frequencies(32)), x[:, :, :2], x[:, :, 2:])
+        got.append(torch.autograd.grad(of(y), x)[0])
+    assert torch.equal(*got)
+
+
 def test_example(A):
     """It runs: losses, the gradient that goes back and all parameters' are finite, and served tokens are those of one pass over all."""
     torch = torch_mod()
