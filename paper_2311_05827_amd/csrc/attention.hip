@@ -38,10 +38,10 @@ constexpr float kBehind = 8.0f;
 // 12 heads of 64: 20 us, twice what its
 // tensors take to go through memory: a workgroup has 8 tiles at most, and its start and end are a good part.  Tried, and slower
 // at the first of these: 32 keys at a time with the next scores' products among the exponentials 1160 to 1208 us; 64 queries a wavefront, whose
-// registers leave one of them a SIMD, 1733; priority for the wavefront that multiplies 1130.  In float32 the products are 2 deep and
+// registers leave one of them a SIMD, 1733; priority for the wavefront that multiplies 1130; eight wavefronts in two halves that take turns at products and exponentials 1079 to 1116.  In float32 the products are 2 deep and
 // are the bound: 4096 tokens, 16 heads of 128, 664 us, 104 TFLOP/s of the 153 that the library's product reaches.
 template <typename T, int DB, bool SPLIT>
-__global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) void attention_kernel(const AttentionArgs g) {
+__global__ __launch_bounds__(kWaves * kWave, groups_a_unit(DB, sizeof(T))) void attention_kernel(const AttentionArgs g) {
   constexpr int NB = sizeof(T) == 2 ? 2 : 1, BN = 32 * NB;
   constexpr int kTile = BN * Head<T, DB>::kRowBytes;
   __shared__ __align__(kTileAlign) uint8_t tiles[4 * kTile];  // keys, values; and the next ones

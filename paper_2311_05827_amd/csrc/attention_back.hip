@@ -48,7 +48,7 @@ __device__ __forceinline__ void clear_rest(T* to, int64_t stride, int head, int 
 // Bound as the forward pass is, with three products of tiles for its two.  12288 tokens in 7 sequences, 32 heads on 8 of 128, bfloat16: 385 to
 // 400 us, 860 TFLOP/s of these products.
 template <typename T, int DB>
-__global__ __launch_bounds__(kWaves * kWave, DB <= 4 && sizeof(T) == 2 ? 2 : 1) void back_queries_kernel(const BackArgs g) {
+__global__ __launch_bounds__(kWaves * kWave, groups_a_unit(DB, sizeof(T))) void back_queries_kernel(const BackArgs g) {
   constexpr int BN = 32 * (sizeof(T) == 2 && DB <= 4 ? 2 : 1);
   constexpr int kTile = BN * Head<T, DB>::kRowBytes;
   __shared__ __align__(kTileAlign) uint8_t tiles[4 * kTile];
