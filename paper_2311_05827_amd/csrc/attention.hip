@@ -103,67 +103,69 @@ __global__ __launch_bounds__(kWaves * kWave, groups_a_unit(DB, sizeof(T))) void 
   const Reader<T, DB> lanes(lane);
   v16f_t acc[DB];
   float largest, sum;
-  // A second time where a result is not finite, with products that keep away from a row what it does not see: zero times an
-  // infinity or NaN of a hidden value would not.
-  const auto run = [&](auto apart) {
 #pragma unroll
-    for (int db = 0; db < DB; ++db) acc[db] = v16f_t{};
-    largest = -INFINITY;
-    sum = 0.0f;
-    if (step0 < steps) fetch(step0);
-    for (int step = step0; step < steps; ++step) {
-      __builtin_amdgcn_s_waitcnt(0);
-      __syncthreads();
-      if (step + 1 < steps) fetch(step + 1);
-      const int key0 = step * BN;
-      if (key0 >= wave_limit) continue;
-      const uint8_t* const kt = tiles + step % 2 * 2 * kTile;
-      const uint8_t* const vt = kt + kTile;
-      const Reader<T, DB> reader = lanes.fresh();
-      v16f_t s[NB];
-      float most = -INFINITY;
-      const bool masked = key0 + BN > first_limit;
+  for (int db = 0; db < DB; ++db) acc[db] = v16f_t{};
+  largest = -INFINITY;
+  sum = 0.0f;
+  if (step0 < steps) fetch(step0);
+  for (int step = step0; step < steps; ++step) {
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if (step + 1 < steps) fetch(step + 1);
+    const int key0 = step * BN;
+    if (key0 >= wave_limit) continue;
+    const uint8_t* const kt = tiles + step % 2 * 2 * kTile;
+    const uint8_t* const vt = kt + kTile;
+    const Reader<T, DB> reader = lanes.fresh();
+    v16f_t s[NB];
+    float most = -INFINITY;
+    const bool masked = key0 + BN > first_limit;
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        s[nb] = rows_product<T, DB>(lds_offset(kt), reader, nb * 32, q);
-        if (masked) {
-          const int left = limit() - key0 - nb * 32 - fresh_lane() / 32 * 4;
+    for (int nb = 0; nb < NB; ++nb) {
+      s[nb] = rows_product<T, DB>(lds_offset(kt), reader, nb * 32, q);
+      if (masked) {
+        const int left = limit() - key0 - nb * 32 - fresh_lane() / 32 * 4;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[nb][r] = result_row(r, 0) < left ? s[nb][r] : -INFINITY;
-        }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) most = fmaxf(most, s[nb][r]);
+        for (int r = 0; r < 16; ++r) s[nb][r] = result_row(r, 0) < left ? s[nb][r] : -INFINITY;
       }
-      most = halves_max(most) * g.scale;
-      if (__any(most > largest + kBehind)) {
-        const float now = fmaxf(largest, most);
-        const float factor = largest == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(largest - now);
-        largest = now;
-        sum *= factor;
 #pragma unroll
-        for (int db = 0; db < DB; ++db) acc[db] *= factor;
-      }
-      const float base = largest == -INFINITY ? 0.0f : -largest;
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        float p[16];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          p[r] = __builtin_amdgcn_exp2f(fmaf(s[nb][r], g.scale, base));
-          sum += p[r];
-        }
-        if (apart.value && masked) {
-          weighted_rows_apart<T, DB>(acc, vt, nb * 32, fresh_lane(), p, bits_between(0, limit() - key0 - nb * 32));
-        } else {
-          Weights<T> w;
-          set_weights(w, p);
-          weighted_rows<T, DB>(acc, lds_offset(vt), reader, nb * 32, w);
-        }
-      }
+      for (int r = 0; r < 16; ++r) most = fmaxf(most, s[nb][r]);
     }
-  };
-  run(Flag<false>{});
-  if (__syncthreads_or(is_row && !finite_column<DB>(acc))) run(Flag<true>{});
+    most = halves_max(most) * g.scale;
+    if (__any(most > largest + kBehind)) {
+      const float now = fmaxf(largest, most);
+      const float factor = largest == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(largest - now);
+      largest = now;
+      sum *= factor;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) acc[db] *= factor;
+    }
+    const float base = largest == -INFINITY ? 0.0f : -largest;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      float p[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        p[r] = __builtin_amdgcn_exp2f(fmaf(s[nb][r], g.scale, base));
+        sum += p[r];
+      }
+      Weights<T> w;
+      set_weights(w, p);
+      weighted_rows<T, DB>(acc, lds_offset(vt), reader, nb * 32, w);
+    }
+  }
+  for (uint32_t bad = columns_where(is_row && !finite_column<DB>(acc)); bad; bad &= bad - 1) {
+    const int c = __builtin_ctz(bad), sees = seen_by(row0 + c), stop = sees < steps * BN ? sees : steps * BN;
+    const T* const q_row = static_cast<const T*>(g.q) + (qs.begin + row0 + c) * g.q_stride + int64_t(head) * g.head;
+    const float base = of_lane(largest == -INFINITY ? 0.0f : -largest, c);
+    Lone<T, DB> lone;
+    for (int j0 = step0 * BN; j0 < stop; j0 += kWave) {
+      const bool is = j0 + lane < stop;
+      const float p = is ? __builtin_amdgcn_exp2f(fmaf(dot(q_row, k0 + (j0 + lane) * g.k_stride, g.head), g.scale, base)) : 0.0f;
+      lone.add(__ballot(is), p, g.head, [&](int t) { return v0 + (j0 + t) * g.v_stride; });
+    }
+    lone.put(acc, c);
+  }
   sum = halves_sum(sum);
   if (!is_row) return;
   const int64_t token = qs.begin + row;

@@ -48,11 +48,6 @@ hipError_t launch_cache_attention(const accept_cache_desc& d, const CachePlan& p
 
 __device__ __forceinline__ int pieces(int v, int of) { return (v + of - 1) / of; }
 
-template <bool B>
-struct Flag {
-  static constexpr bool value = B;
-};
-
 // A value that is the same for all lanes, in a scalar register, and with it what is computed from it.
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ int64_t uniform(int64_t v) {
@@ -318,7 +313,10 @@ __device__ __forceinline__ v16f_t rows_product(uint32_t tile, const Reader<T, DB
   v16f_t c = {};
   const uint32_t at = tile + reader.row;
 #pragma unroll
-  for (int i = 0; i < Head<T, DB>::kPairs; ++i) c = multiply_parts<T>(lds_load16((at ^ uint32_t(i << 5)) + n * Head<T, DB>::kRowBytes), b.p[i], c);
+  for (int i = 0; i < Head<T, DB>::kPairs; ++i) {
+    c = multiply_parts<T>(lds_load16((at ^ uint32_t(i << 5)) + n * Head<T, DB>::kRowBytes), b.p[i], c);
+    if (Head<T, DB>::kPairs >= 32 && i % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // no more loads ahead: they have no registers
+  }
   return c;
 }
 // The same with the other operand's 32 rows in shared memory too.
@@ -408,37 +406,10 @@ __device__ __forceinline__ void weighted_rows(v16f_t (&acc)[DB], uint32_t tile, 
         const float a = *reinterpret_cast<lds_float_t*>((at ^ flips ^ uint32_t(db << 7)) + (n + result_row(r, 0)) * ROWB);
         acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w.w[r], acc[db], 0, 0, 0);
       }
+      if (DB > 4) __builtin_amdgcn_sched_barrier(0);
     }
   }
 }
-// The same where not every column takes every row (bit i of `seen`: lane's column takes row row0 + i), and what it does not take may
-// be an infinity or NaN, which a product with zero would bring in: one row after the other, and none of it where it is not taken.
-template <typename T, int DB>
-__device__ __forceinline__ void weighted_rows_apart(v16f_t (&acc)[DB], const uint8_t* tile, int row0, int lane, const float (&w)[16],
-                                                 uint32_t seen) {
-  constexpr int ROWB = Head<T, DB>::kRowBytes;
-  const int half = lane / 32;
-#pragma unroll 1
-  for (int i = 0; i < 32; ++i) {
-    float mine = 0.0f;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) mine = result_row(r, half) == i ? w[r] : mine;
-    const float weight = __shfl(mine, lane % 32 + (i >> 2 & 1) * 32, kWave);
-    const bool taken = seen >> i & 1;
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int value = db * 32 + result_row(r, half);
-        const uint8_t* const p = tile + part_at<ROWB>(row0 + i, value * int(sizeof(T)) / 16) + value * int(sizeof(T)) % 16;
-        float x;
-        if constexpr (sizeof(T) == 4) x = *reinterpret_cast<const float*>(p);
-        else x = u32_as_f32(uint32_t(*reinterpret_cast<const uint16_t*>(p)) << 16);
-        acc[db][r] = taken ? fmaf(x, weight, acc[db][r]) : acc[db][r];
-      }
-  }
-}
-
 // The lane's column: values result_row of block db, as elements of T in a row, times `factor`.
 template <typename T, int DB>
 __device__ __forceinline__ void store_column(T* row, const v16f_t (&acc)[DB], int half, int head, float factor) {
@@ -474,6 +445,64 @@ __device__ __forceinline__ bool finite_column(const v16f_t (&acc)[DB]) {
     for (int r = 0; r < 16; ++r) zero = fmaf(acc[db][r], 0.0f, zero);
   return zero == 0.0f;
 }
+
+// Masked rows have weight zero, and zero times an infinity or NaN of theirs is NaN.  Columns whose sums are not all finite are therefore made again one by one,
+// by the whole wavefront, from the rows that they take and no others: a lane makes the weight of one of 64 rows, then has values lane, lane + 64, ... of
+// all of them.  (Columns with bit 1 in the mask: those for which `is` holds in either half.)
+__device__ __forceinline__ uint32_t columns_where(bool is) {
+  const uint64_t lanes = __ballot(is);
+  return uint32_t(lanes) | uint32_t(lanes >> 32);
+}
+__device__ __forceinline__ float of_lane(float v, int lane) { return u32_as_f32(uint32_t(__builtin_amdgcn_readlane(int(f32_as_u32(v)), lane))); }
+template <typename T>
+__device__ __forceinline__ float dot(const T* a, const T* b, int head) {
+  constexpr int VEC = 16 / int(sizeof(T));
+  float sum = 0.0f;
+#pragma unroll 1
+  for (int d = 0; d < head; d += VEC) {
+    float x[VEC], y[VEC];
+    load_vec(a + d, x);
+    load_vec(b + d, y);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) sum = fmaf(x[i], y[i], sum);
+  }
+  return sum;
+}
+template <typename T, int DB>
+struct Lone {
+  static constexpr int kValues = (DB + 1) / 2;
+  float x[kValues];
+  __device__ __forceinline__ Lone() {
+#pragma unroll
+    for (int i = 0; i < kValues; ++i) x[i] = 0.0f;
+  }
+  // of the lanes in `of`: their weight times their row
+  template <typename At>
+  __device__ __forceinline__ void add(uint64_t of, float weight, int head, const At& row_at) {
+    const int lane = fresh_lane();
+#pragma unroll 1
+    for (; of; of &= of - 1) {
+      const int t = __builtin_ctzll(of);
+      const float w = of_lane(weight, t);
+      const T* const row = row_at(t);
+#pragma unroll
+      for (int i = 0; i < kValues; ++i)
+        if (lane + i * kWave < head) x[i] = fmaf(w, load_one(row + lane + i * kWave), x[i]);
+    }
+  }
+  __device__ __forceinline__ void put(v16f_t (&acc)[DB], int column) const {
+    const int lane = fresh_lane();
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float v = __shfl(x[db / 2], db % 2 * 32 + result_row(r, lane / 32), kWave);
+        acc[db][r] = lane % 32 == column ? v : acc[db][r];
+      }
+      __builtin_amdgcn_sched_barrier(0);  // not all of them at once: they have no registers
+    }
+  }
+};
 
 // The two halves of a column (lanes l and l + 32): largest, sum.
 __device__ __forceinline__ float other_half(float v, bool second) {

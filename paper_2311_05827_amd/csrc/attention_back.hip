@@ -114,44 +114,52 @@ __global__ __launch_bounds__(kWaves * kWave, groups_a_unit(DB, sizeof(T))) void 
   }
   const Reader<T, DB> lanes(lane);
   v16f_t acc[DB];
-  const auto run = [&](auto apart) {  // (see attention_kernel)
 #pragma unroll
-    for (int db = 0; db < DB; ++db) acc[db] = v16f_t{};
-    if (step0 < steps) fetch(step0);
-    for (int step = step0; step < steps; ++step) {
-      __builtin_amdgcn_s_waitcnt(0);
-      __syncthreads();
-      if (step + 1 < steps) fetch(step + 1);
-      const int key0 = step * BN;
-      if (key0 >= wave_limit) continue;
-      const uint8_t* const kt = tiles + step % 2 * 2 * kTile;
-      const uint8_t* const vt = kt + kTile;
-      const Reader<T, DB> reader = lanes.fresh();
-      const bool masked = key0 + BN > first_limit;
+  for (int db = 0; db < DB; ++db) acc[db] = v16f_t{};
+  if (step0 < steps) fetch(step0);
+  for (int step = step0; step < steps; ++step) {
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if (step + 1 < steps) fetch(step + 1);
+    const int key0 = step * BN;
+    if (key0 >= wave_limit) continue;
+    const uint8_t* const kt = tiles + step % 2 * 2 * kTile;
+    const uint8_t* const vt = kt + kTile;
+    const Reader<T, DB> reader = lanes.fresh();
+    const bool masked = key0 + BN > first_limit;
 #pragma unroll
-      for (int n = 0; n < BN; n += 32) {
-        const v16f_t s = rows_product<T, DB>(lds_offset(kt), reader, n, q);
-        const v16f_t dp = rows_product<T, DB>(lds_offset(vt), reader, n, dout);
-        float ds[16];
+    for (int n = 0; n < BN; n += 32) {
+      const v16f_t s = rows_product<T, DB>(lds_offset(kt), reader, n, q);
+      const v16f_t dp = rows_product<T, DB>(lds_offset(vt), reader, n, dout);
+      float ds[16];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], g.scale2, -lse)) * (dp[r] - along);
-        if (masked) {
-          const int left = limit() - key0 - n - fresh_lane() / 32 * 4;
+      for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], g.scale2, -lse)) * (dp[r] - along);
+      if (masked) {
+        const int left = limit() - key0 - n - fresh_lane() / 32 * 4;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) ds[r] = result_row(r, 0) < left ? ds[r] : 0.0f;
-        }
-        if (apart.value && masked) {
-          weighted_rows_apart<T, DB>(acc, kt, n, fresh_lane(), ds, bits_between(0, limit() - key0 - n));
-        } else {
-          Weights<T> w;
-          set_weights(w, ds);
-          weighted_rows<T, DB>(acc, lds_offset(kt), reader, n, w);
-        }
+        for (int r = 0; r < 16; ++r) ds[r] = result_row(r, 0) < left ? ds[r] : 0.0f;
       }
+      Weights<T> w;
+      set_weights(w, ds);
+      weighted_rows<T, DB>(acc, lds_offset(kt), reader, n, w);
     }
-  };
-  run(Flag<false>{});
-  if (__syncthreads_or(is_row && !finite_column<DB>(acc))) run(Flag<true>{});
+  }
+  for (uint32_t bad = columns_where(is_row && !finite_column<DB>(acc)); bad; bad &= bad - 1) {  // (see Lone)
+    const int c = __builtin_ctz(bad), sees = seen_by(row0 + c), stop = sees < steps * BN ? sees : steps * BN;
+    const T* const q_row = static_cast<const T*>(g.q) + (qs.begin + row0 + c) * g.q_stride + int64_t(head) * g.head;
+    const T* const do_row = static_cast<const T*>(g.dout) + (qs.begin + row0 + c) * g.o_stride + int64_t(head) * g.head;
+    const float lse_c = of_lane(lse, c), along_c = of_lane(along, c);
+    Lone<T, DB> lone;
+    for (int j0 = step0 * BN; j0 < stop; j0 += kWave) {
+      const bool is = j0 + lane < stop;
+      float ds = 0.0f;
+      if (is)
+        ds = __builtin_amdgcn_exp2f(fmaf(dot(q_row, k0 + (j0 + lane) * g.k_stride, g.head), g.scale2, -lse_c)) *
+             (dot(do_row, v0 + (j0 + lane) * g.v_stride, g.head) - along_c);
+      lone.add(__ballot(is), ds, g.head, [&](int t) { return k0 + (j0 + t) * g.k_stride; });
+    }
+    lone.put(acc, c);
+  }
   if (!is_row) return;
   if (g.q_split > 1)
     store_column<float, DB>(g.q_shares + ((int64_t(share) * g.q_tokens + token) * g.heads + head) * g.head, acc, half, g.head, g.scale);
@@ -163,7 +171,8 @@ __global__ __launch_bounds__(kWaves * kWave, groups_a_unit(DB, sizeof(T))) void 
 // head of those that share the key head.  Wide heads in bfloat16 leave their values in shared memory: with both gradients' sums and the
 // keys in registers there are two wavefronts a SIMD then, one of which multiplies while the other one exponentiates.  (12288 tokens in 7 sequences, 32
 // heads on 8 of 128, bfloat16: 505 to 528 us, four products of tiles at 870 TFLOP/s; with the values in registers and one wavefront a SIMD 875.)
-template <typename T, int DB>
+// Heads of 256 have registers for one of the two gradients (K: dk, V: dv), and a launch for each.
+template <typename T, int DB, bool K, bool V>
 __global__ __launch_bounds__(kWaves * kWave, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void back_keys_kernel(const BackArgs g) {
   constexpr int BM = 32;
   constexpr int kTile = BM * Head<T, DB>::kRowBytes;
@@ -182,8 +191,8 @@ __global__ __launch_bounds__(kWaves * kWave, sizeof(T) == 2 && DB <= 4 ? 2 : 1) 
   if (piece.seq < 0) {
     if (g.zeros && share == 0) {
       const int rest = rest_of(g.k_offsets, g.sequences, g.k_tokens);
-      clear_rest(dk, g.dk_stride, g.head, rest, piece.tile, g.k_tokens);
-      clear_rest(dv, g.dv_stride, g.head, rest, piece.tile, g.k_tokens);
+      if constexpr (K) clear_rest(dk, g.dk_stride, g.head, rest, piece.tile, g.k_tokens);
+      if constexpr (V) clear_rest(dv, g.dv_stride, g.head, rest, piece.tile, g.k_tokens);
     }
     return;
   }
@@ -210,7 +219,7 @@ __global__ __launch_bounds__(kWaves * kWave, sizeof(T) == 2 && DB <= 4 ? 2 : 1) 
     const TileRows<T, DB, kRows, kWaves> v_rows(wave, g.v_stride, parts);
     v_rows.fetch(static_cast<const T*>(g.v) + (ks.begin + int64_t(piece.tile) * kRows) * g.v_stride + int64_t(head) * g.head,
                  keys - piece.tile * kRows, values);
-  } else {
+  } else if constexpr (K) {
     v.load(static_cast<const T*>(g.v) + token * g.v_stride + int64_t(head) * g.head, half, parts);
   }
   k.load(static_cast<const T*>(g.k) + token * g.k_stride + int64_t(head) * g.head, half, parts);
@@ -228,7 +237,7 @@ __global__ __launch_bounds__(kWaves * kWave, sizeof(T) == 2 && DB <= 4 ? 2 : 1) 
   };
   const Reader<T, DB> lanes(lane);
   v16f_t sum_k[DB], sum_v[DB];
-  const auto run = [&](auto apart) {  // (see attention_kernel)
+  const auto add_up = [&] {
 #pragma unroll
     for (int db = 0; db < DB; ++db) sum_k[db] = v16f_t{}, sum_v[db] = v16f_t{};
     if (step == step_end) return;
@@ -250,9 +259,9 @@ __global__ __launch_bounds__(kWaves * kWave, sizeof(T) == 2 && DB <= 4 ? 2 : 1) 
       const bool masked = row0 < wave_all || row0 + 32 > rows || key0 + 32 > keys;
       const Reader<T, DB> reader = lanes.fresh();
       const v16f_t s = rows_product<T, DB>(lds_offset(qt), reader, 0, k);
-      v16f_t dp;
+      v16f_t dp = {};
       if constexpr (kValuesInLds) dp = rows_product<T, DB>(lds_offset(ot), reader, lds_offset(values) + uint32_t(wave * 32 * Head<T, DB>::kRowBytes));
-      else dp = rows_product<T, DB>(lds_offset(ot), reader, 0, v);
+      else if constexpr (K) dp = rows_product<T, DB>(lds_offset(ot), reader, 0, v);
       float p[16], ds[16];
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
@@ -277,30 +286,48 @@ __global__ __launch_bounds__(kWaves * kWave, sizeof(T) == 2 && DB <= 4 ? 2 : 1) 
           ds[r] = sees ? ds[r] : 0.0f;
         }
       }
-      if (apart.value && masked) {
-        weighted_rows_apart<T, DB>(sum_v, ot, 0, fresh_lane(), p, seen);
-        weighted_rows_apart<T, DB>(sum_k, qt, 0, fresh_lane(), ds, seen);
-      } else {
-        Weights<T> wp, ws;
-        set_weights(wp, p);
-        set_weights(ws, ds);
-        weighted_rows<T, DB>(sum_v, lds_offset(ot), reader, 0, wp);
-        weighted_rows<T, DB>(sum_k, lds_offset(qt), reader, 0, ws);
-      }
+      Weights<T> wp, ws;
+      set_weights(wp, p);
+      set_weights(ws, ds);
+      if constexpr (V) weighted_rows<T, DB>(sum_v, lds_offset(ot), reader, 0, wp);
+      if constexpr (K) weighted_rows<T, DB>(sum_k, lds_offset(qt), reader, 0, ws);
     }
   };
-  run(Flag<false>{});
-  if (__syncthreads_or(is_key && !(finite_column<DB>(sum_k) && finite_column<DB>(sum_v)))) run(Flag<true>{});
+  add_up();
+  for (uint32_t bad = columns_where(is_key && !((!K || finite_column<DB>(sum_k)) && (!V || finite_column<DB>(sum_v)))); bad; bad &= bad - 1) {  // (see Lone)
+    const int c = __builtin_ctz(bad), from = seen_from(key0 + c);
+    const T* const k_row = static_cast<const T*>(g.k) + (ks.begin + key0 + c) * g.k_stride + int64_t(head) * g.head;
+    const T* const v_row = static_cast<const T*>(g.v) + (ks.begin + key0 + c) * g.v_stride + int64_t(head) * g.head;
+    Lone<T, DB> of_k, of_v;
+    for (int i = step; i < step_end; ++i) {
+      const int h = head * g.group + i / each, row = (first + each - 1 - i % each) * BM + lane;
+      const bool is = lane < BM && row >= from && row < rows;
+      const T* const q0 = static_cast<const T*>(g.q) + int64_t(h) * g.head;
+      const T* const o0 = static_cast<const T*>(g.dout) + int64_t(h) * g.head;
+      float p = 0.0f, ds = 0.0f;
+      if (is) {
+        const int64_t at = int64_t(qs.begin) + row;
+        p = __builtin_amdgcn_exp2f(fmaf(dot(k_row, q0 + at * g.q_stride, g.head), g.scale2, -g.stats[(int64_t(g.heads) + h) * g.q_tokens + at]));
+        ds = p * (dot(v_row, o0 + at * g.o_stride, g.head) - g.stats[int64_t(h) * g.q_tokens + at]);
+      }
+      const uint64_t of = __ballot(is);
+      const int64_t first_row = int64_t(qs.begin) + (first + each - 1 - i % each) * BM;
+      of_v.add(of, p, g.head, [&](int t) { return o0 + (first_row + t) * g.o_stride; });
+      of_k.add(of, ds, g.head, [&](int t) { return q0 + (first_row + t) * g.q_stride; });
+    }
+    if constexpr (K) of_k.put(sum_k, c);
+    if constexpr (V) of_v.put(sum_v, c);
+  }
   if (!is_key) return;
   if (g.split > 1) {
     const int64_t whole = int64_t(g.k_tokens) * g.kv_heads * g.head;
     float* const to = g.shares + 2 * share * whole + (token * g.kv_heads + head) * g.head;
-    store_column<float, DB>(to, sum_k, half, g.head, g.scale);
-    store_column<float, DB>(to + whole, sum_v, half, g.head, 1.0f);
+    if constexpr (K) store_column<float, DB>(to, sum_k, half, g.head, g.scale);
+    if constexpr (V) store_column<float, DB>(to + whole, sum_v, half, g.head, 1.0f);
     return;
   }
-  store_column<T, DB>(dk + token * g.dk_stride, sum_k, half, g.head, g.scale);
-  store_column<T, DB>(dv + token * g.dv_stride, sum_v, half, g.head, 1.0f);
+  if constexpr (K) store_column<T, DB>(dk + token * g.dk_stride, sum_k, half, g.head, g.scale);
+  if constexpr (V) store_column<T, DB>(dv + token * g.dv_stride, sum_v, half, g.head, 1.0f);
 }
 
 // The shares' sums, four values a thread, of `tokens` (those of a sequence) of `row_values` each.
@@ -339,7 +366,13 @@ void launch_both(BackArgs g, int q_tiles, int k_tiles, hipStream_t s) {
     }
   }
   if (k_tiles > 0) {
-    back_keys_kernel<T, DB><<<dim3(uint32_t(k_tiles) * g.kv_heads * g.split), kThreads, 0, s>>>(g);
+    const dim3 grid(uint32_t(k_tiles) * g.kv_heads * g.split);
+    if constexpr (DB == 8) {
+      back_keys_kernel<T, DB, true, false><<<grid, kThreads, 0, s>>>(g);
+      back_keys_kernel<T, DB, false, true><<<grid, kThreads, 0, s>>>(g);
+    } else {
+      back_keys_kernel<T, DB, true, true><<<grid, kThreads, 0, s>>>(g);
+    }
     if (g.split > 1) {
       const int64_t fours = int64_t(g.k_tokens) * g.kv_heads * g.head / 4;
       back_join_kernel<T><<<dim3(uint32_t(blocks_of(fours, kBlock))), kBlock, 0, s>>>(g);

@@ -231,13 +231,11 @@ struct Rows {
     sum = 0.0f;
   }
   // seen: for columns that do not see all of the tile (then `masked`)
-  template <typename Apart, typename Seen>
-  __device__ __forceinline__ void take(const uint8_t* kt, const uint8_t* vt, const Reader<T, DB>& reader, float scale, bool masked, const Seen& seen_of, Apart) {
+  template <typename Seen>
+  __device__ __forceinline__ void take(const uint8_t* kt, const uint8_t* vt, const Reader<T, DB>& reader, float scale, bool masked, const Seen& seen_of) {
     v16f_t s = rows_product<T, DB>(lds_offset(kt), reader, 0, q);
-    uint32_t seen = ~0u;
     if (masked) {
-      seen = seen_of();
-      const uint32_t here = seen >> (fresh_lane() / 32 * 4);
+      const uint32_t here = seen_of() >> (fresh_lane() / 32 * 4);
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = here >> result_row(r, 0) & 1 ? s[r] : -INFINITY;
     }
@@ -260,12 +258,29 @@ struct Rows {
       p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale, base));
       sum += p[r];
     }
-    if (Apart::value && masked) {
-      weighted_rows_apart<T, DB>(acc, vt, 0, fresh_lane(), p, seen);
-    } else {
-      Weights<T> w;
-      set_weights(w, p);
-      weighted_rows<T, DB>(acc, lds_offset(vt), reader, 0, w);
+    Weights<T> w;
+    set_weights(w, p);
+    weighted_rows<T, DB>(acc, lds_offset(vt), reader, 0, w);
+  }
+  // Columns that came out not finite by themselves (see Lone): rows row_of(c), over 32 places from `key` on, `by` apart, below `stop`.
+  template <typename RowOf>
+  __device__ __forceinline__ void mend(const CacheArgs& g, const Step& st, int seq, int kv, uint32_t bad, const RowOf& row_of, int key, int by, int stop) {
+    const int lane = fresh_lane();
+    const int32_t* const table = g.table + int64_t(seq) * g.pages.table_pages;
+    for (; bad; bad &= bad - 1) {
+      const int c = __builtin_ctz(bad), row = row_of(c), of_step = row / g.group, token = st.span.begin + of_step;
+      const T* const q_row = static_cast<const T*>(g.q) + token * g.q_stride + int64_t(kv * g.group + row % g.group) * g.head;
+      const float base = of_lane(largest == -INFINITY ? 0.0f : -largest, c);
+      Lone<T, DB> lone;
+      for (int key0 = key; key0 < stop; key0 += by) {
+        const int j = key0 + lane % 32;
+        const int page = table[(j < st.keys ? j : st.keys - 1) >> g.pages.shift];
+        const bool is = lane < 32 && (seen_among(g, st, of_step, token, key0) >> lane & 1) && is_page(g.pages, page);
+        const int64_t at = is ? cache_row(g.pages, page, j, kv) * g.head : 0;
+        const float p = is ? __builtin_amdgcn_exp2f(fmaf(dot(q_row, static_cast<const T*>(g.k) + at, g.head), g.scale, base)) : 0.0f;
+        lone.add(__ballot(is), p, g.head, [&](int t) { return static_cast<const T*>(g.v) + __shfl(at, t, kWave); });
+      }
+      lone.put(acc, c);
     }
   }
 };
@@ -279,14 +294,13 @@ __global__ __launch_bounds__((KeysShape<T, DB>::kThreads), 1) void cached_keys_k
   constexpr int kItem = S::kItem, kWidth = DB * 32, kPad = kItem + 1;
   __shared__ __align__(kTileAlign) uint8_t tiles[S::kWaves][4 * S::kTile];
   __shared__ float peak[S::kWaves][kItem], total[S::kWaves][kItem];
-  const int lane = threadIdx.x % kWave, wave = uniform(int(threadIdx.x / kWave));
-  const int half = lane / 32, column = lane % 32;
+  const int wave = uniform(int(threadIdx.x / kWave));
   const int kv = blockIdx.y, part = blockIdx.x;
   uint8_t* const mine = tiles[wave];
   const auto clear_mine = [&] {
-    for (int i = lane * 16; i < 4 * S::kTile; i += kWave * 16) *reinterpret_cast<uint4*>(mine + i) = make_uint4(0, 0, 0, 0);
+    for (int i = fresh_lane() * 16; i < 4 * S::kTile; i += kWave * 16) *reinterpret_cast<uint4*>(mine + i) = make_uint4(0, 0, 0, 0);
   };
-  const Reader<T, DB> lanes(lane);
+  const Reader<T, DB> lanes(fresh_lane());
   Rows<T, DB> rows;
   Walk walk = begin_walk<S>(g, part);
   Stretch now;
@@ -296,35 +310,39 @@ __global__ __launch_bounds__((KeysShape<T, DB>::kThreads), 1) void cached_keys_k
     // (rows of a sequence: fewer than 2^28, see the check of the descriptor)
     const int row0 = int(now.item) * kItem, left = st.span.size() * g.group - row0;
     const int count = left < kItem ? left : kItem;
-    const int row = row0 + (column < count ? column : count - 1);
-    const int of_step = row / g.group, token = st.span.begin + of_step, head = kv * g.group + row % g.group;
+    const auto row_of = [&](int c) { return row0 + (c < count ? c : count - 1); };
     const Sight sight = sight_of(g, st, row0, count);
-    rows.q.load(static_cast<const T*>(g.q) + token * g.q_stride + int64_t(head) * g.head, half, g.head * int(sizeof(T)) / 16);
+    {
+      const int row = row_of(fresh_lane() % 32), token = st.span.begin + row / g.group, head = kv * g.group + row % g.group;
+      rows.q.load(static_cast<const T*>(g.q) + token * g.q_stride + int64_t(head) * g.head, fresh_lane() / 32, g.head * int(sizeof(T)) / 16);
+    }
     const int stop = sight.some < now.unit1 * S::kUnit ? sight.some : now.unit1 * S::kUnit;
-    const auto run = [&](auto apart) {
-      rows.clear();
-      Window window(g, st, walk.seq);
-      const auto fetch = [&](int key0, int b) {
-        const uint32_t to = lds_offset(mine) + uint32_t(b) * 2u * S::kTile;
-        return fetch_places<T, DB, 1, true>(g, st, pages_of(g, st, window, key0), kv, key0, 0, to, to + S::kTile);
-      };
-      int key0 = now.unit0 * S::kUnit + wave * 32, b = 0;
-      uint32_t there = 0;
-      if (key0 < stop) there = fetch(key0, 0);
-      for (; key0 < stop; key0 += S::kUnit, b ^= 1) {
-        wait_for_loads<0>();
-        const uint32_t now_there = there;
-        if (key0 + S::kUnit < stop) there = fetch(key0 + S::kUnit, b ^ 1);
-        const uint8_t* const kt = mine + b * 2 * S::kTile;
-        rows.take(kt, kt + S::kTile, lanes.fresh(), g.scale, key0 + 32 > sight.all || now_there != ~0u,
-                  [&] { return seen_among(g, st, of_step, token, key0) & now_there; }, apart);
-      }
+    rows.clear();
+    Window window(g, st, walk.seq);
+    const auto fetch = [&](int key0, int b) {
+      const uint32_t to = lds_offset(mine) + uint32_t(b) * 2u * S::kTile;
+      return fetch_places<T, DB, 1, true>(g, st, pages_of(g, st, window, key0), kv, key0, 0, to, to + S::kTile);
     };
-    run(Flag<false>{});
-    if (__any(column < count && !finite_column<DB>(rows.acc))) run(Flag<true>{});
+    int key0 = now.unit0 * S::kUnit + wave * 32, b = 0;
+    uint32_t there = 0;
+    if (key0 < stop) there = fetch(key0, 0);
+    for (; key0 < stop; key0 += S::kUnit, b ^= 1) {
+      wait_for_loads<0>();
+      const uint32_t now_there = there;
+      if (key0 + S::kUnit < stop) there = fetch(key0 + S::kUnit, b ^ 1);
+      const uint8_t* const kt = mine + b * 2 * S::kTile;
+      rows.take(kt, kt + S::kTile, lanes.fresh(), g.scale, key0 + 32 > sight.all || now_there != ~0u,
+                [&] {
+                const int of_step = row_of(fresh_lane() % 32) / g.group;
+                return seen_among(g, st, of_step, st.span.begin + of_step, key0) & now_there;
+              });
+    }
+    rows.mend(g, st, walk.seq, kv, columns_where(fresh_lane() % 32 < count && !finite_column<DB>(rows.acc)), row_of,
+              now.unit0 * S::kUnit + wave * 32, S::kUnit, stop);
     const float sum = halves_sum(rows.sum);
 
-    // the wavefronts' results together, relative to the largest of their maxima
+    // the wavefronts' results together, relative to the largest of their maxima (lanes anew: nothing of theirs is kept over the keys)
+    const int half = fresh_lane() / 32, column = fresh_lane() % 32;
     if (half == 0) peak[wave][column] = rows.largest;
     __syncthreads();
     float top = -INFINITY;
@@ -377,10 +395,9 @@ __global__ __launch_bounds__((RowsShape<T, DB>::kThreads), 1) void cached_rows_k
   using S = RowsShape<T, DB>;
   constexpr int kItem = S::kItem, kWidth = DB * 32, kRing = S::kRing;
   __shared__ __align__(kTileAlign) uint8_t tiles[2 * kRing * S::kTile];
-  const int lane = threadIdx.x % kWave, wave = uniform(int(threadIdx.x / kWave));
-  const int half = lane / 32, column = lane % 32;
+  const int wave = uniform(int(threadIdx.x / kWave));
   const int kv = blockIdx.y, part = blockIdx.x;
-  const Reader<T, DB> lanes(lane);
+  const Reader<T, DB> lanes(fresh_lane());
   Rows<T, DB> rows;
   Walk walk = begin_walk<S>(g, part);
   Stretch now;
@@ -395,51 +412,50 @@ __global__ __launch_bounds__((RowsShape<T, DB>::kThreads), 1) void cached_rows_k
     const int item_rows = st.span.size() * g.group - item0, item_count = item_rows < kItem ? item_rows : kItem;
     // (a wavefront without rows of its own takes part with the item's last one)
     const auto row_of = [&](int c) { return count > 0 ? row0 + (c < count ? c : count - 1) : item0 + item_count - 1; };
-    const int row = row_of(column);
-    const int token = st.span.begin + row / g.group, head = kv * g.group + row % g.group;
     const Sight of_item = sight_of(g, st, item0, item_count);
     const Sight sight = count > 0 ? sight_of(g, st, row0, count) : Sight{0, 0};
-    rows.q.load(static_cast<const T*>(g.q) + token * g.q_stride + int64_t(head) * g.head, half, g.head * int(sizeof(T)) / 16);
+    {
+      const int row = row_of(fresh_lane() % 32), token = st.span.begin + row / g.group, head = kv * g.group + row % g.group;
+      rows.q.load(static_cast<const T*>(g.q) + token * g.q_stride + int64_t(head) * g.head, fresh_lane() / 32, g.head * int(sizeof(T)) / 16);
+    }
     const int begin = now.unit0 * S::kUnit, stop = of_item.some < now.unit1 * S::kUnit ? of_item.some : now.unit1 * S::kUnit;
     const int steps = begin < stop ? pieces(stop - begin, 32) : 0;
     constexpr int kLoads = 2 * ((32 * Head<T, DB>::kRowBytes / 1024 + S::kWaves - 1) / S::kWaves);  // of a wavefront and step
-    const auto run = [&](auto apart) {
-      rows.clear();
-      uint32_t there[kRing];
-      Window window(g, st, walk.seq);
-      const auto fetch = [&](int step, uint32_t& exists) {
-        exists = 0;
-        if (step >= steps) return;
-        const uint32_t to = lds_offset(tiles) + uint32_t(step % kRing) * 2u * S::kTile;
-        const int key0 = begin + step * 32;
-        exists = fetch_places<T, DB, S::kWaves, false>(g, st, pages_of(g, st, window, key0), kv, key0, wave, to, to + S::kTile);
-      };
-#pragma unroll
-      for (int i = 0; i < kRing - 1; ++i) fetch(i, there[i]);
-      for (int step = 0; step < steps; ++step) {
-        if (step + kRing - 1 <= steps) wait_for_loads<(kRing - 2) * kLoads>();
-        else wait_for_loads<0>();
-        __syncthreads();
-        fetch(step + kRing - 1, there[kRing - 1]);
-        const int key0 = begin + step * 32;
-        const uint32_t now_there = there[0];
-#pragma unroll
-        for (int i = 0; i + 1 < kRing; ++i) there[i] = there[i + 1];
-        if (key0 >= sight.some) continue;
-        const uint8_t* const kt = tiles + step % kRing * 2 * S::kTile;
-        rows.take(kt, kt + S::kTile, lanes.fresh(), g.scale, key0 + 32 > sight.all || now_there != ~0u,
-                  [&] {
-                    const int of_step = row_of(fresh_lane() % 32) / g.group;
-                    return seen_among(g, st, of_step, st.span.begin + of_step, key0) & now_there;
-                  },
-                  apart);
-      }
-      __syncthreads();  // the tiles are free for the next stretch
+    rows.clear();
+    uint32_t there[kRing];
+    Window window(g, st, walk.seq);
+    const auto fetch = [&](int step, uint32_t& exists) {
+      exists = 0;
+      if (step >= steps) return;
+      const uint32_t to = lds_offset(tiles) + uint32_t(step % kRing) * 2u * S::kTile;
+      const int key0 = begin + step * 32;
+      exists = fetch_places<T, DB, S::kWaves, false>(g, st, pages_of(g, st, window, key0), kv, key0, wave, to, to + S::kTile);
     };
-    run(Flag<false>{});
-    if (__syncthreads_or(column < count && !finite_column<DB>(rows.acc))) run(Flag<true>{});
+#pragma unroll
+    for (int i = 0; i < kRing - 1; ++i) fetch(i, there[i]);
+    for (int step = 0; step < steps; ++step) {
+      if (step + kRing - 1 <= steps) wait_for_loads<(kRing - 2) * kLoads>();
+      else wait_for_loads<0>();
+      __syncthreads();
+      fetch(step + kRing - 1, there[kRing - 1]);
+      const int key0 = begin + step * 32;
+      const uint32_t now_there = there[0];
+#pragma unroll
+      for (int i = 0; i + 1 < kRing; ++i) there[i] = there[i + 1];
+      if (key0 >= sight.some) continue;
+      const uint8_t* const kt = tiles + step % kRing * 2 * S::kTile;
+      rows.take(kt, kt + S::kTile, lanes.fresh(), g.scale, key0 + 32 > sight.all || now_there != ~0u,
+                [&] {
+                  const int of_step = row_of(fresh_lane() % 32) / g.group;
+                  return seen_among(g, st, of_step, st.span.begin + of_step, key0) & now_there;
+                });
+    }
+    __syncthreads();  // the tiles are free for the next stretch
+    rows.mend(g, st, walk.seq, kv, columns_where(fresh_lane() % 32 < count && !finite_column<DB>(rows.acc)), row_of, begin, 32, stop);
     const float sum = halves_sum(rows.sum);
+    const int half = fresh_lane() / 32, column = fresh_lane() % 32;  // (anew: nothing of theirs is kept over the keys)
     if (column >= count) continue;
+    const int row = row0 + column, token = st.span.begin + row / g.group, head = kv * g.group + row % g.group;
     const bool begins = now.unit0 == 0, ends = now.unit1 == st.units;
     if (begins && ends) {
       store_column<T, DB>(static_cast<T*>(g.o) + token * g.o_stride + int64_t(head) * g.head, rows.acc, half, g.head, sum == 0.0f ? 0.0f : 1.0f / sum);
