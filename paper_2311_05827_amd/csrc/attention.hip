@@ -35,10 +35,11 @@ constexpr float kBehind = 8.0f;
 // Bound by what a SIMD issues: for 64 keys its wavefronts have 32 products of 32 x 32 x 16 (heads of 128) and, beside them, 1024 exponentials with
 // scale, sum and rounding, and matrix and vector unit are busy 50 and 55 % of the time, one after the other more than side by side.  16384
 // tokens, 16 heads on 2 of 128 in bfloat16: 1.05 to 1.13 ms, 1050 TFLOP/s (the library's 8192^3 product: 1147); 8144 tokens in 16 sequences,
-// 12 heads of 64: 20 us, twice what its
+// 12 heads of 64: 19 us, twice what its
 // tensors take to go through memory: a workgroup has 8 tiles at most, and its start and end are a good part.  Tried, and slower
 // at the first of these: 32 keys at a time with the next scores' products among the exponentials 1160 to 1208 us; 64 queries a wavefront, whose
-// registers leave one of them a SIMD, 1733; priority for the wavefront that multiplies 1130; eight wavefronts in two halves that take turns at products and exponentials 1079 to 1116.  In float32 the products are 2 deep and
+// registers leave one of them a SIMD, 1733; priority for the wavefront that multiplies 1130; eight wavefronts in two halves that take turns at products and exponentials 1079 to 1116.  All of the keys' parts
+// asked for before the first product, instead of each before its own: 1095 us, 1072 so.  In float32 the products are 2 deep and
 // are the bound: 4096 tokens, 16 heads of 128, 664 us, 104 TFLOP/s of the 153 that the library's product reaches.
 template <typename T, int DB, bool SPLIT>
 __global__ __launch_bounds__(kWaves * kWave, groups_a_unit(DB, sizeof(T))) void attention_kernel(const AttentionArgs g) {
@@ -122,7 +123,14 @@ __global__ __launch_bounds__(kWaves * kWave, groups_a_unit(DB, sizeof(T))) void 
     const bool masked = key0 + BN > first_limit;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      s[nb] = rows_product<T, DB>(lds_offset(kt), reader, nb * 32, q);
+      if constexpr (sizeof(T) == 2 && DB <= 4) {  // all of the parts are asked for before the first product
+        RowParts<T, DB> parts_of_keys;
+        load_parts<T, DB>(parts_of_keys, lds_offset(kt), reader, nb * 32);
+        __builtin_amdgcn_sched_barrier(0);
+        s[nb] = rows_product<T, DB>(parts_of_keys, q);
+      } else {
+        s[nb] = rows_product<T, DB>(lds_offset(kt), reader, nb * 32, q);
+      }
       if (masked) {
         const int left = limit() - key0 - nb * 32 - fresh_lane() / 32 * 4;
 #pragma unroll

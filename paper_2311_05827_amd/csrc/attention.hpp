@@ -236,9 +236,8 @@ __device__ __forceinline__ v16f_t multiply_parts(uint4 a, uint4 b, v16f_t c) {
   }
 }
 
-// Workgroups of four wavefronts that a compute unit has room for, where a wavefront goes over keys for its queries: registers allow three of heads up to 64
-// (4096 tokens, 32 heads of 64, forward: two 117 us, three 97; 16 x 509 tokens, 12 heads of 64: 21.8 and 20.0, dq 28.4 and 25.6) and two of those up to
-// 128 (three, with tiles of 32 keys: 1100 us for 1053).  Where keys' gradients are summed three spill (37 us, 57).
+// Workgroups of four wavefronts that a compute unit has to have room for, where a wavefront goes over keys for its queries: two of heads up to 128, whose sums,
+// queries and scores take 199 registers; three of those up to 64 (114 registers, so four; 4096 tokens, 32 heads of 64, forward: two 117 us, more 100).
 constexpr int groups_a_unit(int blocks, int bytes) { return bytes == 4 || blocks > 4 ? 1 : blocks <= 2 ? 3 : 2; }
 
 // DB blocks of 32 values of a head (the last ones zeros where head_size is less).

@@ -170,7 +170,8 @@ __global__ __launch_bounds__(kWaves * kWave, groups_a_unit(DB, sizeof(T))) void 
 // dk and dv: 128 keys of a key head, a lane has a key of its own; tiles of 32 queries and their do come through shared memory, head after
 // head of those that share the key head.  Wide heads in bfloat16 leave their values in shared memory: with both gradients' sums and the
 // keys in registers there are two wavefronts a SIMD then, one of which multiplies while the other one exponentiates.  (12288 tokens in 7 sequences, 32
-// heads on 8 of 128, bfloat16: 505 to 528 us, four products of tiles at 870 TFLOP/s; with the values in registers and one wavefront a SIMD 875.)
+// heads on 8 of 128, bfloat16: 495 to 560 us, four products of tiles at 800 to 900 TFLOP/s; with the values in registers and one wavefront a SIMD
+// 875.  All of a tile's parts asked for before its first product, instead of each before its own: all gradients 993 us, 972 so.)
 // Heads of 256 have registers for one of the two gradients (K: dk, V: dv), and a launch for each.
 template <typename T, int DB, bool K, bool V>
 __global__ __launch_bounds__(kWaves * kWave, sizeof(T) == 2 && DB <= 4 ? 2 : 1) void back_keys_kernel(const BackArgs g) {
@@ -258,7 +259,15 @@ __global__ __launch_bounds__(kWaves * kWave, sizeof(T) == 2 && DB <= 4 ? 2 : 1) 
       if (row0 + 31 < wave_from || key0 >= keys) continue;
       const bool masked = row0 < wave_all || row0 + 32 > rows || key0 + 32 > keys;
       const Reader<T, DB> reader = lanes.fresh();
-      const v16f_t s = rows_product<T, DB>(lds_offset(qt), reader, 0, k);
+      v16f_t s;
+      if constexpr (sizeof(T) == 2 && DB <= 4) {  // all of a tile's parts are asked for before the first product
+        RowParts<T, DB> a;
+        load_parts<T, DB>(a, lds_offset(qt), reader, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        s = rows_product<T, DB>(a, k);
+      } else {
+        s = rows_product<T, DB>(lds_offset(qt), reader, 0, k);
+      }
       v16f_t dp = {};
       if constexpr (kValuesInLds) dp = rows_product<T, DB>(lds_offset(ot), reader, lds_offset(values) + uint32_t(wave * 32 * Head<T, DB>::kRowBytes));
       else if constexpr (K) dp = rows_product<T, DB>(lds_offset(ot), reader, 0, v);

@@ -388,7 +388,7 @@ __global__ __launch_bounds__((KeysShape<T, DB>::kThreads), 1) void cached_keys_k
   }
 }
 
-// Bound by products and exponentials as attention_kernel is: 55000 tokens in six sequences, trees of 40 with 4 query heads a key head, 115 us, of
+// Bound by products and exponentials as attention_kernel is: 55000 tokens in six sequences, trees of 40 with 4 query heads a key head, 105 us, of
 // which about 25 are not the walk over the keys: five of a workgroup's eight wavefronts have rows, so that one SIMD has those of two.
 template <typename T, int DB>
 __global__ __launch_bounds__((RowsShape<T, DB>::kThreads), 1) void cached_rows_kernel(const CacheArgs g) {
