@@ -197,6 +197,26 @@ def test_what_is_not_seen_has_no_effect(A, name, bad, causal):
         assert np.isfinite(dv[21:, 0]).all() and np.isfinite(np.delete(dq[:100], 20, axis=0)).all()
 
 
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("head", [16, 80, 128, 256])
+def test_what_is_not_seen_at_every_width(A, name, head):
+    """NaN in one value that a causal row's later keys hold, and in one row's do: results that the formula makes finite are, within their bounds."""
+    def spoil(values):
+        values["v"][100, 0, head - 3] = np.nan
+        values["do"][20, 0, head - 1] = np.nan
+    c = Case(A, 17, name, [140], [140], 2, 1, head, True, change=spoil)
+    c.forward()
+    grads = c.backward()
+    o, lse, seen = f64(c.o), f64(c.lse), c.seen(0)
+    for h in range(2):
+        check_forward(name, c.x["q"][:, h], c.x["k"][:, 0], c.x["v"][:, 0], seen, c.scale, o[:, h], lse[h])
+    heads = [(c.x["do"][:, h], c.x["q"][:, h], c.x["k"][:, 0], c.x["v"][:, 0], o[:, h], lse[h]) for h in range(2)]
+    dq, dk, dv = (f64(g) for g in grads)
+    check_gradients(name, heads, c.scale, seen, ([dq[:, h] for h in range(2)], dk[:, 0], dv[:, 0]), kinds=False)
+    assert np.isfinite(o[:100]).all() and np.isfinite(np.delete(o, head - 3, axis=2)).all() and not np.isfinite(o[100:, :, head - 3]).any()
+    assert np.isfinite(dv[21:, 0]).all() and np.isfinite(np.delete(dq[:100], 20, axis=0)).all()
+
+
 def test_rows_behind_the_last_sequence(A):
     """Left as they were in what the caller gives, zeros in what the call makes or where the descriptor says so."""
     torch = torch_mod()

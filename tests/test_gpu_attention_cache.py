@@ -249,6 +249,19 @@ def test_a_cache_that_holds_nan(A, name):
     c.check_attention()
 
 
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("head", [16, 80, 256])
+@pytest.mark.parametrize("new", [9, 40])   # wavefronts with keys of their own, and with keys that they share
+def test_a_cache_that_holds_nan_at_every_width(A, name, head, new):
+    c = Cache(A, 18, name, [300], [new], 2, 1, head, 16)
+    c.append()
+    p, at = orc.place(c.table[0], 16, 305)
+    c.v_cache[p, 0, at, head - 3] = float("nan")
+    o = f64(c.attend())
+    assert np.isfinite(o[:5]).all() and np.isnan(o[5:, :, head - 3]).all() and np.isfinite(np.delete(o, head - 3, axis=2)).all()
+    c.check_attention()
+
+
 def test_steps_of_a_server(A):
     """A prompt, then token after token: the same attention as over the whole sequence at once, to the bounds of both (the cache holds the
     same bfloat16 keys, so the scores agree; weights and results are rounded in two orders)."""
