@@ -138,7 +138,7 @@ __device__ __forceinline__ uint32_t seen_among(const CacheArgs& g, const Step& s
   const int64_t sees = int64_t(st.length) + of_step + 1;
   const int limit = g.tree_words ? st.keys : int(sees < st.keys ? sees : st.keys);
   uint32_t seen = bits_between(0, limit - key0);
-  if (g.tree_words && key0 + 32 > st.length) {
+  if (g.tree_words && st.length - key0 < 32) {
     const int first = key0 - st.length;  // the node that bit 0 is; below 0: cached
     const uint64_t* const words = g.tree + int64_t(token) * g.tree_words;
     const auto word = [&](int i) { return i < g.tree_words ? words[i] : 0; };
@@ -182,7 +182,7 @@ struct TwoPages {
   int page[2];
 };
 __device__ __forceinline__ TwoPages pages_of(const CacheArgs& g, const Step& st, Window& window, int key0) {
-  const int i = key0 >> g.pages.shift, j = (key0 + 16 < st.keys ? key0 + 16 : st.keys - 1) >> g.pages.shift;
+  const int i = key0 >> g.pages.shift, j = place_at(key0, 16, st.keys) >> g.pages.shift;
   if (j >= window.first + Window::kReach || i < window.first) window.load(i);
   return {window.at(i), window.at(j)};
 }
@@ -193,7 +193,7 @@ __device__ __forceinline__ uint32_t fetch_places(const CacheArgs& g, const Step&
   using H = Head<T, DB>;
   constexpr int kPer = 1024 / H::kRowBytes, kAll = 32 / kPer, kLoads = (kAll + WAVES - 1) / WAVES;
   const int row_bytes = g.head * int(sizeof(T)), parts = row_bytes / 16;
-  const auto place = [&](int half) { return key0 + 16 * half < st.keys ? key0 + 16 * half : st.keys - 1; };
+  const auto place = [&](int half) { return place_at(key0, 16 * half, st.keys); };
   uint32_t there = 0;
   int64_t first[2];
 #pragma unroll
@@ -208,7 +208,7 @@ __device__ __forceinline__ uint32_t fetch_places(const CacheArgs& g, const Step&
   for (int i = 0; i < kLoads; ++i) {
     const int load = WAVES == 1 ? i : (i * WAVES + wave) % kAll, row = load * kPer, h = row >= 16;
     const int r = row + lane / H::kRowParts, p = lane % H::kRowParts ^ turn<H::kRowBytes>(r);
-    const int j = key0 + r < st.keys ? key0 + r : st.keys - 1;
+    const int j = place_at(key0, r, st.keys);
     const uint32_t offset = uint32_t(j - place(h)) * uint32_t(row_bytes) + uint32_t(p) * 16u;
     if (p < parts) {
       load_tile_part<ONCE>(static_cast<const uint8_t*>(g.k) + first[h], offset, k_to + load * 1024);
@@ -272,9 +272,9 @@ struct Rows {
       const T* const q_row = static_cast<const T*>(g.q) + token * g.q_stride + int64_t(kv * g.group + row % g.group) * g.head;
       const float base = of_lane(largest == -INFINITY ? 0.0f : -largest, c);
       Lone<T, DB> lone;
-      for (int key0 = key; key0 < stop; key0 += by) {
-        const int j = key0 + lane % 32;
-        const int page = table[(j < st.keys ? j : st.keys - 1) >> g.pages.shift];
+      for (int ahead = stop - key; ahead > 0; ahead -= by) {
+        const int key0 = stop - ahead, j = place_at(key0, lane % 32, st.keys);
+        const int page = table[j >> g.pages.shift];
         const bool is = lane < 32 && (seen_among(g, st, of_step, token, key0) >> lane & 1) && is_page(g.pages, page);
         const int64_t at = is ? cache_row(g.pages, page, j, kv) * g.head : 0;
         const float p = is ? __builtin_amdgcn_exp2f(fmaf(dot(q_row, static_cast<const T*>(g.k) + at, g.head), g.scale, base)) : 0.0f;
@@ -316,22 +316,23 @@ __global__ __launch_bounds__((KeysShape<T, DB>::kThreads), 1) void cached_keys_k
       const int row = row_of(fresh_lane() % 32), token = st.span.begin + row / g.group, head = kv * g.group + row % g.group;
       rows.q.load(static_cast<const T*>(g.q) + token * g.q_stride + int64_t(head) * g.head, fresh_lane() / 32, g.head * int(sizeof(T)) / 16);
     }
-    const int stop = sight.some < now.unit1 * S::kUnit ? sight.some : now.unit1 * S::kUnit;
+    const int stop = units_end(now.unit1, S::kUnit, sight.some);
     rows.clear();
     Window window(g, st, walk.seq);
     const auto fetch = [&](int key0, int b) {
       const uint32_t to = lds_offset(mine) + uint32_t(b) * 2u * S::kTile;
       return fetch_places<T, DB, 1, true>(g, st, pages_of(g, st, window, key0), kv, key0, 0, to, to + S::kTile);
     };
-    int key0 = now.unit0 * S::kUnit + wave * 32, b = 0;
+    int ahead = stop - (now.unit0 * S::kUnit + wave * 32), b = 0;  // places in front of `stop`
     uint32_t there = 0;
-    if (key0 < stop) there = fetch(key0, 0);
-    for (; key0 < stop; key0 += S::kUnit, b ^= 1) {
+    if (ahead > 0) there = fetch(stop - ahead, 0);
+    for (; ahead > 0; ahead -= S::kUnit, b ^= 1) {
+      const int key0 = stop - ahead;
       wait_for_loads<0>();
       const uint32_t now_there = there;
-      if (key0 + S::kUnit < stop) there = fetch(key0 + S::kUnit, b ^ 1);
+      if (ahead > S::kUnit) there = fetch(key0 + S::kUnit, b ^ 1);
       const uint8_t* const kt = mine + b * 2 * S::kTile;
-      rows.take(kt, kt + S::kTile, lanes.fresh(), g.scale, key0 + 32 > sight.all || now_there != ~0u,
+      rows.take(kt, kt + S::kTile, lanes.fresh(), g.scale, sight.all - key0 < 32 || now_there != ~0u,
                 [&] {
                 const int of_step = row_of(fresh_lane() % 32) / g.group;
                 return seen_among(g, st, of_step, st.span.begin + of_step, key0) & now_there;
@@ -418,7 +419,7 @@ __global__ __launch_bounds__((RowsShape<T, DB>::kThreads), 1) void cached_rows_k
       const int row = row_of(fresh_lane() % 32), token = st.span.begin + row / g.group, head = kv * g.group + row % g.group;
       rows.q.load(static_cast<const T*>(g.q) + token * g.q_stride + int64_t(head) * g.head, fresh_lane() / 32, g.head * int(sizeof(T)) / 16);
     }
-    const int begin = now.unit0 * S::kUnit, stop = of_item.some < now.unit1 * S::kUnit ? of_item.some : now.unit1 * S::kUnit;
+    const int begin = now.unit0 * S::kUnit, stop = units_end(now.unit1, S::kUnit, of_item.some);
     const int steps = begin < stop ? pieces(stop - begin, 32) : 0;
     constexpr int kLoads = 2 * ((32 * Head<T, DB>::kRowBytes / 1024 + S::kWaves - 1) / S::kWaves);  // of a wavefront and step
     rows.clear();
@@ -444,7 +445,7 @@ __global__ __launch_bounds__((RowsShape<T, DB>::kThreads), 1) void cached_rows_k
       for (int i = 0; i + 1 < kRing; ++i) there[i] = there[i + 1];
       if (key0 >= sight.some) continue;
       const uint8_t* const kt = tiles + step % kRing * 2 * S::kTile;
-      rows.take(kt, kt + S::kTile, lanes.fresh(), g.scale, key0 + 32 > sight.all || now_there != ~0u,
+      rows.take(kt, kt + S::kTile, lanes.fresh(), g.scale, sight.all - key0 < 32 || now_there != ~0u,
                 [&] {
                   const int of_step = row_of(fresh_lane() % 32) / g.group;
                   return seen_among(g, st, of_step, st.span.begin + of_step, key0) & now_there;

@@ -24,5 +24,13 @@ ACCEPT_BOTH bool is_page(const Pages& p, int32_t page) { return page >= 0 && pag
 ACCEPT_BOTH int64_t cache_row(const Pages& p, int32_t page, int64_t j, int head) {
   return ((int64_t(page) * p.kv_heads + head) << p.shift) + (j & ((int64_t(1) << p.shift) - 1));
 }
+// Places are counted in 32 bits, and a table may have all but 16 of 2^31 of them: a sum of one with a tile's or a unit's size does not fit.
+// Place key0 + by, or the last one of `keys` where that is none (0 <= key0 < keys).
+ACCEPT_BOTH int32_t place_at(int32_t key0, int32_t by, int32_t keys) { return by < keys - key0 ? key0 + by : keys - 1; }
+// Where the places of units that end before unit `unit1`, `unit` places each, end among the first `some`.
+ACCEPT_BOTH int32_t units_end(int32_t unit1, int32_t unit, int32_t some) {
+  const int64_t end = int64_t(unit1) * unit;
+  return end < some ? int32_t(end) : some;
+}
 
 }  // namespace accept

@@ -61,6 +61,33 @@ int main() {
             assert row == (page * 3 + 2) * size + at and 0 <= row < count * 3 * size
 
 
+def test_places_up_to_the_last_that_32_bits_hold(tmp_path):
+    """The kernels' own arithmetic of places, compiled for the host with every overflow an error: tables of up to 2^31 - 16 places."""
+    source = tmp_path / "places.cpp"
+    source.write_text('''
+#include <cstdio>
+#include <initializer_list>
+#include "pages.hpp"
+int main() {
+  for (int keys : {1, 15, 16, 31, 32, 33, 2147483520, 2147483521, 2147483584, 2147483631, 2147483632})
+    for (int unit : {32, 64, 128}) {
+      const int units = int((keys + 0LL + unit - 1) / unit);
+      for (int unit1 : {1, units > 1 ? units - 1 : 1, units})
+        for (int some : {0, keys - 1, keys}) std::printf("end %d %d %d %d\\n", unit1, unit, some, accept::units_end(unit1, unit, some));
+      for (int by : {0, 1, 15, 16, 31}) for (int key0 : {0, (units - 1) * unit, (keys - 1) / 32 * 32}) std::printf("at %d %d %d %d\\n", key0, by, keys, accept::place_at(key0, by, keys));
+    }
+}
+''')
+    program = tmp_path / "places"
+    subprocess.run(["g++", "-std=c++17", "-Wall", "-Werror", "-fsanitize=undefined", "-fno-sanitize-recover=all", "-I", CSRC, str(source), "-o", str(program)],
+                   check=True)
+    lines = subprocess.run([str(program)], check=True, capture_output=True, text=True).stdout.splitlines()
+    assert len(lines) == 11 * 3 * (9 + 15)
+    for line in lines:
+        what, (a, b, c, got) = line.split()[0], map(int, line.split()[1:])
+        assert got == (min(a * b, c) if what == "end" else min(a + b, c - 1)), line
+
+
 BAD_ROTATE = [dict(tokens=-1), dict(heads=0), dict(heads=65536), dict(head_size=0), dict(head_size=12), dict(head_size=264), dict(rotated=-2),
               dict(rotated=3), dict(rotated=66), dict(dtype=2), dict(pairs=2), dict(inverse=2), dict(rest=3), dict(sequences=-1),
               dict(x_stride=120), dict(x_stride=130), dict(y_stride=126), dict(x_stride=(1 << 22) + 8), dict(tokens=1 << 31),

@@ -323,6 +323,32 @@ def test_a_long_cache(A):
         check_forward("bf16", f64(q)[:, h], k64, v64, np.ones((1, context + 1), bool), head ** -0.5, o[:, h])
 
 
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [1, 40])   # wavefronts with keys of their own, and with keys that they share
+def test_a_context_as_long_as_a_table_can_be(A, name, new):
+    """2^31 - 64 places, all but the last page's the same page of zeros, whose weights are e^-80 of the others': the last tokens are among what is
+    seen.  (2^31 e^-60 is below 2^-55: what the zeros add is far inside the bounds.)"""
+    torch = torch_mod()
+    head, page, width = 8, 64, (1 << 25) - 1
+    assert A.make_cache_desc(new, 1, 1, 1, head, page, 2, width).table_pages * page == (1 << 31) - 64
+    g = torch.Generator(device="cuda").manual_seed(19)
+    dtype = torch.float32 if name == "f32" else torch.bfloat16
+    k_cache = torch.zeros(2, 1, page, head, dtype=dtype, device="cuda")
+    v_cache = torch.ones_like(k_cache)
+    k_cache[1] = 10 + torch.randn(1, page, head, device="cuda", generator=g)
+    v_cache[1] = 5 + torch.randn(1, page, head, device="cuda", generator=g)
+    q, k, v = (torch.randn(new, 1, head, device="cuda", generator=g) for _ in range(3))
+    q, k, v = (1 + 0.1 * q).to(dtype), (10 + k).to(dtype), v.to(dtype)
+    table = torch.zeros(1, width, dtype=torch.int32, device="cuda")
+    table[0, -1] = 1
+    lengths = ints([width * page - new])
+    desc = A.make_cache_desc(new, 1, 1, 1, head, page, 2, width, dtype=A.F32 if name == "f32" else A.BF16, scale=1.0)
+    A.accept_cache_append(desc, None, k, v, k_cache, v_cache, table, lengths)
+    o = A.accept_cache_attention(desc, q, k_cache, v_cache, table, lengths)
+    assert torch.equal(k_cache[1, 0, -new:], k[:, 0]) and torch.equal(v_cache[1, 0, -new:], v[:, 0])
+    check_forward(name, f64(q)[:, 0], f64(k_cache)[1, 0], f64(v_cache)[1, 0], orc.causal(new, page), 1.0, f64(o)[:, 0])
+
+
 def test_captured_steps_that_share_a_workspace(A):
     """A graph of one step's append and attention, replayed while lengths and inputs change in place, beside a second graph with the same
     workspace: every replay is what the eager calls give."""
