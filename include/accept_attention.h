@@ -56,7 +56,7 @@ typedef struct {
 
 /*
  * Pair i of a token at position p: (a, b) becomes (a cos t - b sin t, a sin t + b cos t) with t = p * frequencies_dev[i]
- * (rotated / 2 floats; the product and its remainder by a full turn are taken in 64 bits, so far positions lose nothing),
+ * (rotated / 2 floats; the angle's remainder by a full turn is taken to 2^-100 of it, so far positions lose nothing),
  * rounded once.  positions_dev (tokens int32) null: a token's place in its sequence.  With positions offsets_dev is needed only to tell the
  * tokens of no sequence (null: there are none), and any number of sequences will do.  y_dev may be x_dev (with equal strides).
  */

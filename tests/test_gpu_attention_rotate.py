@@ -68,6 +68,31 @@ def test_far_positions(A, neighbours):
     check("f32", f64(y), values, positions, f64s, neighbours, False)
 
 
+@pytest.mark.parametrize("times", [1.0, 300.0, 1e6])
+def test_far_angles(A, times):
+    """The farthest positions, with frequencies from `times` / 2 to `times`: as near as near ones.  The oracle's angles come from whole numbers, by
+    1 / (2 pi) with 80 digits: 64 bits would lose the last ones that count."""
+    torch = torch_mod()
+    from fractions import Fraction
+    turn = Fraction(15915494309189533576888376337251436203445964574046, 10 ** 50)   # 1 / (2 pi)
+    rng = np.random.default_rng(5)
+    n, pairs = 64, 32
+    positions = (1 << 31) - 1 - rng.integers(0, 1 << 20, n)
+    f = (times * (1 + np.arange(pairs)) / (2 * pairs) + times / 2).astype(np.float32)
+    left = np.empty((n, pairs))
+    for i, p in enumerate(positions):
+        for j, freq in enumerate(f):
+            turns = int(p) * Fraction(float(freq)) * turn
+            left[i, j] = float(turns - round(turns)) * 2 * np.pi
+    x, values = tokens_of(rng.standard_normal((n, 2, 2 * pairs)), "f32")
+    y = A.accept_rotate(A.make_rotate_desc(n, 2, 2 * pairs, dtype=A.F32), x, torch.tensor(f, device="cuda"), positions=ints(positions))
+    a, b = values[..., :pairs], values[..., pairs:]
+    c, s = np.cos(left)[:, None], np.sin(left)[:, None]
+    want, terms = np.concatenate([a * c - b * s, a * s + b * c], -1), np.concatenate([np.abs(a) + np.abs(b)] * 2, -1)
+    bound = (4 + 3) * U * terms      # (see check)
+    assert np.all(np.abs(f64(y) - want) <= bound + rounding("f32", np.abs(want) + bound))
+
+
 @pytest.mark.parametrize("given", [False, True])
 def test_sequences_and_the_tokens_behind_them(A, given):
     torch = torch_mod()
