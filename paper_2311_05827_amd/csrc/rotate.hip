@@ -7,9 +7,9 @@ namespace {
 // cos and sin of a position's angle.  In turns, as sums of two numbers of 64 bits: the product and what its rounding left, times 1 / (2 pi) and what that one's
 // left.  The part of a turn that is left is then off by 2^-53, and by 2^-100 of the whole angle, so by nothing that 32 bits hold, which do from there.
 // (In 64 bits alone the angle was off by up to 2^-52 of itself: by 14 steps of 2^-24 at position 2^32 and frequency 1, more at higher ones.)
-__device__ __forceinline__ void turn_of(int position, float frequency, float* c, float* s) {
+__device__ __forceinline__ void turn_of(double position, float frequency, float* c, float* s) {
   constexpr double kTurn = 0x1.45f306dc9c883p-3, kTurnRest = -0x1.6b01ec5417056p-57;
-  const double angle = double(position) * double(frequency), angle_rest = fma(double(position), double(frequency), -angle);
+  const double angle = position * double(frequency), angle_rest = fma(position, double(frequency), -angle);
   const double whole = rint(angle * kTurn);
   const double turns = fma(angle, kTurn, -whole) + fma(angle, kTurnRest, angle_rest * kTurn);
   sincospif(float(2.0 * turns), s, c);
@@ -133,7 +133,8 @@ __global__ __launch_bounds__(kBlock) void rotate_kernel(const RotateArgs g) {
   const bool pair = item < g.pair_lanes;
   float c[N], s[N];
   if (pair && !outside) {
-    const int position = g.positions ? g.positions[token] : length + place;
+    // (a place may be one that 32 bits do not count: no key goes there, but its query turns)
+    const double position = g.positions ? double(g.positions[token]) : double(length) + double(place);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       turn_of(position, g.frequencies[item * N + i], &c[i], &s[i]);

@@ -1,4 +1,6 @@
 """The cache of pages, and attention over it, against the oracle in 64 bits."""
+from fractions import Fraction
+
 import numpy as np
 import pytest
 
@@ -168,6 +170,23 @@ def test_positions_are_those_given(A):
     k, _, _ = c.held(0)
     assert np.all(np.abs(k[20:] - want) <= (8 * 2 + 1) * U * np.abs(c.xk).max())
     assert np.all(np.abs(f64(q) - orc.rotate(c.xq, positions, f64(c.frequencies), False)) <= (8 * 2 + 1) * U * np.abs(c.xq).max())
+
+
+def test_queries_of_places_beyond_32_bits(A):
+    """A sequence of 2^31 - 2 tokens goes on: its new keys have no place, but their queries turn by where they would be."""
+    c = Cache(A, 20, "f32", [20], [5], 2, 1, 64, 16, rotated=64)
+    before = c.k_cache.clone()
+    c.lengths = ints([(1 << 31) - 2])
+    q = f64(c.append())
+    # what is left of a turn, from whole numbers: 64 bits would lose the last ones that count
+    f, positions = f64(c.frequencies), (1 << 31) - 2 + np.arange(5)
+    turn = Fraction(15915494309189533576888376337251436203445964574046, 10 ** 50)
+    left = np.array([[float(t - round(t)) for t in (int(p) * Fraction(float(x)) * turn for x in f)] for p in positions]) * 2 * np.pi
+    a, b = c.xq[..., :32], c.xq[..., 32:]
+    cos, sin = np.cos(left)[:, None], np.sin(left)[:, None]
+    want, terms = np.concatenate([a * cos - b * sin, a * sin + b * cos], -1), np.concatenate([np.abs(a) + np.abs(b)] * 2, -1)
+    assert np.all(np.abs(q - want) <= (4 + 3) * U * terms + U * (np.abs(want) + 7 * U * terms))
+    assert np.array_equal(f64(c.k_cache), f64(before), equal_nan=True)
 
 
 def test_in_place_and_without_queries(A):
