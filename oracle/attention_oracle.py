@@ -23,15 +23,16 @@ def causal(queries, keys):
 
 
 def attention(q, k, v, seen, scale):
-    """One head: (o, lse, p); rows that see nothing are zeros, their lse minus infinity.  What is not seen takes no part, whatever it is."""
+    """One head: (o, lse, p); rows that see nothing are zeros, their lse minus infinity; rows that see scores, but none above minus infinity, have NaN
+    for weights.  What is not seen takes no part, whatever it is."""
     with np.errstate(invalid="ignore", over="ignore"):
         s = np.where(seen, (q @ k.T) * scale, -np.inf)
     top = s.max(axis=1, initial=-np.inf, keepdims=True)
     e = np.where(seen, np.exp(s - np.where(np.isinf(top), 0, top)), 0.0)
     total = e.sum(axis=1, keepdims=True)
-    with np.errstate(divide="ignore"):
+    with np.errstate(divide="ignore", invalid="ignore"):
         lse = (np.log(total) + np.where(np.isinf(top), 0, top))[:, 0]
-    p = np.divide(e, total, out=np.zeros_like(e), where=total > 0)
+        p = np.where(seen, e / total, 0.0)
     return weighted(p, v, seen), lse, p
 
 
@@ -40,15 +41,16 @@ def weighted(w, x, seen):
     if np.isfinite(x).all():
         return w @ x
     out = np.zeros((w.shape[0], x.shape[1]))
-    for i in range(w.shape[0]):
-        out[i] = w[i, seen[i]] @ x[seen[i]]
+    with np.errstate(invalid="ignore"):
+        for i in range(w.shape[0]):
+            out[i] = w[i, seen[i]] @ x[seen[i]]
     return out
 
 
 def gradients(do, q, k, v, o, lse, seen, scale):
     """One head: (dq, dk, dv, p, ds) from the forward pass's outputs."""
     with np.errstate(invalid="ignore", over="ignore"):
-        p = np.where(seen, np.exp((q @ k.T) * scale - np.where(np.isfinite(lse), lse, 0)[:, None]), 0.0)
+        p = np.where(seen, np.exp((q @ k.T) * scale - lse[:, None]), 0.0)
         ds = np.where(seen, p * (do @ v.T - (do * o).sum(axis=1, keepdims=True)) * scale, 0.0)
     return weighted(ds, k, seen), weighted(ds.T, q, seen.T), weighted(p.T, do, seen.T), p, ds
 

@@ -176,19 +176,24 @@ __global__ __launch_bounds__(kWaves * kWave, groups_a_unit(DB, sizeof(T))) void 
   }
   sum = halves_sum(sum);
   if (!is_row) return;
+  // A row that sees keys, but no score above minus infinity, has no weights: minus infinity less itself.
+  const int sees = seen_by(row), stop = sees < steps * BN ? sees : steps * BN;
+  const bool lost = sum == 0.0f && stop > step0 * BN;
   const int64_t token = qs.begin + row;
   if constexpr (SPLIT) {
     float* const to = g.shares + ((int64_t(share) * g.heads + head) * g.q_tokens + token) * (DB * 32 + 2);
     store_pairs<DB>(to, acc, half);
-    if (half == 0) *reinterpret_cast<float2*>(to + DB * 32) = make_float2(largest, sum);
+    if (half == 0) *reinterpret_cast<float2*>(to + DB * 32) = make_float2(largest, lost ? 1.0f : sum);
     return;
   }
-  store_column<T, DB>(static_cast<T*>(g.o) + token * g.o_stride + int64_t(head) * g.head, acc, half, g.head, sum == 0.0f ? 0.0f : 1.0f / sum);
+  store_column<T, DB>(static_cast<T*>(g.o) + token * g.o_stride + int64_t(head) * g.head, acc, half, g.head,
+                      lost ? NAN : sum == 0.0f ? 0.0f : 1.0f / sum);
   if (g.lse && half == 0)
     g.lse[int64_t(head) * g.q_tokens + token] = sum == 0.0f ? -INFINITY : (largest + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-// A row's shares together, relative to the largest of their maxima: four values a thread.
+// A row's shares together, relative to the largest of their maxima: four values a thread.  (Maximum minus infinity and a sum: a share that sees keys, and
+// nothing above that.)
 template <typename T, int DB>
 __global__ __launch_bounds__(kBlock) void attention_join_kernel(const AttentionArgs g) {
   constexpr int kWidth = DB * 32, kFours = kWidth / 4;
@@ -203,14 +208,14 @@ __global__ __launch_bounds__(kBlock) void attention_join_kernel(const AttentionA
   for (int p = 0; p < g.split; ++p) top = fmaxf(top, from[p * apart + kWidth]);
   float v[4] = {0, 0, 0, 0}, sum = 0.0f;
   for (int p = 0; p < g.split; ++p) {
-    const float peak = from[p * apart + kWidth], factor = peak == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(peak - top);
+    const float peak = from[p * apart + kWidth], factor = peak == -INFINITY ? float(top == -INFINITY) : __builtin_amdgcn_exp2f(peak - top);
     sum = fmaf(factor, from[p * apart + kWidth + 1], sum);
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = fmaf(factor, from[p * apart + d + j], v[j]);
   }
   if (g.lse && d == 0) g.lse[row] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
   if (d >= g.head) return;
-  const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
+  const float inverse = sum == 0.0f ? 0.0f : top == -INFINITY ? NAN : 1.0f / sum;
   T* const to = static_cast<T*>(g.o) + token * g.o_stride + int64_t(head) * g.head + d;
   if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(to) = make_float4(v[0] * inverse, v[1] * inverse, v[2] * inverse, v[3] * inverse);
   else *reinterpret_cast<uint2*>(to) = make_uint2(bf16_pair(v[0] * inverse, v[1] * inverse), bf16_pair(v[2] * inverse, v[3] * inverse));

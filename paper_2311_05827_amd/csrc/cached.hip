@@ -262,6 +262,27 @@ struct Rows {
     set_weights(w, p);
     weighted_rows<T, DB>(acc, lds_offset(vt), reader, 0, w);
   }
+  // Both halves' sum of weights.  A row that sees keys (of those that `mend` names), but no score above minus infinity, has no weights, as it is minus infinity less
+  // itself: with a maximum of minus infinity its sum is 1, that of a row which sees nothing 0.
+  template <typename RowOf>
+  __device__ __forceinline__ float whole_sum(const CacheArgs& g, const Step& st, int seq, int count, const RowOf& row_of, int key, int by, int stop) const {
+    float whole = halves_sum(sum);
+    const int column = fresh_lane() % 32;
+    uint64_t unsure = __ballot(column < count && whole == 0.0f);
+    if (unsure) {
+      const int32_t* const table = g.table + int64_t(seq) * g.pages.table_pages;
+      const int of_step = row_of(column) / g.group;
+#pragma unroll 1
+      for (int ahead = stop - key; ahead > 0 && unsure; ahead -= by) {
+        const int key0 = stop - ahead;
+        const uint32_t there = (is_page(g.pages, uniform(table[key0 >> g.pages.shift])) ? 0xFFFFu : 0u) |
+                               (is_page(g.pages, uniform(table[place_at(key0, 16, st.keys) >> g.pages.shift])) ? 0xFFFF0000u : 0u);
+        if (whole == 0.0f && (seen_among(g, st, of_step, st.span.begin + of_step, key0) & there)) whole = 1.0f;
+        unsure &= __ballot(whole == 0.0f);
+      }
+    }
+    return whole;
+  }
   // Columns that came out not finite by themselves (see Lone): rows row_of(c), over 32 places from `key` on, `by` apart, below `stop`.
   template <typename RowOf>
   __device__ __forceinline__ void mend(const CacheArgs& g, const Step& st, int seq, int kv, uint32_t bad, const RowOf& row_of, int key, int by, int stop) {
@@ -340,7 +361,7 @@ __global__ __launch_bounds__((KeysShape<T, DB>::kThreads), 1) void cached_keys_k
     }
     rows.mend(g, st, walk.seq, kv, columns_where(fresh_lane() % 32 < count && !finite_column<DB>(rows.acc)), row_of,
               now.unit0 * S::kUnit + wave * 32, S::kUnit, stop);
-    const float sum = halves_sum(rows.sum);
+    const float sum = rows.whole_sum(g, st, walk.seq, count, row_of, now.unit0 * S::kUnit + wave * 32, S::kUnit, stop);
 
     // the wavefronts' results together, relative to the largest of their maxima (lanes anew: nothing of theirs is kept over the keys)
     const int half = fresh_lane() / 32, column = fresh_lane() % 32;
@@ -349,7 +370,7 @@ __global__ __launch_bounds__((KeysShape<T, DB>::kThreads), 1) void cached_keys_k
     float top = -INFINITY;
 #pragma unroll
     for (int w = 0; w < S::kWaves; ++w) top = fmaxf(top, peak[w][column]);
-    const float factor = rows.largest == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(rows.largest - top);
+    const float factor = rows.largest == -INFINITY ? float(top == -INFINITY) : __builtin_amdgcn_exp2f(rows.largest - top);
     if (half == 0) total[wave][column] = sum * factor;
     float* const out = reinterpret_cast<float*>(mine);
 #pragma unroll
@@ -362,23 +383,21 @@ __global__ __launch_bounds__((KeysShape<T, DB>::kThreads), 1) void cached_keys_k
     float* const slot = slot_at<S>(g, kv, part, begins, kWidth);
     for (int i = threadIdx.x; i < count * kWidth; i += S::kThreads) {
       const int r = i / kWidth, d = i % kWidth;
-      float v = 0.0f, l = 0.0f;
+      float v = 0.0f, l = 0.0f, top_r = -INFINITY;
 #pragma unroll
       for (int w = 0; w < S::kWaves; ++w) {
         v += reinterpret_cast<const float*>(tiles[w])[d * kPad + r];
         l += total[w][r];
+        top_r = fmaxf(top_r, peak[w][r]);
       }
       if (begins && ends) {
         const int flat = row0 + r;
         if (d < g.head)
           store_one(static_cast<T*>(g.o) + (st.span.begin + flat / g.group) * g.o_stride + (kv * g.group + flat % g.group) * g.head + d,
-                    l == 0.0f ? 0.0f : v / l);
+                    l == 0.0f ? 0.0f : top_r == -INFINITY ? NAN : v / l);
       } else {
         slot[r * kWidth + d] = v;
         if (d == 0) {
-          float top_r = -INFINITY;
-#pragma unroll
-          for (int w = 0; w < S::kWaves; ++w) top_r = fmaxf(top_r, peak[w][r]);
           slot[kItem * kWidth + r] = top_r;
           slot[kItem * kWidth + kItem + r] = l;
         }
@@ -453,13 +472,14 @@ __global__ __launch_bounds__((RowsShape<T, DB>::kThreads), 1) void cached_rows_k
     }
     __syncthreads();  // the tiles are free for the next stretch
     rows.mend(g, st, walk.seq, kv, columns_where(fresh_lane() % 32 < count && !finite_column<DB>(rows.acc)), row_of, begin, 32, stop);
-    const float sum = halves_sum(rows.sum);
+    const float sum = rows.whole_sum(g, st, walk.seq, count, row_of, begin, 32, stop);
     const int half = fresh_lane() / 32, column = fresh_lane() % 32;  // (anew: nothing of theirs is kept over the keys)
     if (column >= count) continue;
     const int row = row0 + column, token = st.span.begin + row / g.group, head = kv * g.group + row % g.group;
     const bool begins = now.unit0 == 0, ends = now.unit1 == st.units;
     if (begins && ends) {
-      store_column<T, DB>(static_cast<T*>(g.o) + token * g.o_stride + int64_t(head) * g.head, rows.acc, half, g.head, sum == 0.0f ? 0.0f : 1.0f / sum);
+      store_column<T, DB>(static_cast<T*>(g.o) + token * g.o_stride + int64_t(head) * g.head, rows.acc, half, g.head,
+                         sum == 0.0f ? 0.0f : rows.largest == -INFINITY ? NAN : 1.0f / sum);
     } else {
       float* const slot = slot_at<S>(g, kv, part, begins, kWidth);
       const int r = wave * 32 + column;
@@ -531,11 +551,11 @@ __global__ __launch_bounds__(kBlock) void cached_join_kernel(const CacheArgs g) 
     float top = -INFINITY, l = 0.0f;
     for (int p = 0; p < pieces_of; ++p) top = fmaxf(top, factors[p][r]);
     for (int p = 0; p < pieces_of; ++p) {
-      const float f = factors[p][r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(factors[p][r] - top);
+      const float f = factors[p][r] == -INFINITY ? float(top == -INFINITY) : __builtin_amdgcn_exp2f(factors[p][r] - top);
       factors[p][r] = f;
       l = fmaf(f, sums[p][r], l);
     }
-    total[r] = l;
+    total[r] = l != 0.0f && top == -INFINITY ? NAN : l;
   }
   __syncthreads();
   // four values a thread; where there are few, several threads share the pieces

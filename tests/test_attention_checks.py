@@ -266,3 +266,13 @@ def test_oracle_against_sums_by_hand():
     x = np.array([[[1.0, 0.0, 5.0, 7.0]]])
     assert np.allclose(orc.rotate(x, np.array([1]), np.array([np.pi / 2]), True), [[[0, 1, 5, 7]]])
     assert np.allclose(orc.rotate(x, np.array([1]), np.array([np.pi / 2, 0.0]), False), [[[-5, 0, 1, 7]]])
+
+
+def test_oracle_where_all_scores_are_minus_infinity():
+    """Such a score has no weight beside another, and no weight of its own: exp(-inf - -inf)."""
+    q, k, v = np.array([[1.0], [2.0]]), np.array([[-np.inf], [2.0]]), np.array([[1.0], [10.0]])
+    seen = orc.causal(2, 2)
+    o, lse, p = orc.attention(q, k, v, seen, 1.0)
+    assert np.isnan(o[0, 0]) and lse[0] == -np.inf and np.isnan(p[0, 0]) and p[0, 1] == 0 and o[1, 0] == 10.0 and lse[1] == 4.0
+    _, dk, dv, p, ds = orc.gradients(np.ones((2, 1)), q, k, v, o, lse, seen, 1.0)
+    assert np.isnan(dk[0, 0]) and np.isnan(dv[0, 0]) and np.isnan(ds[0, 0]) and ds[0, 1] == 0 and dk[1, 0] == 0 and dv[1, 0] == 1

@@ -217,6 +217,39 @@ def test_what_is_not_seen_at_every_width(A, name, head):
     assert np.isfinite(dv[21:, 0]).all() and np.isfinite(np.delete(dq[:100], 20, axis=0)).all()
 
 
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("head", [16, 64, 128, 256])
+@pytest.mark.parametrize("causal", [True, False])
+def test_scores_of_minus_infinity(A, name, head, causal):
+    """A sequence's first 70 keys have no score but minus infinity.  Rows that see nothing else are NaN, and so is what keys get from them; for the
+    others it is as if those keys were not there.  Rows that see no key are zeros beside them."""
+    def spoil(values):
+        values["q"][:, :, 0] = 1.0
+        values["k"][:70, :, 0] = -np.inf
+        values["k"][150:180, :, 0] = -np.inf    # all of the second sequence
+    c = Case(A, 21, name, [150, 30, 40], [150, 30, 20], 2, 1, head, causal, change=spoil)
+    c.forward()
+    o, lse = f64(c.o), f64(c.lse)
+    grads = [f64(g) for g in c.backward()]
+    for s, rows, keys in c.pieces():
+        seen = c.seen(s)
+        for h in range(2):
+            q, k, v = c.x["q"][rows, h], c.x["k"][keys, 0], c.x["v"][keys, 0]
+            with np.errstate(invalid="ignore"):
+                check_forward(name, q, k, v, seen, c.scale, o[rows, h], lse[h, rows], "sequence %d head %d" % (s, h))
+            if s == 0:   # to the bounds of the keys that count
+                behind = slice(70, 150) if causal else slice(0, 150)
+                check_forward(name, q[behind], k[70:], v[70:], seen[behind, 70:], c.scale, o[behind, h], lse[h, behind], "head %d" % h)
+        heads = [(c.x["do"][rows, h], c.x["q"][rows, h], c.x["k"][keys, 0], c.x["v"][keys, 0], o[rows, h], lse[h, rows]) for h in range(2)]
+        with np.errstate(invalid="ignore"):
+            check_gradients(name, heads, c.scale, seen, ([grads[0][rows, h] for h in range(2)], grads[1][keys, 0], grads[2][keys, 0]),
+                            "sequence %d" % s, kinds=False)
+    if causal:
+        assert np.isnan(o[:70]).all() and np.isfinite(o[70:150]).all() and np.all(o[180:200] == 0)
+        assert np.isnan(grads[2][:70]).all() and np.isfinite(grads[2][70:150]).all()
+    assert np.isnan(o[150:180]).all() and np.all(lse[:, 150:180] == -np.inf) and np.isnan(grads[1][150:180]).all() and np.isnan(grads[0][150:180]).all()
+
+
 def test_rows_behind_the_last_sequence(A):
     """Left as they were in what the caller gives, zeros in what the call makes or where the descriptor says so."""
     torch = torch_mod()

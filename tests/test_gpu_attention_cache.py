@@ -281,6 +281,29 @@ def test_a_cache_that_holds_nan_at_every_width(A, name, head, new):
     c.check_attention()
 
 
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("head", [16, 80, 128, 256])
+@pytest.mark.parametrize("new", [1, 9, 40])   # wavefronts with keys of their own, and with keys that they share
+def test_scores_of_minus_infinity(A, name, head, new):
+    """Rows that see nothing else are NaN: of a context in one part, and of one in many.  Beside another score those keys are as if they were not there;
+    and rows that see no place (there are pages for none) are zeros."""
+    contexts = [20, 900, 700, 0]
+    c = Cache(A, 21, name, contexts, [new] * 4, 2, 1, head, 16, bad=[(3, i, -1) for i in range(-(-new // 16))])
+    c.q[:, :, 0], c.xq[:, :, 0] = 1.0, 1.0
+    c.k[:2 * new, :, 0], c.xk[:2 * new, :, 0] = -float("inf"), -np.inf
+    for s, many in ((0, 20), (1, 900), (2, 600)):
+        for j in range(many):
+            p, at = orc.place(c.table[s], 16, j)
+            c.k_cache[p, :, at, 0] = -float("inf")
+    c.append()
+    o = f64(c.attend())
+    assert np.isnan(o[:2 * new]).all() and np.isfinite(o[2 * new:]).all() and np.all(o[3 * new:] == 0)
+    k, v, _ = c.held(2)
+    seen = orc.causal(new, 700 + new)[:, 600:]
+    for h in range(2):
+        check_forward(name, c.xq[2 * new:3 * new, h], k[600:, 0], v[600:, 0], seen, c.scale, o[2 * new:3 * new, h])
+
+
 def test_steps_of_a_server(A):
     """A prompt, then token after token: the same attention as over the whole sequence at once, to the bounds of both (the cache holds the
     same bfloat16 keys, so the scores agree; weights and results are rounded in two orders)."""

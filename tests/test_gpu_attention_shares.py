@@ -3,7 +3,7 @@ share does not see or has none of."""
 import numpy as np
 import pytest
 
-from attention_util import ints
+from attention_util import check_forward, ints
 from stage_util import f64, torch_mod
 from test_gpu_attention import Case
 
@@ -67,6 +67,24 @@ def test_what_is_not_seen_has_no_effect(A, name):
     o = f64(c.forward()[0])
     assert np.isfinite(o[:1300]).all() and np.isnan(o[1300:, 0, 5]).all() and np.isfinite(np.delete(o, 5, axis=2)).all()
     c.check_forward()
+
+
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("minus", [2500, 3000])
+def test_scores_of_minus_infinity(A, name, minus):
+    """Of all keys: the row is NaN; of all but the last share's: it is as if those were not there.  (The second sequence's row sees no key.)"""
+    def spoil(values):
+        values["q"][:, :, 0] = 1.0
+        values["k"][:minus, :, 0] = -np.inf
+    c = Case(A, 6, name, [1, 3], [3000, 0], 2, 1, 64, False, change=spoil)
+    assert A.accept_attention_workspace_size(c.desc) > 0
+    o, lse = (f64(t) for t in c.forward())
+    assert np.all(o[1:] == 0) and np.all(lse[:, 1:] == -np.inf)
+    for h in range(2):
+        if minus == 3000:
+            assert np.isnan(o[0, h]).all() and lse[h, 0] == -np.inf
+        else:
+            check_forward(name, c.x["q"][:1, h], c.x["k"][minus:, 0], c.x["v"][minus:, 0], np.ones((1, 3000 - minus), bool), c.scale, o[:1, h], lse[h, :1])
 
 
 def test_the_same_bits_and_workspaces(A):
