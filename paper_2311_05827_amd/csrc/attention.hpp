@@ -357,29 +357,6 @@ __device__ __forceinline__ short4_t transposed(uint32_t at) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_short4_t*>(at));
 }
 
-// A tile's rows n + 16 * s on, 16 of them, as the left operand of weighted_rows; and that half of its products.
-template <int DB>
-struct Columns {
-  bf16x8_t a[DB];
-};
-template <int DB>
-__device__ __forceinline__ void load_columns(Columns<DB>& c, uint32_t tile, const Reader<bf16_t, DB>& reader, int n, int s) {
-  constexpr int ROWB = Head<bf16_t, DB>::kRowBytes;
-  const uint32_t at = tile + reader.columns;
-#pragma unroll
-  for (int db = 0; db < DB; ++db) {
-    const uint32_t from = at ^ uint32_t(db << 6);
-    const short4_t lo = transposed(from + (n + 16 * s) * ROWB), hi = transposed((from ^ 32u) + (n + 16 * s + 8) * ROWB);
-    typedef short short8_t __attribute__((ext_vector_type(8)));
-    c.a[db] = __builtin_bit_cast(bf16x8_t, short8_t(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)));
-  }
-}
-template <int DB>
-__device__ __forceinline__ void weighted_half(v16f_t (&acc)[DB], const Columns<DB>& c, bf16x8_t w) {
-#pragma unroll
-  for (int db = 0; db < DB; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c.a[db], w, acc[db], 0, 0, 0);
-}
-
 // acc[value of a head][lane's column] += sum over 32 rows of a tile, from row n (a multiple of 32) on, of x[row][value] * w[row][column].
 template <typename T, int DB>
 __device__ __forceinline__ void weighted_rows(v16f_t (&acc)[DB], uint32_t tile, const Reader<T, DB>& reader, int n, const Weights<T>& w) {
@@ -503,11 +480,7 @@ struct Lone {
   }
 };
 
-// The two halves of a column (lanes l and l + 32): largest, sum.
-__device__ __forceinline__ float other_half(float v, bool second) {
-  const auto r = __builtin_amdgcn_permlane32_swap(f32_as_u32(v), f32_as_u32(v), false, false);
-  return u32_as_f32(second ? r[0] : r[1]);
-}
+// Of the two halves of a column (lanes l and l + 32): the larger, the sum.
 __device__ __forceinline__ float halves_max(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(f32_as_u32(v), f32_as_u32(v), false, false);
   return fmaxf(u32_as_f32(r[0]), u32_as_f32(r[1]));
