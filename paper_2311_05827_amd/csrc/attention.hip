@@ -162,19 +162,37 @@ __global__ __launch_bounds__(kWaves * kWave, groups_a_unit(DB, sizeof(T))) void 
       weighted_rows<T, DB>(acc, lds_offset(vt), reader, nb * 32, w);
     }
   }
-  for (uint32_t bad = columns_where(is_row && !finite_column<DB>(acc)); bad; bad &= bad - 1) {
-    const int c = __builtin_ctz(bad), sees = seen_by(row0 + c), stop = sees < steps * BN ? sees : steps * BN;
-    const T* const q_row = static_cast<const T*>(g.q) + (qs.begin + row0 + c) * g.q_stride + int64_t(head) * g.head;
-    const float base = of_lane(largest == -INFINITY ? 0.0f : -largest, c);
-    Lone<T, DB> lone;
-    for (int j0 = step0 * BN; j0 < stop; j0 += kWave) {
-      const bool is = j0 + lane < stop;
-      const float p = is ? __builtin_amdgcn_exp2f(fmaf(dot(q_row, k0 + (j0 + lane) * g.k_stride, g.head), g.scale, base)) : 0.0f;
-      lone.add(__ballot(is), p, g.head, [&](int t) { return v0 + (j0 + t) * g.v_stride; });
-    }
-    lone.put(acc, c);
-  }
   sum = halves_sum(sum);
+  // (see of_both_halves; a row whose sum is not finite is NaN whatever its values are)
+  const bool bad = of_both_halves(is_row && !finite_column<DB>(acc)) && sum * 0.0f == 0.0f;
+  if (__builtin_expect(__any(bad), false)) {
+    const AttentionArgs f = fresh_arguments<AttentionArgs>();
+    const int lane_now = fresh_lane();
+    const Masked masked = masked_keys(first_limit, keys, step0 * BN, steps * BN, BN);
+    bool spoiled = false;
+    for (int j = masked.unseen + lane_now; j < masked.end; j += kWave) spoiled |= !finite_row(v0 + j * f.v_stride, parts);
+    if (__any(spoiled)) {
+      const T* const mine = static_cast<const T*>(f.q) + (qs.begin + (is_row ? row : last)) * f.q_stride + int64_t(head) * f.head;
+      const float base = largest == -INFINITY ? 0.0f : -largest;
+      clear_columns<DB>(acc, bad);
+#pragma unroll 1
+      for (int key0 = step0 * BN; key0 < masked.first; key0 += 32) {
+        const v16f_t s = rows_product_far<T, DB>(k0 + (key0 + lane_now % 32) * f.k_stride, mine, parts);
+        float p[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) p[r] = bad ? __builtin_amdgcn_exp2f(fmaf(s[r], f.scale, base)) : 0.0f;
+        Weights<T> w;
+        set_weights(w, p);
+        weighted_rows_far<T, DB>(acc, v0 + key0 * f.v_stride, v0 + (key0 + 16) * f.v_stride, f.v_stride, f.head, w);
+      }
+      const int stop = wave_limit < masked.end ? wave_limit : masked.end;
+#pragma unroll 1
+      for (int j = masked.first; j < stop; ++j) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(dot_far<T, DB>(mine, k0 + j * f.k_stride, parts), f.scale, base));
+        add_row<T, DB>(acc, v0 + j * f.v_stride, p, bad && j < limit(), f.head);
+      }
+    }
+  }
   if (!is_row) return;
   // A row that sees keys, but no score above minus infinity, has no weights: minus infinity less itself.
   const int sees = seen_by(row), stop = sees < steps * BN ? sees : steps * BN;

@@ -67,6 +67,16 @@ __device__ __forceinline__ int fresh_lane() {
   return lane;
 }
 
+// A kernel's argument (its only one) from memory again: for code that is rarely reached, so that nothing of it takes a scalar register through the loops before.
+template <typename A>
+__device__ __forceinline__ A fresh_arguments() {
+  auto at = __builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(at));
+  A a;
+  __builtin_memcpy(&a, (const void*)at, sizeof(A));
+  return a;
+}
+
 // ---- sequences ---------------------------------------------------------------------------------
 // First token and end of a sequence; whatever the offsets hold, inside 0 .. tokens.
 struct Span {
@@ -422,64 +432,6 @@ __device__ __forceinline__ bool finite_column(const v16f_t (&acc)[DB]) {
   return zero == 0.0f;
 }
 
-// Masked rows have weight zero, and zero times an infinity or NaN of theirs is NaN.  Columns whose sums are not all finite are therefore made again one by one,
-// by the whole wavefront, from the rows that they take and no others: a lane makes the weight of one of 64 rows, then has values lane, lane + 64, ... of
-// all of them.  (Columns with bit 1 in the mask: those for which `is` holds in either half.)
-__device__ __forceinline__ uint32_t columns_where(bool is) {
-  const uint64_t lanes = __ballot(is);
-  return uint32_t(lanes) | uint32_t(lanes >> 32);
-}
-__device__ __forceinline__ float of_lane(float v, int lane) { return u32_as_f32(uint32_t(__builtin_amdgcn_readlane(int(f32_as_u32(v)), lane))); }
-template <typename T>
-__device__ __forceinline__ float dot(const T* a, const T* b, int head) {
-  constexpr int VEC = 16 / int(sizeof(T));
-  float sum = 0.0f;
-#pragma unroll 1
-  for (int d = 0; d < head; d += VEC) {
-    float x[VEC], y[VEC];
-    load_vec(a + d, x);
-    load_vec(b + d, y);
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) sum = fmaf(x[i], y[i], sum);
-  }
-  return sum;
-}
-template <typename T, int DB>
-struct Lone {
-  static constexpr int kValues = (DB + 1) / 2;
-  float x[kValues];
-  __device__ __forceinline__ Lone() {
-#pragma unroll
-    for (int i = 0; i < kValues; ++i) x[i] = 0.0f;
-  }
-  // of the lanes in `of`: their weight times their row
-  template <typename At>
-  __device__ __forceinline__ void add(uint64_t of, float weight, int head, const At& row_at) {
-    const int lane = fresh_lane();
-#pragma unroll 1
-    for (; of; of &= of - 1) {
-      const int t = __builtin_ctzll(of);
-      const float w = of_lane(weight, t);
-      const T* const row = row_at(t);
-#pragma unroll
-      for (int i = 0; i < kValues; ++i)
-        if (lane + i * kWave < head) x[i] = fmaf(w, load_one(row + lane + i * kWave), x[i]);
-    }
-  }
-  __device__ __forceinline__ void put(v16f_t (&acc)[DB], int column) const {
-    const int lane = fresh_lane();
-#pragma unroll
-    for (int db = 0; db < DB; ++db) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float v = __shfl(x[db / 2], db % 2 * 32 + result_row(r, lane / 32), kWave);
-        acc[db][r] = lane % 32 == column ? v : acc[db][r];
-      }
-      __builtin_amdgcn_sched_barrier(0);  // not all of them at once: they have no registers
-    }
-  }
-};
-
 // Of the two halves of a column (lanes l and l + 32): the larger, the sum.
 __device__ __forceinline__ float halves_max(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(f32_as_u32(v), f32_as_u32(v), false, false);
@@ -488,6 +440,130 @@ __device__ __forceinline__ float halves_max(float v) {
 __device__ __forceinline__ float halves_sum(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(f32_as_u32(v), f32_as_u32(v), false, false);
   return u32_as_f32(r[0]) + u32_as_f32(r[1]);
+}
+
+// ---- columns that masked rows spoiled ---------------------------------------------------------------
+// A masked row has weight zero, and zero times an infinity or NaN of its is NaN.  So where a wavefront's sums are not all finite, and its masked tiles (the few that some of
+// its columns do not see all of) hold a row that is not, these columns are made again: over the other tiles by products as before,
+// then from the masked tiles' rows one by one, where a lane has its own column's weight and adds its values of a row that the column sees, times that.  Operands come from memory
+// here: nothing is kept for it in the registers of the loops, and no other wavefront has to wait.  16384 tokens, 16 heads on 2 of 128, bfloat16: with NaN
+// in one token's values, or in one row of do, 1.0 and 3.4 ms, as with none; in all values 6.5 ms forward, in all of do 28 backward.  (Going over the masked tiles
+// first, so that only their rows are left to make again, took 1 to 7 % of the time of calls that have no such value.)
+__device__ __forceinline__ bool of_both_halves(bool is) {
+  const uint64_t lanes = __ballot(is);
+  return (uint32_t(lanes) | uint32_t(lanes >> 32)) >> (fresh_lane() % 32) & 1;
+}
+template <int DB>
+__device__ __forceinline__ void clear_columns(v16f_t (&acc)[DB], bool is) {
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[db][r] = is ? 0.0f : acc[db][r];
+}
+// Of a wavefront's keys, which are those from `begin` to `end` (both whole tiles of `tile`; places from `keys` on give the last key again): the first one of its masked
+// tiles, the first one that some column does not see (the last key, if it is taken for places that no column sees), and the end.
+struct Masked {
+  int first, unseen, end;
+};
+__device__ __forceinline__ Masked masked_keys(int all_see, int keys, int begin, int end, int tile) {
+  int first = all_see / tile * tile;
+  first = first < begin ? begin : first > end ? end : first;
+  const int unseen = all_see < first ? first : all_see;
+  return {first, end > keys && unseen > keys - 1 ? keys - 1 : unseen, end < keys ? end : keys};
+}
+// Is a row of `parts` parts finite everywhere?  A row a lane.
+template <typename T>
+__device__ __forceinline__ bool finite_row(const T* row, int parts) {
+  constexpr int VEC = 16 / int(sizeof(T));
+  float zero = 0.0f;
+#pragma unroll 4
+  for (int i = 0; i < parts; ++i) {
+    float x[VEC];
+    load_vec(row + i * VEC, x);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) zero = fmaf(x[j], 0.0f, zero);
+  }
+  return zero == 0.0f;
+}
+// rows_product with a lane's row of either operand in memory.
+template <typename T, int DB>
+__device__ __forceinline__ v16f_t rows_product_far(const T* a, const T* b, int parts) {
+  constexpr int VEC = 16 / int(sizeof(T));
+  const int half = fresh_lane() / 32;
+  v16f_t c = {};
+#pragma unroll
+  for (int i = 0; i < Head<T, DB>::kPairs; ++i) {
+    const int part = 2 * i + half;
+    const bool is = part < parts;
+    const int at = (is ? part : 0) * VEC;
+    const uint4 x = load16(a + at), y = load16(b + at), none = make_uint4(0, 0, 0, 0);
+    c = multiply_parts<T>(is ? x : none, is ? y : none, c);
+    if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // no more loads at a time: they have no registers
+  }
+  return c;
+}
+// weighted_rows with the 32 rows in memory: 16 from `low` and 16 from `high` on (the same for all lanes), `stride` elements apart.
+template <typename T, int DB>
+__device__ __forceinline__ void weighted_rows_far(v16f_t (&acc)[DB], const T* low, const T* high, int64_t stride, int head, const Weights<T>& w) {
+  const int lane = fresh_lane(), column = lane % 32;
+  const uint32_t mine = uint32_t(lane / 32 * 4) * uint32_t(stride);
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    const T* const from = uniform(s ? high : low);
+    const auto value = [&](int e, int db) {  // (what is behind head_size is not stored: the last value again)
+      return load_one(from + result_row(e, 0) * stride + (mine + uint32_t(db * 32 + column < head ? db * 32 + column : head - 1)));
+    };
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = value(e, db);
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, narrow(f)), w.w[s], acc[db], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(value(e, db), w.w[8 * s + e], acc[db], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+}
+// The product of this lane's column and a row that is the same for all lanes; both in memory.
+template <typename T, int DB>
+__device__ __forceinline__ float dot_far(const T* mine, const T* row, int parts) {
+  constexpr int VEC = 16 / int(sizeof(T));
+  const int half = fresh_lane() / 32;
+  float sum = 0.0f;
+#pragma unroll 4
+  for (int part = half; part < parts; part += 2) {
+    float x[VEC], y[VEC];
+    load_vec(mine + part * VEC, x);
+    load_vec(row + part * VEC, y);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) sum = fmaf(x[j], y[j], sum);
+  }
+  return halves_sum(sum);
+}
+// Columns that take it: their sums and weight * row.
+template <typename T, int DB>
+__device__ __forceinline__ void add_row(v16f_t (&acc)[DB], const T* row, float weight, bool takes, int head) {
+  const int half = fresh_lane() / 32;
+#pragma unroll
+  for (int db = 0; db < DB; ++db) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (db * 32 + q * 8 >= head) continue;
+      float x[4];
+      load_quad(row + db * 32 + q * 8 + half * 4, x);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[db][4 * q + j] = takes ? fmaf(weight, x[j], acc[db][4 * q + j]) : acc[db][4 * q + j];
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
 }
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;

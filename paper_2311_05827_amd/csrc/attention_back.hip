@@ -3,6 +3,8 @@
 // of tiles where a single kernel would do with five, but each gradient is one workgroup's own sum, in a fixed order: no atomics.
 #include "attention.hpp"
 
+#include <type_traits>
+
 namespace accept {
 namespace {
 
@@ -144,21 +146,38 @@ __global__ __launch_bounds__(kWaves * kWave, groups_a_unit(DB, sizeof(T))) void 
       weighted_rows<T, DB>(acc, lds_offset(kt), reader, n, w);
     }
   }
-  for (uint32_t bad = columns_where(is_row && !finite_column<DB>(acc)); bad; bad &= bad - 1) {  // (see Lone)
-    const int c = __builtin_ctz(bad), sees = seen_by(row0 + c), stop = sees < steps * BN ? sees : steps * BN;
-    const T* const q_row = static_cast<const T*>(g.q) + (qs.begin + row0 + c) * g.q_stride + int64_t(head) * g.head;
-    const T* const do_row = static_cast<const T*>(g.dout) + (qs.begin + row0 + c) * g.o_stride + int64_t(head) * g.head;
-    const float lse_c = of_lane(lse, c), along_c = of_lane(along, c);
-    Lone<T, DB> lone;
-    for (int j0 = step0 * BN; j0 < stop; j0 += kWave) {
-      const bool is = j0 + lane < stop;
-      float ds = 0.0f;
-      if (is)
-        ds = __builtin_amdgcn_exp2f(fmaf(dot(q_row, k0 + (j0 + lane) * g.k_stride, g.head), g.scale2, -lse_c)) *
-             (dot(do_row, v0 + (j0 + lane) * g.v_stride, g.head) - along_c);
-      lone.add(__ballot(is), ds, g.head, [&](int t) { return k0 + (j0 + t) * g.k_stride; });
+  const bool bad = of_both_halves(is_row && !finite_column<DB>(acc)) && lse == lse;  // (as in attention_kernel)
+  if (__builtin_expect(__any(bad), false)) {
+    const BackArgs f = fresh_arguments<BackArgs>();
+    const int lane_now = fresh_lane();
+    const Masked masked = masked_keys(first_limit, keys, step0 * BN, steps * BN, BN);
+    bool spoiled = false;
+    for (int j = masked.unseen + lane_now; j < masked.end; j += kWave) spoiled |= !finite_row(k0 + j * f.k_stride, parts);
+    if (__any(spoiled)) {
+      const int64_t at = qs.begin + (is_row ? row : last);
+      const T* const q_row = static_cast<const T*>(f.q) + at * f.q_stride + int64_t(head) * f.head;
+      const T* const do_row = static_cast<const T*>(f.dout) + at * f.o_stride + int64_t(head) * f.head;
+      clear_columns<DB>(acc, bad);
+#pragma unroll 1
+      for (int key0 = step0 * BN; key0 < masked.first; key0 += 32) {
+        const int j = key0 + lane_now % 32;
+        const v16f_t s = rows_product_far<T, DB>(k0 + j * f.k_stride, q_row, parts);
+        const v16f_t dp = rows_product_far<T, DB>(v0 + j * f.v_stride, do_row, parts);
+        float ds[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) ds[r] = bad ? __builtin_amdgcn_exp2f(fmaf(s[r], f.scale2, -lse)) * (dp[r] - along) : 0.0f;
+        Weights<T> w;
+        set_weights(w, ds);
+        weighted_rows_far<T, DB>(acc, k0 + key0 * f.k_stride, k0 + (key0 + 16) * f.k_stride, f.k_stride, f.head, w);
+      }
+      const int stop = wave_limit < masked.end ? wave_limit : masked.end;
+#pragma unroll 1
+      for (int j = masked.first; j < stop; ++j) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(dot_far<T, DB>(q_row, k0 + j * f.k_stride, parts), f.scale2, -lse));
+        const float ds = p * (dot_far<T, DB>(do_row, v0 + j * f.v_stride, parts) - along);
+        add_row<T, DB>(acc, k0 + j * f.k_stride, ds, bad && j < limit(), f.head);
+      }
     }
-    lone.put(acc, c);
   }
   if (!is_row) return;
   if (g.q_split > 1)
@@ -200,7 +219,6 @@ __global__ __launch_bounds__(kWaves * kWave, sizeof(T) == 2 && DB <= 4 ? 2 : 1) 
   const Span qs = uniform_span(g.q_offsets, piece.seq, g.q_tokens, g.q_each), ks = uniform_span(g.k_offsets, piece.seq, g.k_tokens, g.k_each);
   const int rows = qs.size(), keys = ks.size(), more = keys - rows, last = keys - 1;
   const int key0 = piece.tile * kRows + wave * 32, key = key0 + column;
-  const bool is_key = key < keys;
   // the first query that sees a key
   const auto seen_from = [&](int j) { return !g.causal || j - more < 0 ? 0 : j - more; };
   const int wave_from = seen_from(key0), wave_all = seen_from(key0 + 31);
@@ -209,7 +227,7 @@ __global__ __launch_bounds__(kWaves * kWave, sizeof(T) == 2 && DB <= 4 ? 2 : 1) 
   const int steps = each * g.group, step = int(int64_t(steps) * share / g.split), step_end = int(int64_t(steps) * (share + 1) / g.split);
 
   const int parts = g.head * int(sizeof(T)) / 16;
-  const int64_t token = ks.begin + (is_key ? key : last);
+  const int64_t token = ks.begin + (key < keys ? key : last);
   if (g.head < DB * 32) {
     clear_tiles<int(sizeof(tiles)), kWaves * kWave>(tiles);
     __syncthreads();
@@ -303,40 +321,82 @@ __global__ __launch_bounds__(kWaves * kWave, sizeof(T) == 2 && DB <= 4 ? 2 : 1) 
     }
   };
   add_up();
-  for (uint32_t bad = columns_where(is_key && !((!K || finite_column<DB>(sum_k)) && (!V || finite_column<DB>(sum_v)))); bad; bad &= bad - 1) {  // (see Lone)
-    const int c = __builtin_ctz(bad), from = seen_from(key0 + c);
-    const T* const k_row = static_cast<const T*>(g.k) + (ks.begin + key0 + c) * g.k_stride + int64_t(head) * g.head;
-    const T* const v_row = static_cast<const T*>(g.v) + (ks.begin + key0 + c) * g.v_stride + int64_t(head) * g.head;
-    Lone<T, DB> of_k, of_v;
-    for (int i = step; i < step_end; ++i) {
-      const int h = head * g.group + i / each, row = (first + each - 1 - i % each) * BM + lane;
-      const bool is = lane < BM && row >= from && row < rows;
-      const T* const q0 = static_cast<const T*>(g.q) + int64_t(h) * g.head;
-      const T* const o0 = static_cast<const T*>(g.dout) + int64_t(h) * g.head;
-      float p = 0.0f, ds = 0.0f;
-      if (is) {
-        const int64_t at = int64_t(qs.begin) + row;
-        p = __builtin_amdgcn_exp2f(fmaf(dot(k_row, q0 + at * g.q_stride, g.head), g.scale2, -g.stats[(int64_t(g.heads) + h) * g.q_tokens + at]));
-        ds = p * (dot(v_row, o0 + at * g.o_stride, g.head) - g.stats[int64_t(h) * g.q_tokens + at]);
-      }
-      const uint64_t of = __ballot(is);
-      const int64_t first_row = int64_t(qs.begin) + (first + each - 1 - i % each) * BM;
-      of_v.add(of, p, g.head, [&](int t) { return o0 + (first_row + t) * g.o_stride; });
-      of_k.add(of, ds, g.head, [&](int t) { return q0 + (first_row + t) * g.q_stride; });
+  // (as in attention_kernel; here masked tiles are of queries: those that some keys are not seen by, and where there are fewer than 32 left)
+  const int lane_now = fresh_lane(), key_now = key0 + lane_now % 32;  // (anew: nothing of theirs is kept over the queries)
+  const bool bad = of_both_halves(key_now < keys && !((!K || finite_column<DB>(sum_k)) && (!V || finite_column<DB>(sum_v))));
+  if (__builtin_expect(__any(bad), false)) {
+    const BackArgs f = fresh_arguments<BackArgs>();
+    const int j = key_now < keys ? key_now : last, from = seen_from(j);
+    const auto tile_of = [&](int i) { return (first + each - 1 - i % each) * BM; };  // its first query
+    const auto row_of = [&](const void* x, int64_t stride, int i, int row) {
+      return static_cast<const T*>(x) + (qs.begin + row) * stride + int64_t(head * f.group + i / each) * f.head;
+    };
+    const auto is_masked = [&](int row0) { return row0 < wave_all || row0 + BM > rows; };
+    bool spoiled = false;
+    for (int i = step; i < step_end; ++i) {  // (a lane for a row of q, one for a row of do)
+      const int row0 = tile_of(i), row = row0 + lane_now % 32 < rows ? row0 + lane_now % 32 : rows - 1;
+      if (row0 + BM - 1 < wave_from || !is_masked(row0)) continue;
+      if (row < wave_all || (row == rows - 1 && row0 + BM > rows))
+        spoiled |= !finite_row(lane_now < 32 ? row_of(f.q, f.q_stride, i, row) : row_of(f.dout, f.o_stride, i, row), parts);
     }
-    if constexpr (K) of_k.put(sum_k, c);
-    if constexpr (V) of_v.put(sum_v, c);
+    if (__any(spoiled)) {
+      const T* const k_row = static_cast<const T*>(f.k) + (ks.begin + j) * f.k_stride + int64_t(head) * f.head;
+      const T* const v_row = static_cast<const T*>(f.v) + (ks.begin + j) * f.v_stride + int64_t(head) * f.head;
+      const auto again = [&](v16f_t (&sum)[DB], auto of_k) {  // (one gradient after the other: both at a time have no registers)
+        constexpr bool kOfK = decltype(of_k)::value;
+        clear_columns<DB>(sum, bad);
+#pragma unroll 1
+        for (int i = step; i < step_end; ++i) {
+          const int row0 = tile_of(i);
+          if (row0 + BM - 1 < wave_from || is_masked(row0)) continue;
+          const int row = row0 + lane_now % 32;
+          const float* const e = f.stats + int64_t(head * f.group + i / each) * f.q_tokens + qs.begin + row0 + lane_now / 32 * 4;
+          const float* const l = e + int64_t(f.heads) * f.q_tokens;
+          const v16f_t s = rows_product_far<T, DB>(row_of(f.q, f.q_stride, i, row), k_row, parts);
+          float p[16];
+#pragma unroll
+          for (int r = 0; r < 16; ++r) p[r] = bad ? __builtin_amdgcn_exp2f(fmaf(s[r], f.scale2, -l[result_row(r, 0)])) : 0.0f;
+          if constexpr (kOfK) {
+            const v16f_t dp = rows_product_far<T, DB>(row_of(f.dout, f.o_stride, i, row), v_row, parts);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) p[r] = bad ? p[r] * (dp[r] - e[result_row(r, 0)]) : 0.0f;
+          }
+          Weights<T> w;
+          set_weights(w, p);
+          const void* const x = kOfK ? f.q : f.dout;
+          const int64_t stride = kOfK ? f.q_stride : f.o_stride;
+          weighted_rows_far<T, DB>(sum, row_of(x, stride, i, row0), row_of(x, stride, i, row0 + 16), stride, f.head, w);
+        }
+#pragma unroll 1
+        for (int i = step; i < step_end; ++i) {
+          const int row0 = tile_of(i);
+          if (row0 + BM - 1 < wave_from || !is_masked(row0)) continue;
+          const float* const e = f.stats + int64_t(head * f.group + i / each) * f.q_tokens + qs.begin;
+#pragma unroll 1
+          for (int row = row0; row < row0 + BM && row < rows; ++row) {
+            const T* const q_row = row_of(f.q, f.q_stride, i, row);
+            const T* const do_row = row_of(f.dout, f.o_stride, i, row);
+            float w = __builtin_amdgcn_exp2f(fmaf(dot_far<T, DB>(k_row, q_row, parts), f.scale2, -e[int64_t(f.heads) * f.q_tokens + row]));
+            if constexpr (kOfK) w *= dot_far<T, DB>(v_row, do_row, parts) - e[row];
+            add_row<T, DB>(sum, kOfK ? q_row : do_row, w, bad && row >= from, f.head);
+          }
+        }
+      };
+      if constexpr (V) again(sum_v, std::false_type{});
+      if constexpr (K) again(sum_k, std::true_type{});
+    }
   }
-  if (!is_key) return;
+  if (key_now >= keys) return;
+  const int64_t token_now = ks.begin + key_now;
   if (g.split > 1) {
     const int64_t whole = int64_t(g.k_tokens) * g.kv_heads * g.head;
-    float* const to = g.shares + 2 * share * whole + (token * g.kv_heads + head) * g.head;
-    if constexpr (K) store_column<float, DB>(to, sum_k, half, g.head, g.scale);
-    if constexpr (V) store_column<float, DB>(to + whole, sum_v, half, g.head, 1.0f);
+    float* const to = g.shares + 2 * share * whole + (token_now * g.kv_heads + head) * g.head;
+    if constexpr (K) store_column<float, DB>(to, sum_k, lane_now / 32, g.head, g.scale);
+    if constexpr (V) store_column<float, DB>(to + whole, sum_v, lane_now / 32, g.head, 1.0f);
     return;
   }
-  if constexpr (K) store_column<T, DB>(dk + token * g.dk_stride, sum_k, half, g.head, g.scale);
-  if constexpr (V) store_column<T, DB>(dv + token * g.dv_stride, sum_v, half, g.head, 1.0f);
+  if constexpr (K) store_column<T, DB>(dk + token_now * g.dk_stride, sum_k, lane_now / 32, g.head, g.scale);
+  if constexpr (V) store_column<T, DB>(dv + token_now * g.dv_stride, sum_v, lane_now / 32, g.head, 1.0f);
 }
 
 // The shares' sums, four values a thread, of `tokens` (those of a sequence) of `row_values` each.

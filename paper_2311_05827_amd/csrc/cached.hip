@@ -186,7 +186,8 @@ __device__ __forceinline__ TwoPages pages_of(const CacheArgs& g, const Step& st,
   if (j >= window.first + Window::kReach || i < window.first) window.load(i);
   return {window.at(i), window.at(j)};
 }
-// Those keys and values into tiles, by WAVES wavefronts; places behind the last one give that one again.  Returns which of the places exist.
+// Those keys and values into tiles, by WAVES wavefronts; places behind the last one give that one again, places that do not exist some of page 0.  Returns which
+// of them exist.
 template <typename T, int DB, int WAVES, bool ONCE>
 __device__ __forceinline__ uint32_t fetch_places(const CacheArgs& g, const Step& st, const TwoPages& two, int kv, int key0, int wave, uint32_t k_to,
                                                  uint32_t v_to) {
@@ -196,20 +197,21 @@ __device__ __forceinline__ uint32_t fetch_places(const CacheArgs& g, const Step&
   const auto place = [&](int half) { return place_at(key0, 16 * half, st.keys); };
   uint32_t there = 0;
   int64_t first[2];
+  int more[2];  // places behind that
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int page = uniform(two.page[h]);
     const bool is = is_page(g.pages, page);
     there |= is ? 0xFFFFu << (16 * h) : 0u;
     first[h] = cache_row(g.pages, is ? page : 0, place(h), kv) * row_bytes;
+    more[h] = st.keys - 1 - place(h);
   }
   const int lane = fresh_lane();
 #pragma unroll
   for (int i = 0; i < kLoads; ++i) {
     const int load = WAVES == 1 ? i : (i * WAVES + wave) % kAll, row = load * kPer, h = row >= 16;
     const int r = row + lane / H::kRowParts, p = lane % H::kRowParts ^ turn<H::kRowBytes>(r);
-    const int j = place_at(key0, r, st.keys);
-    const uint32_t offset = uint32_t(j - place(h)) * uint32_t(row_bytes) + uint32_t(p) * 16u;
+    const uint32_t offset = uint32_t(r % 16 < more[h] ? r % 16 : more[h]) * uint32_t(row_bytes) + uint32_t(p) * 16u;
     if (p < parts) {
       load_tile_part<ONCE>(static_cast<const uint8_t*>(g.k) + first[h], offset, k_to + load * 1024);
       load_tile_part<ONCE>(static_cast<const uint8_t*>(g.v) + first[h], offset, v_to + load * 1024);
@@ -265,11 +267,12 @@ struct Rows {
   // Both halves' sum of weights.  A row that sees keys (of those that `mend` names), but no score above minus infinity, has no weights, as it is minus infinity less
   // itself: with a maximum of minus infinity its sum is 1, that of a row which sees nothing 0.
   template <typename RowOf>
-  __device__ __forceinline__ float whole_sum(const CacheArgs& g, const Step& st, int seq, int count, const RowOf& row_of, int key, int by, int stop) const {
+  __device__ __forceinline__ float whole_sum(const Step& st, int seq, int count, const RowOf& row_of, int key, int by, int stop) const {
     float whole = halves_sum(sum);
     const int column = fresh_lane() % 32;
     uint64_t unsure = __ballot(column < count && whole == 0.0f);
-    if (unsure) {
+    if (__builtin_expect(unsure != 0, false)) {
+      const CacheArgs g = fresh_arguments<CacheArgs>();
       const int32_t* const table = g.table + int64_t(seq) * g.pages.table_pages;
       const int of_step = row_of(column) / g.group;
 #pragma unroll 1
@@ -283,25 +286,63 @@ struct Rows {
     }
     return whole;
   }
-  // Columns that came out not finite by themselves (see Lone): rows row_of(c), over 32 places from `key` on, `by` apart, below `stop`.
+  // Columns that masked rows spoiled (see of_both_halves): row row_of(c) of the sequence each, of which all see the first `all` places that exist.  Tiles as in
+  // whole_sum; those with places that do not exist are masked ones too.
   template <typename RowOf>
-  __device__ __forceinline__ void mend(const CacheArgs& g, const Step& st, int seq, int kv, uint32_t bad, const RowOf& row_of, int key, int by, int stop) {
-    const int lane = fresh_lane();
+  __device__ __forceinline__ void mend(const Step& st, int seq, int kv, bool bad, const RowOf& row_of, int all, int key, int by, int stop) {
+    const CacheArgs g = fresh_arguments<CacheArgs>();
+    const int lane = fresh_lane(), parts = g.head * int(sizeof(T)) / 16, row = row_of(lane % 32), of_step = row / g.group, token = st.span.begin + of_step;
+    const T* const mine = static_cast<const T*>(g.q) + token * g.q_stride + int64_t(kv * g.group + row % g.group) * g.head;
+    const float base = largest == -INFINITY ? 0.0f : -largest;
     const int32_t* const table = g.table + int64_t(seq) * g.pages.table_pages;
-    for (; bad; bad &= bad - 1) {
-      const int c = __builtin_ctz(bad), row = row_of(c), of_step = row / g.group, token = st.span.begin + of_step;
-      const T* const q_row = static_cast<const T*>(g.q) + token * g.q_stride + int64_t(kv * g.group + row % g.group) * g.head;
-      const float base = of_lane(largest == -INFINITY ? 0.0f : -largest, c);
-      Lone<T, DB> lone;
-      for (int ahead = stop - key; ahead > 0; ahead -= by) {
-        const int key0 = stop - ahead, j = place_at(key0, lane % 32, st.keys);
-        const int page = table[j >> g.pages.shift];
-        const bool is = lane < 32 && (seen_among(g, st, of_step, token, key0) >> lane & 1) && is_page(g.pages, page);
-        const int64_t at = is ? cache_row(g.pages, page, j, kv) * g.head : 0;
-        const float p = is ? __builtin_amdgcn_exp2f(fmaf(dot(q_row, static_cast<const T*>(g.k) + at, g.head), g.scale, base)) : 0.0f;
-        lone.add(__ballot(is), p, g.head, [&](int t) { return static_cast<const T*>(g.v) + __shfl(at, t, kWave); });
+    int64_t first[2];  // the rows of a tile's two halves in the caches, as fetch_places takes them
+    const auto look = [&](int key0) {
+      uint32_t there = 0;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int j = place_at(key0, 16 * h, st.keys), page = uniform(table[j >> g.pages.shift]);
+        const bool is = is_page(g.pages, page);
+        there |= is ? 0xFFFFu << (16 * h) : 0u;
+        first[h] = cache_row(g.pages, is ? page : 0, j, kv);
       }
-      lone.put(acc, c);
+      return there;
+    };
+    const auto row_at = [&](const void* cache, int key0, int i) {  // of place key0 + i, or the last one
+      const int j = place_at(key0, i, st.keys);
+      return static_cast<const T*>(cache) + ((i < 16 ? first[0] : first[1]) + (j - place_at(key0, i < 16 ? 0 : 16, st.keys))) * g.head;
+    };
+    bool spoiled = false;
+    for (int ahead = stop - key; ahead > 0; ahead -= by) {
+      const int key0 = stop - ahead;
+      if (look(key0) != ~0u || all - key0 < 32) spoiled |= !finite_row(row_at(g.v, key0, lane % 32), parts);
+    }
+    if (!__any(spoiled)) return;
+    clear_columns<DB>(acc, bad);
+#pragma unroll 1
+    for (int ahead = stop - key; ahead > 0; ahead -= by) {
+      const int key0 = stop - ahead;
+      if (look(key0) != ~0u || all - key0 < 32) continue;
+      const v16f_t s = rows_product_far<T, DB>(row_at(g.k, key0, lane % 32), mine, parts);
+      float p[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) p[r] = bad ? __builtin_amdgcn_exp2f(fmaf(s[r], g.scale, base)) : 0.0f;
+      Weights<T> w;
+      set_weights(w, p);
+      weighted_rows_far<T, DB>(acc, row_at(g.v, key0, 0), row_at(g.v, key0, 16), g.head, g.head, w);
+    }
+#pragma unroll 1
+    for (int ahead = stop - key; ahead > 0; ahead -= by) {
+      const int key0 = stop - ahead;
+      const uint32_t there = look(key0);
+      if (there == ~0u && all - key0 >= 32) continue;
+      const uint32_t seen = seen_among(g, st, of_step, token, key0) & there;
+#pragma unroll 1
+      for (int i = 0; i < 32; ++i) {
+        const bool takes = bad && (seen >> i & 1);
+        if (!__any(takes)) continue;
+        const float p = __builtin_amdgcn_exp2f(fmaf(dot_far<T, DB>(mine, row_at(g.k, key0, i), parts), g.scale, base));
+        add_row<T, DB>(acc, row_at(g.v, key0, i), p, takes, g.head);
+      }
     }
   }
 };
@@ -359,9 +400,10 @@ __global__ __launch_bounds__((KeysShape<T, DB>::kThreads), 1) void cached_keys_k
                 return seen_among(g, st, of_step, st.span.begin + of_step, key0) & now_there;
               });
     }
-    rows.mend(g, st, walk.seq, kv, columns_where(fresh_lane() % 32 < count && !finite_column<DB>(rows.acc)), row_of,
-              now.unit0 * S::kUnit + wave * 32, S::kUnit, stop);
-    const float sum = rows.whole_sum(g, st, walk.seq, count, row_of, now.unit0 * S::kUnit + wave * 32, S::kUnit, stop);
+    const int first = now.unit0 * S::kUnit + wave * 32;
+    const float sum = rows.whole_sum(st, walk.seq, count, row_of, first, S::kUnit, stop);
+    const bool bad = of_both_halves(fresh_lane() % 32 < count && !finite_column<DB>(rows.acc)) && sum * 0.0f == 0.0f;
+    if (__builtin_expect(__any(bad), false)) rows.mend(st, walk.seq, kv, bad, row_of, sight.all, first, S::kUnit, stop);
 
     // the wavefronts' results together, relative to the largest of their maxima (lanes anew: nothing of theirs is kept over the keys)
     const int half = fresh_lane() / 32, column = fresh_lane() % 32;
@@ -371,7 +413,8 @@ __global__ __launch_bounds__((KeysShape<T, DB>::kThreads), 1) void cached_keys_k
 #pragma unroll
     for (int w = 0; w < S::kWaves; ++w) top = fmaxf(top, peak[w][column]);
     const float factor = rows.largest == -INFINITY ? float(top == -INFINITY) : __builtin_amdgcn_exp2f(rows.largest - top);
-    if (half == 0) total[wave][column] = sum * factor;
+    const bool begins = now.unit0 == 0, ends = now.unit1 == st.units;
+    if (half == 0) total[wave][column] = begins && ends && top == -INFINITY && sum != 0.0f ? NAN : sum * factor;
     float* const out = reinterpret_cast<float*>(mine);
 #pragma unroll
     for (int db = 0; db < DB; ++db)
@@ -379,25 +422,26 @@ __global__ __launch_bounds__((KeysShape<T, DB>::kThreads), 1) void cached_keys_k
       for (int r = 0; r < 16; ++r)
         out[(db * 32 + result_row(r, half)) * kPad + column] = rows.largest == -INFINITY ? 0.0f : rows.acc[db][r] * factor;
     __syncthreads();
-    const bool begins = now.unit0 == 0, ends = now.unit1 == st.units;
     float* const slot = slot_at<S>(g, kv, part, begins, kWidth);
     for (int i = threadIdx.x; i < count * kWidth; i += S::kThreads) {
       const int r = i / kWidth, d = i % kWidth;
-      float v = 0.0f, l = 0.0f, top_r = -INFINITY;
+      float v = 0.0f, l = 0.0f;
 #pragma unroll
       for (int w = 0; w < S::kWaves; ++w) {
         v += reinterpret_cast<const float*>(tiles[w])[d * kPad + r];
         l += total[w][r];
-        top_r = fmaxf(top_r, peak[w][r]);
       }
       if (begins && ends) {
         const int flat = row0 + r;
         if (d < g.head)
           store_one(static_cast<T*>(g.o) + (st.span.begin + flat / g.group) * g.o_stride + (kv * g.group + flat % g.group) * g.head + d,
-                    l == 0.0f ? 0.0f : top_r == -INFINITY ? NAN : v / l);
+                    l == 0.0f ? 0.0f : v / l);
       } else {
         slot[r * kWidth + d] = v;
         if (d == 0) {
+          float top_r = -INFINITY;
+#pragma unroll
+          for (int w = 0; w < S::kWaves; ++w) top_r = fmaxf(top_r, peak[w][r]);
           slot[kItem * kWidth + r] = top_r;
           slot[kItem * kWidth + kItem + r] = l;
         }
@@ -471,8 +515,9 @@ __global__ __launch_bounds__((RowsShape<T, DB>::kThreads), 1) void cached_rows_k
                 });
     }
     __syncthreads();  // the tiles are free for the next stretch
-    rows.mend(g, st, walk.seq, kv, columns_where(fresh_lane() % 32 < count && !finite_column<DB>(rows.acc)), row_of, begin, 32, stop);
-    const float sum = rows.whole_sum(g, st, walk.seq, count, row_of, begin, 32, stop);
+    const float sum = rows.whole_sum(st, walk.seq, count, row_of, begin, 32, stop);
+    const bool bad = of_both_halves(fresh_lane() % 32 < count && !finite_column<DB>(rows.acc)) && sum * 0.0f == 0.0f;
+    if (__builtin_expect(__any(bad), false)) rows.mend(st, walk.seq, kv, bad, row_of, sight.all, begin, 32, sight.some < stop ? sight.some : stop);
     const int half = fresh_lane() / 32, column = fresh_lane() % 32;  // (anew: nothing of theirs is kept over the keys)
     if (column >= count) continue;
     const int row = row0 + column, token = st.span.begin + row / g.group, head = kv * g.group + row % g.group;

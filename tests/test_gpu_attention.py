@@ -217,6 +217,71 @@ def test_what_is_not_seen_at_every_width(A, name, head):
     assert np.isfinite(dv[21:, 0]).all() and np.isfinite(np.delete(dq[:100], 20, axis=0)).all()
 
 
+SPOILED = {"v": (300, 5), "k": (200, 2), "q": (150, 1), "do": (250, 7)}
+
+
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("head", [16, 64, 80, 128, 256])
+@pytest.mark.parametrize("what", ["v", "k", "q", "do"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_one_value_in_the_middle_of_many(A, name, head, what, bad):
+    """Rows and keys next to the one that holds it have tiles that they see all of, before and behind: what does not see it is within its bounds."""
+    token, value = SPOILED[what]
+
+    def spoil(values):
+        values[what][token, -1, value] = bad
+    c = Case(A, 22, name, [401, 70], [401, 70], 4, 2, head, change=spoil)
+    c.forward()
+    o, lse = f64(c.o), f64(c.lse)
+    dq, dk, dv = (f64(g) for g in c.backward())
+    with np.errstate(invalid="ignore"):
+        for s, rows, keys in c.pieces():
+            for kv in range(2):
+                heads = [(c.x["do"][rows, h], c.x["q"][rows, h], c.x["k"][keys, kv], c.x["v"][keys, kv], o[rows, h], lse[h, rows]) for h in (2 * kv, 2 * kv + 1)]
+                if what != "k" or kv == 0 or s:   # (scores of infinity: see below)
+                    for h, (_, q, k, v, *_) in zip((2 * kv, 2 * kv + 1), heads):
+                        check = slice(0, rows.stop - rows.start) if what != "q" or h != 3 or s else slice(0, token)
+                        check_forward(name, q[check], k, v, c.seen(s)[check], c.scale, o[rows, h][check], lse[h, rows][check], "sequence %d head %d" % (s, h))
+                check_gradients(name, heads, c.scale, c.seen(s), ([dq[rows, 2 * kv], dq[rows, 2 * kv + 1]], dk[keys, kv], dv[keys, kv]),
+                                "sequence %d key head %d" % (s, kv), kinds=False)
+    if what == "v":
+        assert np.isfinite(np.delete(o, value, axis=2)).all() and np.isfinite(o[:token]).all() and not np.isfinite(o[token:401, 2:, value]).any()
+    if what == "k":
+        assert np.isfinite(o[:token]).all() and np.isfinite(dq[:token]).all()
+    if what == "q":
+        assert np.isfinite(np.delete(o, token, axis=0)).all() and np.isfinite(dv[token + 1:]).all() and np.isfinite(dk[token + 1:]).all()
+    if what == "do":
+        assert np.isfinite(np.delete(dq, token, axis=0)).all() and np.isfinite(dv[token + 1:]).all() and np.isfinite(dk[token + 1:]).all()
+
+
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+def test_the_last_value_of_rows_that_see_all(A, name):
+    """Its row stands in for the rest of the last tile, where it has weight zero: infinities stay infinities."""
+    def spoil(values):
+        values["v"][129, 0, 5], values["do"][149, 0, 7] = np.inf, -np.inf
+    c = Case(A, 23, name, [150], [130], 1, 1, 64, False, change=spoil)
+    c.forward()
+    c.check_forward()
+    o = f64(c.o)
+    assert np.all(o[:, 0, 5] == np.inf)
+    c.t["v"][129, 0, 5], c.x["v"][129, 0, 5] = 1.0, 1.0
+    c.forward()
+    dv = f64(c.backward()[2])
+    assert np.all(dv[:, 0, 7] == -np.inf) and np.isfinite(np.delete(dv, 7, axis=2)).all()
+
+
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+def test_one_value_at_the_start_of_many(A, name):
+    """Thousands of rows see it: they are NaN in that value, at no more than a look at their last tiles."""
+    def spoil(values):
+        values["v"][0, 0, 3], values["do"][6000, 0, 9] = np.nan, np.nan
+    c = Case(A, 24, name, [6001], [6001], 1, 1, 64, change=spoil)
+    o = f64(c.forward()[0])
+    assert np.isnan(o[:, 0, 3]).all() and np.isfinite(np.delete(o, 3, axis=2)).all()
+    dv = f64(c.backward()[2])
+    assert np.isnan(dv[:, 0, 9]).all() and np.isfinite(np.delete(dv, 9, axis=2)).all()
+
+
 @pytest.mark.parametrize("name", ["bf16", "f32"])
 @pytest.mark.parametrize("head", [16, 64, 128, 256])
 @pytest.mark.parametrize("causal", [True, False])

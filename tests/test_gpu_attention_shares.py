@@ -3,7 +3,7 @@ share does not see or has none of."""
 import numpy as np
 import pytest
 
-from attention_util import check_forward, ints
+from attention_util import check_forward, check_gradients, ints
 from stage_util import f64, torch_mod
 from test_gpu_attention import Case
 
@@ -67,6 +67,30 @@ def test_what_is_not_seen_has_no_effect(A, name):
     o = f64(c.forward()[0])
     assert np.isfinite(o[:1300]).all() and np.isnan(o[1300:, 0, 5]).all() and np.isfinite(np.delete(o, 5, axis=2)).all()
     c.check_forward()
+
+
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("token", [40, 780, 1490])
+def test_gradients_of_what_is_not_seen(A, name, token):
+    """A gradient that is NaN, in one share of the queries, and a key, in one of the keys."""
+    def spoil_do(values):
+        values["do"][token, 1, 5] = np.nan
+
+    def spoil_k(values):
+        values["k"][token, 0, 5] = np.nan
+    for spoil in (spoil_do, spoil_k):
+        c = Case(A, 7, name, [1500], [1500], 2, 1, 128, change=spoil)
+        assert A.accept_attention_backward_workspace_size(c.desc) > 8 * 2 * c.nq + 256
+        c.forward()
+        o, lse = f64(c.o), f64(c.lse)
+        dq, dk, dv = (f64(g) for g in c.backward())
+        heads = [(c.x["do"][:, h], c.x["q"][:, h], c.x["k"][:, 0], c.x["v"][:, 0], o[:, h], lse[h]) for h in range(2)]
+        with np.errstate(invalid="ignore"):
+            check_gradients(name, heads, c.scale, c.seen(0), ([dq[:, 0], dq[:, 1]], dk[:, 0], dv[:, 0]), kinds=False)
+        if spoil is spoil_do:
+            assert np.isfinite(dv[token + 1:]).all() and np.isfinite(dk[token + 1:]).all() and np.isfinite(np.delete(dq, token, axis=0)).all()
+        else:
+            assert np.isfinite(o[:token]).all() and np.isfinite(dq[:token]).all()
 
 
 @pytest.mark.parametrize("name", ["bf16", "f32"])
