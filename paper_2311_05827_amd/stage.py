@@ -352,9 +352,19 @@ class SelfAttention(torch.nn.Module):
         self.pairs = T.ROTATE_NEIGHBOURS if neighbours else T.ROTATE_HALVES
         self.entry = NormLinear(features, (heads + 2 * self.kv_heads) * self.head_size, eps=eps, device=device, dtype=dtype)
         self.out = BlockLinear(heads * self.head_size, features, device=device, dtype=dtype)
-        rotated = self.head_size if rotated is None else rotated
-        self.register_buffer("frequencies", (base ** (-torch.arange(0, rotated, 2, dtype=torch.float64) / max(rotated, 1))).float().to(device),
-                             persistent=False)
+        self._rotated = self.head_size if rotated is None else rotated, base
+        self.register_buffer("frequencies", self._make_frequencies().to(device), persistent=False)
+
+    def _make_frequencies(self):
+        rotated, base = self._rotated
+        return (base ** (-torch.arange(0, rotated, 2, dtype=torch.float64) / max(rotated, 1))).float()
+
+    def _apply(self, fn, recurse=True):
+        kept = self.frequencies
+        super()._apply(fn, recurse)
+        # It moves with the module, but in float32 with the values that it has: fewer bits are angles off by radians, and it is in no state to load.
+        self.frequencies = (self._make_frequencies() if kept.is_meta else kept).to(self.frequencies.device)
+        return self
 
     def cache(self, sequences, capacity, page_size=64, dtype=torch.bfloat16):
         """A cache of this block's keys and values for so many sequences of up to `capacity` tokens."""

@@ -254,6 +254,21 @@ def test_shapes_that_a_stage_refuses(A):
             bad()
 
 
+def test_frequencies_stay_float32(A):
+    """Casting a block casts its weights; the frequencies keep their type and every bit, there and back."""
+    import torch
+    layer = A.stage.SelfAttention(64, 2, 1, 32, device="cpu")
+    want = layer.frequencies.clone()
+    assert want.dtype == torch.float32 and want.numel() == 16
+    for cast in (lambda m: m.bfloat16(), lambda m: m.float(), lambda m: m.half(), lambda m: m.to(torch.float64), lambda m: m.to("cpu", torch.bfloat16)):
+        assert cast(layer) is layer and layer.frequencies.dtype == torch.float32 and torch.equal(layer.frequencies, want)
+    assert layer.out.weight.dtype == torch.bfloat16 and "frequencies" in dict(layer.named_buffers()) and "frequencies" not in layer.state_dict()
+    away = A.stage.SelfAttention(64, 2, 1, 32, device="meta")
+    assert away.frequencies.is_meta and torch.equal(away.to_empty(device="cpu").frequencies, want)
+    layer.frequencies = want / 8    # somebody's own
+    assert torch.equal(layer.float().frequencies, want / 8)
+
+
 def test_oracle_against_sums_by_hand():
     """Three keys, two queries, one channel."""
     q, k, v = np.array([[1.0], [2.0]]), np.array([[0.5], [-1.0], [3.0]]), np.array([[1.0], [10.0], [100.0]])

@@ -145,6 +145,26 @@ def test_a_stage_served_from_a_cache(A, frozen):
         layer(x, cache=cache)   # with gradients
 
 
+def test_a_block_with_bfloat16_weights(A):
+    """The same float32 weights, rounded: trained and served as the block whose weights hold those values in float32 (its gradients, but for their rounding)."""
+    torch = torch_mod()
+    torch.manual_seed(5)
+    layer = A.stage.SelfAttention(128, 2, 1, 64).bfloat16()
+    same = A.stage.SelfAttention(128, 2, 1, 64)
+    same.load_state_dict(layer.state_dict())
+    x = torch.randn(2, 30, 128, device="cuda").bfloat16()
+    y, want = layer(x), same(x)
+    assert torch.equal(y, want)
+    y.backward(x)
+    want.backward(x)
+    for a, b in zip(layer.parameters(), same.parameters()):
+        assert a.grad.dtype == torch.bfloat16
+        assert torch.all((a.grad.float() - b.grad).abs() <= HALF_BF16 * b.grad.abs())
+    with torch.no_grad():
+        cache, other = layer.eval().cache(2, 64), same.eval().cache(2, 64)
+        assert torch.equal(layer(x, cache=cache), same(x, cache=other))
+
+
 def test_drafts_and_what_is_accepted(A):
     """A tree of drafted tokens attends without making the sequence longer; the accepted ones, appended again, give what their path in the
     tree gave: the same keys in the same order for every row but for where they lie, to the bounds of both."""
