@@ -197,6 +197,12 @@ def _tokens(t):
     return t.as_strided(t.shape, (heads * head, head, 1))  # one token has any stride, and is contiguous
 
 
+def _no_gradients(what, *tensors):
+    """Where a tensor's gradient would be lost without a word."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise ValueError("%s has no gradients: call it without them" % what)
+
+
 def _same_batch(offsets, *tensors):
     """Without offsets the tensors' sequences are those of one batch."""
     if offsets is None and len({t.shape[0] if t.dim() == 4 else None for t in tensors}) > 1:
@@ -312,10 +318,11 @@ class Cache:
 
     def step(self, q, k, v, offsets=None, frequencies=None, positions=None, tree=None, neighbours=False, scale=None, advance=None):
         """Append the new tokens' keys (turned, where there are frequencies) and values, and let their queries (turned) attend to all that their
-        sequences hold: o (tokens, heads, head), without gradients.  The tokens are those of `offsets`, or as many of each sequence.  tree (tokens, words)
+        sequences hold: o (tokens, heads, head), without gradients (tensors that ask for some are refused).  The tokens are those of `offsets`, or as many of each sequence.  tree (tokens, words)
         int64: the new tokens of its sequence that each token sees, as bits, instead of those up to itself; with it a token's position has to be given.
         Then the sequences are longer by their new tokens, unless `advance` says no: a tree's are to be appended again, those that were
         accepted, so `advance` is no for trees if nothing is said."""
+        _no_gradients("a cache", q, k, v, frequencies)
         if tree is not None and frequencies is not None and positions is None:
             raise ValueError("tokens of a tree need positions")
         _same_batch(offsets, q, k, v)
@@ -378,8 +385,7 @@ class SelfAttention(torch.nn.Module):
                 raise ValueError("positions and trees are for calls with a cache")
             o = _TurnedAttention.apply(qkv, self.frequencies, offsets, sequences, self.heads, self.kv_heads, self.pairs)
         else:
-            if torch.is_grad_enabled() and qkv.requires_grad:
-                raise ValueError("a cache holds no gradients: call it without them")
+            _no_gradients("a cache", qkv)
             if offsets is None and x.dim() == 3 and x.shape[0] != cache.table.shape[0]:
                 raise ValueError("a batch of %d for %d sequences" % (x.shape[0], cache.table.shape[0]))
             q, k, v = qkv.split([self.heads, self.kv_heads, self.kv_heads], 1)

@@ -254,6 +254,18 @@ def test_shapes_that_a_stage_refuses(A):
             bad()
 
 
+def test_a_cache_has_no_gradients(A):
+    """A step whose tensors ask for gradients is refused, as a block with a cache is: what it returned would have none."""
+    import torch
+    cache, x, f = A.stage.Cache(1, 16, 2, 64, device="cpu", dtype=torch.float32), torch.zeros(3, 2, 64), torch.zeros(32)
+    for i in range(4):
+        ask = [t.clone().requires_grad_(True) if j == i else t for j, t in enumerate((x, x, x, f))]
+        with pytest.raises(ValueError, match="gradients"):
+            cache.step(*ask[:3], frequencies=ask[3])
+        with torch.no_grad(), pytest.raises(A.AcceptError):   # (these tensors are on the host)
+            cache.step(*ask[:3], frequencies=ask[3])
+
+
 def test_frequencies_stay_float32(A):
     """Casting a block casts its weights; the frequencies keep their type and every bit, there and back."""
     import torch
