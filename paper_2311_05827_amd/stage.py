@@ -235,7 +235,8 @@ class _Rotate(torch.autograd.Function):
 def rotate(x, frequencies, offsets=None, positions=None, neighbours=False):
     """x (batch, n, heads, head) or (tokens, heads, head) turned by its tokens' positions: their places in their sequences (those of a
     batch; or of `offsets`, sequences + 1 int32 device values), or `positions` (int32, one a token).  frequencies: a float32 for each pair, the angle of a
-    step; pairs are a value of the first half of those that turn and one of the second, or two neighbours."""
+    step (no gradient: one that asks for it is refused); pairs are a value of the first half of those that turn and one of the second, or two neighbours."""
+    _no_gradients("rotation by frequencies", frequencies)
     return _Rotate.apply(x, frequencies, offsets, positions, T.ROTATE_NEIGHBOURS if neighbours else T.ROTATE_HALVES)
 
 

@@ -254,6 +254,15 @@ def test_shapes_that_a_stage_refuses(A):
             bad()
 
 
+def test_frequencies_have_no_gradients(A):
+    import torch
+    x, f = torch.zeros(6, 2, 64, requires_grad=True), torch.zeros(32, requires_grad=True)
+    with pytest.raises(ValueError, match="gradients"):
+        A.stage.rotate(x, f)
+    with torch.no_grad(), pytest.raises(A.AcceptError):   # (they are on the host)
+        A.stage.rotate(x, f)
+
+
 def test_a_cache_has_no_gradients(A):
     """A step whose tensors ask for gradients is refused, as a block with a cache is: what it returned would have none."""
     import torch
