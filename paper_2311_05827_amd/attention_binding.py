@@ -4,7 +4,7 @@ gradients, a cache of pages and the attention over it.
 Argument marshalling only, as in stage_binding.py: tensors are checked on the host against the descriptor, outputs that are not
 given are allocated, and the kernels run on the current stream of the current device, where the tensors have to be.  Queries, keys, values and
 outputs are (tokens, heads, head_size), their tokens `stride` elements apart, or (tokens, heads * head_size).  What a call allocates
-holds zeros for tokens behind the last sequence, whatever the descriptor's `rest` says; what it is given follows the descriptor.
+holds zeros (lse: minus infinity) for tokens behind the last sequence, whatever the descriptor's `rest` says; what it is given follows the descriptor.
 csrc/native.cpp makes the same checks and calls without the interpreter; whatever it does not take comes to the code here, which says
 what is wrong.
 """
@@ -213,11 +213,13 @@ def accept_attention(desc, q, k, v, q_offsets=None, k_offsets=None, o=None, lse=
     where = "accept_attention"
     _check_attention(where, desc, q, k, v, q_offsets, k_offsets)
     sizes = (desc.q_tokens, desc.heads, desc.head_size)
-    made = o is None
+    made = o is None and lse is None
+    one = not made and q_offsets is not None  # one of the two: what is made here has its rest from here
     if lse is None:
-        lse = torch.empty((desc.heads, desc.q_tokens), dtype=torch.float32, device=q.device)
-    if made:
-        o = _make_tokens(q, *sizes, desc.o_stride)
+        lse = torch.full((desc.heads, desc.q_tokens), float("-inf"), dtype=torch.float32, device=q.device) if one else \
+            torch.empty((desc.heads, desc.q_tokens), dtype=torch.float32, device=q.device)
+    if o is None:
+        o = _make_tokens(q, *sizes, desc.o_stride, one)
     _check_tokens(o, where, "o", q.dtype, *sizes, desc.o_stride)
     S._check_table(lse, where, "lse", torch.float32, desc.heads, desc.q_tokens)
     workspace = _workspace(where, workspace, accept_attention_workspace_size(desc), q.device)

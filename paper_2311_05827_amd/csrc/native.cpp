@@ -465,7 +465,8 @@ PyObject* attention(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (o) tokens(o, d.q_tokens, d.heads, d.head_size, d.o_stride);
     if (lse) c.table(lse, at::kFloat, d.heads, d.q_tokens);
     if (wb && ws) c.ok = c.ok && fits(ws, wb) && ws->get_device() == c.device;
-    if (!c.ok) return PyLong_FromLong(kNotHere);
+    // one of the two made here and the other given: the slow way's, as their rests differ
+    if (!c.ok || (qo && !o != !lse)) return PyLong_FromLong(kNotHere);
     at::Tensor mo, ml, mws;
     if (!o) {
       mo = make_tokens(*q, d.q_tokens, d.heads, d.head_size, d.o_stride, q->scalar_type()), o = &mo;

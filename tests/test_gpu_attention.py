@@ -338,6 +338,22 @@ def test_rows_behind_the_last_sequence(A):
     assert all(torch.equal(g, m) for g, m in zip(grads, made))
 
 
+def test_one_output_given_and_one_made(A):
+    """Each has its own rest: kept in what is given, zeros or minus infinity in what is made."""
+    torch = torch_mod()
+    c = Case(A, 25, "bf16", [50, 20], [50, 20], 2, 1, 64, behind=300)
+    o, lse = (t.clone() for t in c.forward())
+    torch.full((2, 370), 9.0, device="cuda"), torch.full((370, 2, 64), 9.0, device="cuda").bfloat16()   # (what an allocation may find)
+    given = torch.full_like(lse, 7.0)
+    made, same = c.forward(lse=given)
+    assert same is given and torch.all(given[:, 70:] == 7) and torch.equal(given[:, :70], lse[:, :70]) and torch.equal(made, o)
+    given = torch.full_like(o, 7.0)
+    same, made = c.forward(o=given)
+    assert same is given and torch.all(given[70:] == 7) and torch.equal(given[:70], o[:70]) and torch.equal(made, lse)
+    c.desc.rest = A.REST_ZEROS
+    assert torch.equal(c.forward(lse=torch.full_like(lse, 7.0))[1], lse) and torch.equal(c.forward(o=torch.full_like(o, 7.0))[0], o)
+
+
 def test_offsets_beyond_the_tokens_stay_inside(A):
     """Offsets are device data that no host check sees: whatever they hold, nothing outside the tensors is read or written.  (The kernels
     bring them inside first; what such a call computes is not specified.)"""
