@@ -173,32 +173,39 @@ __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
   return uniform(a / b);
 }
 
-// The same with the longest sequences first (of every 64), so that a launch ends with short pieces of work: 12288 tokens in seven sequences,
+// find_among of up to 64 sequences with the longest ones first, so that a launch ends with short pieces of work: 12288 tokens in seven sequences,
 // 32 heads, the gradients of keys and values in 793 us in their own order, 718 so; 16 x 509 tokens, 12 heads of 64, forward 28.4 and 22.2.
 template <typename F, typename L>
 __device__ __forceinline__ Found find_longest_first(int sequences, int64_t at, const F& size, const L& length) {
   const int lane = threadIdx.x % kWave;
-  int64_t before = 0;
-  for (int base = 0; base < sequences; base += kWave) {
-    const int here = sequences - base < kWave ? sequences - base : kWave;
-    const int n = lane < here ? int(size(base + lane)) : 0, key = lane < here ? int(length(base + lane)) : -1;
-    int64_t mine = before, all = 0;
-    for (int j = 0; j < here; ++j) {
-      const int n_j = __builtin_amdgcn_readlane(n, j), key_j = __builtin_amdgcn_readlane(key, j);
-      if (key_j > key || (key_j == key && j < lane)) mine += n_j;
-      all += n_j;
-    }
-    const uint64_t it = __ballot(lane < here && mine <= at && at < mine + n);
-    if (it) {
-      const int first = __builtin_ctzll(it);
-      return {base + first, __shfl(mine, first, kWave)};
-    }
-    before += all;
+  const int n = lane < sequences ? int(size(lane)) : 0, key = lane < sequences ? int(length(lane)) : -1;
+  int64_t mine = 0, all = 0;
+  for (int j = 0; j < sequences; ++j) {
+    const int n_j = __builtin_amdgcn_readlane(n, j), key_j = __builtin_amdgcn_readlane(key, j);
+    if (key_j > key || (key_j == key && j < lane)) mine += n_j;
+    all += n_j;
   }
-  return {-1, before};
+  const uint64_t it = __ballot(lane < sequences && mine <= at && at < mine + n);
+  if (!it) return {-1, all};
+  const int first = __builtin_ctzll(it);
+  return {first, __shfl(mine, first, kWave)};
+}
+// The last s of 0 .. count for which value(s) <= at, where value does not fall from one s to the next (0 if there is none); 64 of them at a time.
+template <typename F>
+__device__ __forceinline__ int last_up_to(int count, int64_t at, const F& value) {
+  const int lane = threadIdx.x % kWave;
+  int lo = 0, left = count;  // it is one of lo .. lo + left
+  while (left > 0) {
+    const int step = (left + kWave - 1) / kWave, mine = step * (lane + 1) < left ? step * (lane + 1) : left;
+    const int n = __builtin_popcountll(__ballot(value(lo + mine) <= at));
+    const int below = step * n < left ? step * n : left, above = step * (n + 1) < left ? step * (n + 1) : left;
+    left = n == kWave || above == below ? 0 : above - 1 - below;
+    lo += below;
+  }
+  return uniform(lo);
 }
 // Piece number `index`, heaviest ones first, of sequences that are cut in pieces of `rows` tokens: its sequence, and its place in it with the
-// last piece first (seq -1: number `tile` of the pieces of the tokens behind the last sequence).
+// last piece first (seq -1: number `tile` of the pieces of the tokens behind the last sequence, or behind those).
 struct Piece {
   int seq, tile;
 };
@@ -206,6 +213,19 @@ __device__ __forceinline__ Piece find_piece(const int32_t* offsets, int sequence
   if (!offsets) {
     const int per = pieces(each, rows);
     return {index % sequences, per - 1 - index / sequences};
+  }
+  if (sequences > kWave) {
+    // More than a look at all of them: sequence s has the numbers from first(s) on, of which there are as many as it has pieces at least (some
+    // are nobody's).  1024 sequences of 16 tokens, 32 heads on 8 of 128, forward: 320 us, and 5060 by counting the pieces of those in front, which grows with the
+    // square of their number; 65 of 250 122, where counting 64 of 256 takes 178 and gives the order of lengths.
+    const auto first = [&](int s) { return span_of(offsets, s, tokens, 0).begin / rows + s; };
+    const int rest = rest_of(offsets, sequences, tokens), behind = index - (rest / rows + sequences);
+    if (behind >= 0) return {-1, uniform(behind)};
+    const int seq = last_up_to(sequences - 1, index, first);
+    const Span span = uniform_span(offsets, seq, tokens, 0);
+    const int in = index - (span.begin / rows + seq), of = pieces(span.size(), rows);
+    if (in < 0 || in >= of) return {-1, tokens / rows + 1};
+    return {seq, of - 1 - in};
   }
   const Found f = find_longest_first(sequences, index, [&](int s) { return pieces(span_of(offsets, s, tokens, 0).size(), rows); },
                                      [&](int s) { return span_of(offsets, s, tokens, 0).size(); });

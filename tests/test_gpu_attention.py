@@ -108,6 +108,22 @@ def test_both_passes(A, name, causal, q_lengths, k_lengths, heads, kv_heads, hea
 
 
 @pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("sequences", [65, 600, 5000])
+def test_many_short_sequences(A, name, sequences):
+    """More than a workgroup looks at: a few longer than its rows among them, empty ones, and tokens behind the last."""
+    lengths = [0 if s % 11 == 0 else 260 if s % 400 == 33 else 129 if s % 300 == 64 else 1 + s * s % 7 for s in range(sequences)]
+    keys = [n + 3 * (s % 2) if s % 13 else 0 for s, n in enumerate(lengths)]
+    c = Case(A, 26, name, lengths, keys, 2, 1, 16, behind=150)
+    o, lse = c.forward()
+    grads = c.backward()
+    c.check_forward()
+    c.check_backward(grads)
+    for t, n in ((o, c.q_ends[-1]), (grads[0], c.q_ends[-1]), (grads[1], c.k_ends[-1]), (grads[2], c.k_ends[-1])):
+        assert n + 150 == t.shape[0] and (t[n:] == 0).all()
+    assert (lse[:, c.q_ends[-1]:] == -np.inf).all()
+
+
+@pytest.mark.parametrize("name", ["bf16", "f32"])
 def test_equal_sequences_without_offsets(A, name):
     c = Case(A, 2, name, [45] * 3, [45] * 3, 4, 2, 64, packed=False)
     c.forward()
