@@ -37,6 +37,7 @@ struct CachePlan {
   bool rows;      // many rows a sequence: items of 128 (see cached_rows_kernel), else of 32
   int64_t items;  // at most so many
   int parts;      // of the work of a key head
+  size_t sums;    // in the workspace, behind the parts' results: sums over more sequences than a wavefront counts
   size_t bytes;   // workspace
 };
 CachePlan make_cache_plan(const accept_cache_desc& d);
@@ -101,69 +102,60 @@ __device__ __forceinline__ int rest_of(const int32_t* offsets, int sequences, in
   return e < 0 ? 0 : e > tokens ? tokens : e;
 }
 
-// Where number `at` is when the sequences have size(s) numbers each: the sequence, and its first number; seq = -1 where there
-// are fewer, `before` being how many there are then.  A wavefront together; the same for all of its lanes.
+// The last s of 0 .. count for which value(s) <= at, where value does not fall from one s to the next (0 if there is none); 64 of them at a time.
+template <typename F>
+__device__ __forceinline__ int last_up_to(int count, int64_t at, const F& value) {
+  const int lane = threadIdx.x % kWave;
+  int lo = 0, left = count;  // it is one of lo .. lo + left
+  while (left > 0) {
+    const int step = (left + kWave - 1) / kWave, mine = step * (lane + 1) < left ? step * (lane + 1) : left;
+    const int n = __builtin_popcountll(__ballot(value(lo + mine) <= at));
+    const int below = step * n < left ? step * n : left, above = step * (n + 1) < left ? step * (n + 1) : left;
+    left = n == kWave || above == below ? 0 : above - 1 - below;
+    lo += below;
+  }
+  return uniform(lo);
+}
+// Where a number is when the sequences have size(s) numbers each, one behind the other: the sequence, and its first number; seq = -1 where there
+// are fewer, `before` being how many there are then.  A wavefront counts them together, up to 64 sequences; where there are more, `sums` has what lies in front of each
+// and in all.  The same for all lanes.
 struct Found {
   int seq;
   int64_t before;
 };
-template <typename F>
-__device__ __forceinline__ Found find_among(int sequences, int64_t at, const F& size) {
-  const int lane = threadIdx.x % kWave;
-  int64_t before = 0;
-  for (int base = 0; base < sequences; base += kWave) {
-    const int64_t n = base + lane < sequences ? int64_t(size(base + lane)) : 0;
-    int64_t incl = n;
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-      const int64_t up = __shfl_up(incl, d, kWave);
-      if (lane >= d) incl += up;
-    }
-    const uint64_t past = __ballot(before + incl > at);
-    if (past) {
-      const int first = __builtin_ctzll(past);
-      return {base + first, before + __shfl(incl - n, first, kWave)};
-    }
-    before += __shfl(incl, kWave - 1, kWave);
-  }
-  return {-1, before};
-}
-// find_among for several questions: up to 64 sequences are counted once.
-template <typename F>
 struct Index {
   int sequences;
-  const F& size;
+  const int64_t* sums;
   int64_t incl, total;
-  __device__ __forceinline__ Index(int sequences_, const F& size_) : sequences(sequences_), size(size_) {
-    if (sequences <= kWave) {
-      const int lane = threadIdx.x % kWave;
-      incl = lane < sequences ? int64_t(size(lane)) : 0;
-      if (sequences > 1) {
+  template <typename F>
+  __device__ __forceinline__ Index(int sequences_, const int64_t* sums_, const F& size) : sequences(sequences_), sums(sums_), incl(0) {
+    if (sums) {
+      total = uniform(sums[sequences]);
+      return;
+    }
+    const int lane = threadIdx.x % kWave;
+    incl = lane < sequences ? int64_t(size(lane)) : 0;
+    if (sequences > 1) {
 #pragma unroll
-        for (int d = 1; d < kWave; d *= 2) {
-          const int64_t up = __shfl_up(incl, d, kWave);
-          if (lane >= d) incl += up;
-        }
-        total = uniform(__shfl(incl, kWave - 1, kWave));
-      } else {
-        total = uniform(incl);  // lane 0's
+      for (int d = 1; d < kWave; d *= 2) {
+        const int64_t up = __shfl_up(incl, d, kWave);
+        if (lane >= d) incl += up;
       }
+      total = uniform(__shfl(incl, kWave - 1, kWave));
     } else {
-      total = uniform(find_among(sequences, INT64_MAX, size).before);
+      total = uniform(incl);  // lane 0's
     }
   }
   // what lies in front of a sequence
   __device__ __forceinline__ int64_t before(int seq) const {
-    if (sequences > kWave) return uniform(find_among(seq, INT64_MAX, size).before);
+    if (sums) return uniform(sums[seq]);
     return seq == 0 ? 0 : uniform(__shfl(incl, seq - 1, kWave));
   }
   __device__ __forceinline__ Found find(int64_t at) const {
-    if (sequences > kWave) {
-      const Found f = find_among(sequences, at, size);
-      return {uniform(f.seq), uniform(f.before)};
-    }
     if (at >= total) return {-1, total};
-    const int seq = sequences > 1 ? __builtin_ctzll(__ballot(incl > at)) : 0;
+    int seq = 0;
+    if (sums) seq = last_up_to(sequences - 1, at, [&](int s) { return sums[s]; });
+    else if (sequences > 1) seq = __builtin_ctzll(__ballot(incl > at));
     return {seq, before(seq)};
   }
 };
@@ -173,7 +165,7 @@ __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
   return uniform(a / b);
 }
 
-// find_among of up to 64 sequences with the longest ones first, so that a launch ends with short pieces of work: 12288 tokens in seven sequences,
+// The same of up to 64 sequences with the longest ones first, so that a launch ends with short pieces of work: 12288 tokens in seven sequences,
 // 32 heads, the gradients of keys and values in 793 us in their own order, 718 so; 16 x 509 tokens, 12 heads of 64, forward 28.4 and 22.2.
 template <typename F, typename L>
 __device__ __forceinline__ Found find_longest_first(int sequences, int64_t at, const F& size, const L& length) {
@@ -189,20 +181,6 @@ __device__ __forceinline__ Found find_longest_first(int sequences, int64_t at, c
   if (!it) return {-1, all};
   const int first = __builtin_ctzll(it);
   return {first, __shfl(mine, first, kWave)};
-}
-// The last s of 0 .. count for which value(s) <= at, where value does not fall from one s to the next (0 if there is none); 64 of them at a time.
-template <typename F>
-__device__ __forceinline__ int last_up_to(int count, int64_t at, const F& value) {
-  const int lane = threadIdx.x % kWave;
-  int lo = 0, left = count;  // it is one of lo .. lo + left
-  while (left > 0) {
-    const int step = (left + kWave - 1) / kWave, mine = step * (lane + 1) < left ? step * (lane + 1) : left;
-    const int n = __builtin_popcountll(__ballot(value(lo + mine) <= at));
-    const int below = step * n < left ? step * n : left, above = step * (n + 1) < left ? step * (n + 1) : left;
-    left = n == kWave || above == below ? 0 : above - 1 - below;
-    lo += below;
-  }
-  return uniform(lo);
 }
 // Piece number `index`, heaviest ones first, of sequences that are cut in pieces of `rows` tokens: its sequence, and its place in it with the
 // last piece first (seq -1: number `tile` of the pieces of the tokens behind the last sequence, or behind those).

@@ -10,6 +10,8 @@ struct CacheArgs {
   const void* v;
   void* o;
   float* parts_at;  // results of pieces of an item: see slot_at
+  const int64_t* item_sums;  // items in front of every sequence, and in all; units.  Null where a wavefront counts them
+  const int64_t* unit_sums;
   const int32_t* offsets;
   const int32_t* lengths;
   const int32_t* table;
@@ -52,8 +54,7 @@ struct Step {
   int keys;    // places that its tokens may see
   int64_t items, units;  // units of every item
 };
-template <typename S>
-__device__ __forceinline__ Step step_of(const CacheArgs& g, int seq) {
+__device__ __forceinline__ Step step_of(const CacheArgs& g, int seq, int item, int unit) {
   Step s;
   s.span = span_of(g.offsets, seq, g.tokens, g.each);
   const int64_t capacity = g.pages.count > 0 ? int64_t(g.pages.table_pages) << g.pages.shift : 0;
@@ -61,10 +62,14 @@ __device__ __forceinline__ Step step_of(const CacheArgs& g, int seq) {
   s.length = given < 0 ? 0 : given;
   const int64_t all = int64_t(s.length) + n;
   s.keys = int(all < capacity ? all : capacity);
-  s.items = (int64_t(n) * g.group + S::kItem - 1) / S::kItem;
-  const int64_t units = (int64_t(s.keys) + S::kUnit - 1) / S::kUnit;
+  s.items = (int64_t(n) * g.group + item - 1) / item;
+  const int64_t units = (int64_t(s.keys) + unit - 1) / unit;
   s.units = units > 0 ? units : 1;
   return s;
+}
+template <typename S>
+__device__ __forceinline__ Step step_of(const CacheArgs& g, int seq) {
+  return step_of(g, seq, S::kItem, S::kUnit);
 }
 template <typename S>
 __device__ __forceinline__ Step uniform_step(const CacheArgs& g, int seq) {
@@ -93,7 +98,7 @@ __device__ __forceinline__ Walk begin_walk(const CacheArgs& g, int part) {
     const Step st = step_of<S>(g, s);
     return st.items * st.units;
   };
-  const Index<decltype(work)> index(g.sequences, work);
+  const Index index(g.sequences, g.unit_sums, work);
   const int parts = used_parts(index.total, g.parts);
   if (part >= parts) return {0, 0, 0, 0};
   const int64_t at = part_begin(index.total, parts, part);
@@ -113,6 +118,10 @@ __device__ __forceinline__ bool next_stretch(const CacheArgs& g, Walk& w, Stretc
     if (in >= all) {
       w.before += all;
       ++w.seq;
+      if (g.unit_sums && w.seq < g.sequences && uniform(g.unit_sums[w.seq + 1]) <= w.at) {  // (not one by one over those without work)
+        w.seq = last_up_to(g.sequences - 1, w.at, [&](int i) { return g.unit_sums[i]; });
+        w.before = uniform(g.unit_sums[w.seq]);
+      }
       continue;
     }
     s.item = quotient(in, s.st.units);
@@ -537,6 +546,47 @@ __global__ __launch_bounds__((RowsShape<T, DB>::kThreads), 1) void cached_rows_k
   }
 }
 
+// Items and units in front of every sequence, and in all, for Index: in one workgroup, where there are more than 64 sequences.  (8192 of 5 tokens, one
+// new token each, 32 heads on 8 of 128, bfloat16: 1795 us, and 23700 with every wavefront counting all of them, which grows with the square of their number; 65 of 700
+// tokens 53 and 56.)
+constexpr int kSumThreads = 1024;
+__global__ __launch_bounds__(kSumThreads) void cached_sums_kernel(const CacheArgs g, int64_t* item_sums, int64_t* unit_sums, int item, int unit) {
+  __shared__ int64_t of_waves[2][kSumThreads / kWave];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  int64_t before[2] = {0, 0};
+  for (int base = 0; base < g.sequences; base += kSumThreads) {
+    const int seq = base + int(threadIdx.x);
+    int64_t n[2] = {0, 0}, incl[2];
+    if (seq < g.sequences) {
+      const Step st = step_of(g, seq, item, unit);
+      n[0] = st.items;
+      n[1] = st.items * st.units;
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      incl[i] = n[i];
+#pragma unroll
+      for (int d = 1; d < kWave; d *= 2) {
+        const int64_t up = __shfl_up(incl[i], d, kWave);
+        if (lane >= d) incl[i] += up;
+      }
+      if (lane == kWave - 1) of_waves[i][wave] = incl[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      int64_t front = before[i];
+      for (int w = 0; w < kSumThreads / kWave; ++w) {
+        if (w < wave) front += of_waves[i][w];
+        before[i] += of_waves[i][w];
+      }
+      if (seq < g.sequences) (i ? unit_sums : item_sums)[seq] = front + incl[i] - n[i];
+    }
+    __syncthreads();
+  }
+  if (threadIdx.x < 2) (threadIdx.x ? unit_sums : item_sums)[g.sequences] = before[threadIdx.x];
+}
+
 constexpr int kMaxParts = 256;  // of a key head's work
 __device__ __forceinline__ int up_to_block(int v) { return (v + kBlock - 1) / kBlock * kBlock; }
 
@@ -549,7 +599,7 @@ __global__ __launch_bounds__(kBlock) void cached_join_kernel(const CacheArgs g) 
   __shared__ v4f_t halves[kBlock];
   const int kv = blockIdx.y, row_in = int(blockIdx.z) * kRows;  // of the item
   const auto items = [&](int s) { return step_of<S>(g, s).items; };
-  const Found f = Index<decltype(items)>(g.sequences, items).find(blockIdx.x);
+  const Found f = Index(g.sequences, g.item_sums, items).find(blockIdx.x);
   const int seq = f.seq;
   const int64_t item = int64_t(blockIdx.x) - f.before;
   if (seq < 0) {
@@ -567,7 +617,7 @@ __global__ __launch_bounds__(kBlock) void cached_join_kernel(const CacheArgs g) 
     const Step each = step_of<S>(g, s);
     return each.items * each.units;
   };
-  const Index<decltype(work)> index(g.sequences, work);
+  const Index index(g.sequences, g.unit_sums, work);
   const int64_t all = index.total, before = index.before(seq);
   const int parts = used_parts(all, g.parts);
   const int64_t first = before + item * st.units, last = first + st.units - 1;
@@ -639,6 +689,10 @@ __global__ __launch_bounds__(kBlock) void cached_join_kernel(const CacheArgs g) 
 template <typename T, int DB>
 void launch_both(const CacheArgs& g, const CachePlan& p, int kv_heads, hipStream_t s) {
   const dim3 grid(uint32_t(g.parts), uint32_t(kv_heads));
+  if (g.item_sums)
+    cached_sums_kernel<<<dim3(1), kSumThreads, 0, s>>>(g, const_cast<int64_t*>(g.item_sums), const_cast<int64_t*>(g.unit_sums),
+                                                       p.rows ? RowsShape<T, DB>::kItem : KeysShape<T, DB>::kItem,
+                                                       p.rows ? RowsShape<T, DB>::kUnit : KeysShape<T, DB>::kUnit);
   if (p.rows) {
     using S = RowsShape<T, DB>;
     cached_rows_kernel<T, DB><<<grid, S::kThreads, 0, s>>>(g);
@@ -673,7 +727,8 @@ CachePlan make_cache_plan(const accept_cache_desc& d) {
   // as many workgroups as the chip has room for: one a compute unit, two where few rows of short heads leave room in shared memory
   const int64_t groups = !p.rows && d.dtype == ACCEPT_BF16 && d.head_size <= 64 ? 512 : 256;
   p.parts = int(blocks_of(groups, d.kv_heads) < kMaxParts ? blocks_of(groups, d.kv_heads) : kMaxParts);
-  p.bytes = size_t(up_to(int64_t(d.kv_heads) * p.parts * 2 * item * (width + 2) * 4, 256));
+  p.sums = size_t(up_to(int64_t(d.kv_heads) * p.parts * 2 * item * (width + 2) * 4, 256));
+  p.bytes = p.sums + (d.sequences > kWave ? size_t(up_to(16 * (d.sequences + 1), 256)) : 0);
   return p;
 }
 
@@ -684,6 +739,10 @@ hipError_t launch_cache_attention(const accept_cache_desc& d, const CachePlan& p
   const int64_t whole = int64_t(d.heads) * d.head_size;
   g.q = q, g.k = k_cache, g.v = v_cache, g.o = o;
   g.parts_at = static_cast<float*>(ws);
+  if (d.sequences > kWave) {
+    g.item_sums = reinterpret_cast<const int64_t*>(static_cast<const uint8_t*>(ws) + p.sums);
+    g.unit_sums = g.item_sums + d.sequences + 1;
+  }
   g.offsets = offsets, g.lengths = lengths, g.table = table, g.tree = tree;
   g.q_stride = d.q_stride ? d.q_stride : whole;
   g.o_stride = d.o_stride ? d.o_stride : whole;

@@ -62,6 +62,31 @@ def test_parts_with_several_items(A, name, contexts, new, heads, kv_heads, head,
     c.check_attention()
 
 
+MANY = {
+    "few rows": ([(s * s) % 45 for s in range(600)], [(s % 4) if s % 7 else 0 for s in range(600)]),
+    "many rows": ([(s * s) % 45 for s in range(300)], [33 + s % 5 if s % 7 else 0 for s in range(300)]),
+    "few of them, few rows": ([(s * s) % 45 for s in range(3000)], [2 * (s % 500 == 7 or s == 2999) for s in range(3000)]),
+    "few of them, many rows": ([700 * (s == 1007) for s in range(1025)], [3001 * (s in (0, 1007, 1008, 1024)) for s in range(1025)]),
+    "none": ([5] * 100, [0] * 100),
+}
+
+
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("which", MANY)
+def test_more_sequences_than_are_counted(A, name, which):
+    """Sequences without new tokens between and behind those with some, tokens behind the last one, and a workspace that holds what was there."""
+    torch = torch_mod()
+    contexts, new = MANY[which]
+    heads = 12 if which.endswith("them, many rows") else 2
+    c = Cache(A, 4, name, contexts, new, heads, 1, 16, 16, behind=70)
+    many = sum(new) * heads > 32 * len(new)
+    assert many == (which.endswith("many rows"))
+    c.append()
+    c.attend(workspace=torch.full((A.accept_cache_workspace_size(c.desc),), 255, dtype=torch.uint8, device="cuda"))
+    assert torch.all(c.o[c.ends[-1]:] == 0)
+    c.check_attention()
+
+
 @pytest.mark.parametrize("name", ["bf16", "f32"])
 @pytest.mark.parametrize("new", [9, 70])   # wavefronts with keys of their own, and with keys that they share
 def test_a_value_that_some_do_not_see(A, name, new):
