@@ -98,7 +98,8 @@ typedef struct {
 /*
  * o_i = sum over the keys j that i sees of p_ij v_j, p_ij = exp(scale * q_i k_j - lse_i), lse_i = log(sum over j of exp(scale * q_i k_j)).
  * Rows that see no key: o = 0, lse = minus infinity.  Rows that see scores of minus infinity only: o = NaN, as the formula has it, lse = minus infinity,
- * and gradients as from there.  What a row does not see has no effect on it, infinities and NaN included.
+ * and gradients as from there.  Rows that see a score that is NaN or plus infinity (also one that float32 does not hold): o and lse NaN.  What a row does not see has no effect on it,
+ * infinities and NaN included.
  * lse_dev (heads x q_tokens floats) may be null.  Products and sums are float32's; with bfloat16 tensors p is rounded to
  * bfloat16 for its product with v, as an operand of the matrix instruction.  workspace_dev: accept_attention_workspace_size bytes, 16-byte aligned (null where that is 0).
  */

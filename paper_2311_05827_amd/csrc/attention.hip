@@ -33,14 +33,14 @@ constexpr float kBehind = 8.0f;
 // takes them from.  Tiles of keys and values come into shared memory one ahead.
 //
 // Bound by what a SIMD issues: for 64 keys its wavefronts have 32 products of 32 x 32 x 16 (heads of 128) and, beside them, 1024 exponentials with
-// scale, sum and rounding, and matrix and vector unit are busy 50 and 55 % of the time, one after the other more than side by side.  16384
-// tokens, 16 heads on 2 of 128 in bfloat16: 1.05 to 1.13 ms, 1050 TFLOP/s (the library's 8192^3 product: 1147); 8144 tokens in 16 sequences,
-// 12 heads of 64: 19 us, twice what its
+// scale, sum and rounding, and matrix and vector unit are busy 58 and 59 % of the time, one after the other more than side by side.  16384
+// tokens, 16 heads on 2 of 128 in bfloat16: 1.00 to 1.09 ms, 1050 TFLOP/s (the library's 8192^3 product: 1150 to 1390); 8144 tokens in 16 sequences,
+// 12 heads of 64: 16 to 18 us, twice what its
 // tensors take to go through memory: a workgroup has 8 tiles at most, and its start and end are a good part.  Tried, and slower
 // at the first of these: 32 keys at a time with the next scores' products among the exponentials 1160 to 1208 us; 64 queries a wavefront, whose
 // registers leave one of them a SIMD, 1733; priority for the wavefront that multiplies 1130; eight wavefronts in two halves that take turns at products and exponentials 1079 to 1116.  All of the keys' parts
 // asked for before the first product, instead of each before its own: 1095 us, 1072 so.  In float32 the products are 2 deep and
-// are the bound: 4096 tokens, 16 heads of 128, 664 us, 104 TFLOP/s of the 153 that the library's product reaches.
+// are the bound: 4096 tokens, 32 heads of 64, 610 us, 112 TFLOP/s of the 153 that the library's product reaches.
 template <typename T, int DB, bool SPLIT>
 __global__ __launch_bounds__(kWaves * kWave, groups_a_unit(DB, sizeof(T))) void attention_kernel(const AttentionArgs g) {
   constexpr int NB = sizeof(T) == 2 ? 2 : 1, BN = 32 * NB;

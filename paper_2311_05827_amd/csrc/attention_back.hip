@@ -47,7 +47,7 @@ __device__ __forceinline__ void clear_rest(T* to, int64_t stride, int head, int 
 }
 
 // dq: 128 queries of a head, a lane has a query of its own as in the forward pass; the sums of do * o, which both kernels need, are made on the way.
-// Bound as the forward pass is, with three products of tiles for its two.  12288 tokens in 7 sequences, 32 heads on 8 of 128, bfloat16: 385 to
+// Bound as the forward pass is, with three products of tiles for its two.  12288 tokens in 7 sequences, 32 heads on 8 of 128, bfloat16: 380 to
 // 400 us, 860 TFLOP/s of these products.
 template <typename T, int DB>
 __global__ __launch_bounds__(kWaves * kWave, groups_a_unit(DB, sizeof(T))) void back_queries_kernel(const BackArgs g) {
@@ -189,7 +189,7 @@ __global__ __launch_bounds__(kWaves * kWave, groups_a_unit(DB, sizeof(T))) void 
 // dk and dv: 128 keys of a key head, a lane has a key of its own; tiles of 32 queries and their do come through shared memory, head after
 // head of those that share the key head.  Wide heads in bfloat16 leave their values in shared memory: with both gradients' sums and the
 // keys in registers there are two wavefronts a SIMD then, one of which multiplies while the other one exponentiates.  (12288 tokens in 7 sequences, 32
-// heads on 8 of 128, bfloat16: 495 to 560 us, four products of tiles at 800 to 900 TFLOP/s; with the values in registers and one wavefront a SIMD
+// heads on 8 of 128, bfloat16: 490 to 520 us, four products of tiles at 800 to 900 TFLOP/s; with the values in registers and one wavefront a SIMD
 // 875.  All of a tile's parts asked for before its first product, instead of each before its own: all gradients 993 us, 972 so.)
 // Heads of 256 have registers for one of the two gradients (K: dk, V: dv), and a launch for each.
 template <typename T, int DB, bool K, bool V>

@@ -356,7 +356,7 @@ struct Rows {
   }
 };
 
-// Bound by memory where there is enough of it to read: 240000 tokens in 48 sequences, 32 heads on 8 of 128, bfloat16, 164 to 176 us, 5.6 to 6.0 TB/s
+// Bound by memory where there is enough of it to read: 240000 tokens in 48 sequences, 32 heads on 8 of 128, bfloat16, 160 to 166 us, 5.9 to 6.1 TB/s
 // (a copy: 5.2).  With a single sequence of 4001 tokens it is trips to memory one behind the other (the lengths, the table, the tiles: 7.6 us).  Loads with
 // the hint that a line is read once took 176 to 164 us off the former.
 template <typename T, int DB>
@@ -461,8 +461,9 @@ __global__ __launch_bounds__((KeysShape<T, DB>::kThreads), 1) void cached_keys_k
   }
 }
 
-// Bound by products and exponentials as attention_kernel is: 55000 tokens in six sequences, trees of 40 with 4 query heads a key head, 105 us, of
-// which about 25 are not the walk over the keys: five of a workgroup's eight wavefronts have rows, so that one SIMD has those of two.
+// 55000 tokens in six sequences, trees of 40 with 4 query heads a key head, bfloat16: 109 us.  Bound by waiting: matrix and vector unit are busy 15 and 25 % of the
+// time.  Five of a workgroup's eight wavefronts have rows, one SIMD those of two, and all meet at a barrier for every 32 keys, a chain of product, maximum,
+// exponential and product apart.
 template <typename T, int DB>
 __global__ __launch_bounds__((RowsShape<T, DB>::kThreads), 1) void cached_rows_kernel(const CacheArgs g) {
   using S = RowsShape<T, DB>;
@@ -720,7 +721,9 @@ int blocks_of_head(int head) { return head <= 32 ? 1 : head <= 64 ? 2 : head <= 
 CachePlan make_cache_plan(const accept_cache_desc& d) {
   CachePlan p{};
   const int64_t rows = d.tokens * (d.heads / d.kv_heads);
-  p.rows = rows > 32 * d.sequences;  // more than one wavefront's, of a sequence on average
+  // More than one wavefront's, of a sequence on average: for all of a step's sequences, whatever each has.  (Contexts of 8000, 32 heads on 8 of 128, bfloat16: a chunk of
+  // 512 takes 150 us so by itself, 47 single tokens 245 the other way, and both in one step 755 the other way, 127 with the chunk 960.)
+  p.rows = rows > 32 * d.sequences;
   const int blocks = blocks_of_head(d.head_size), width = blocks * 32;
   const int item = !p.rows ? 32 : blocks * (d.dtype == ACCEPT_F32 ? 4 : 2) <= 8 ? 256 : 128;  // (as in RowsShape)
   p.items = rows / item + d.sequences + 1;

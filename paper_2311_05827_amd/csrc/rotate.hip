@@ -76,7 +76,7 @@ __global__ __launch_bounds__(kBlock) void rotate_kernel(const RotateArgs g) {
   const int64_t all = int64_t(per_token) * g.tokens;
   const bool mine = at < all;
   const int token = !mine ? g.tokens - 1 : all >> 32 == 0 ? int(uint32_t(at) / per_token) : int(at / per_token);
-  // the token's sequence: a wavefront's tokens lie next to each other, so the first one's is searched for, and from there on
+  // the token's sequence, searched for (a wavefront's tokens lie next to each other, so its lanes look at the same offsets)
   int seq = 0, place = token;
   bool outside = false;
   if (!g.offsets) {

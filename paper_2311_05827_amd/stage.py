@@ -304,7 +304,9 @@ class Cache:
     """Keys and values of the sequences that a server is at, in pages of `page_size` tokens, and how many tokens each has (`lengths`).
 
     Sequences have room for `capacity` tokens each, their pages in order, unless `pages` (how many there are) and `table` (sequences, pages of each;
-    int32 on the device) say otherwise; a table may be changed between steps, and sequences may share the pages that none of them writes."""
+    int32 on the device) say otherwise; a table may be changed between steps, and sequences may share the pages that none of them writes.  `lengths` are on
+    the device, so no call looks whether there is room: a token behind its sequence's last page in the table has no place, its key and value are
+    dropped, and nobody sees it, itself included."""
 
     def __init__(self, sequences, capacity, kv_heads, head_size, page_size=64, dtype=torch.bfloat16, device="cuda", pages=None, table=None):
         each = -(-capacity // page_size)

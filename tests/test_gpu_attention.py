@@ -382,6 +382,23 @@ def test_offsets_beyond_the_tokens_stay_inside(A):
     assert c.o.shape == (70, 2, 64)
 
 
+def test_offsets_of_many_sequences_beyond_the_tokens_stay_inside(A):
+    """The same with more sequences than a workgroup looks at: offsets that rise, fall and go outside."""
+    torch = torch_mod()
+    rng = np.random.default_rng(27)
+    c = Case(A, 27, "bf16", [2] * 300, [2] * 300, 2, 1, 64)
+    want, _ = c.forward()
+    want = want.clone()
+    good = c.q_off, c.k_off
+    c.q_off, c.k_off = (ints(rng.integers(-(1 << 31), 1 << 31, 301)) for _ in range(2))
+    c.forward()
+    c.backward()
+    torch.cuda.synchronize()
+    assert c.o.shape == (600, 2, 64)
+    c.q_off, c.k_off = good
+    assert torch.equal(c.forward()[0], want)
+
+
 def test_no_tokens(A):
     torch = torch_mod()
     for name in ("bf16", "f32"):
