@@ -331,6 +331,24 @@ def test_scores_of_minus_infinity(A, name, head, causal):
     assert np.isnan(o[150:180]).all() and np.all(lse[:, 150:180] == -np.inf) and np.isnan(grads[1][150:180]).all() and np.isnan(grads[0][150:180]).all()
 
 
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [150, 1500])   # one share, and some
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_scores_that_are_not_finite(A, name, n, bad):
+    """Rows that see a score of NaN or plus infinity are NaN, and the logarithm of their sum is; the others are as without that key."""
+    def spoil(values):
+        values["q"][:, :, 0] = 1.0
+        values["k"][n - 50, :, 0] = bad
+    c = Case(A, 28, name, [n], [n], 1, 1, 64, change=spoil)
+    assert (A.accept_attention_workspace_size(c.desc) > 0) == (n == 1500)
+    o, lse = (f64(t) for t in c.forward())
+    assert np.isnan(o[n - 50:]).all() and np.isnan(lse[:, n - 50:]).all()
+    first = slice(0, n - 50)
+    check_forward(name, c.x["q"][first, 0], c.x["k"][first, 0], c.x["v"][first, 0], c.seen(0)[first, first], c.scale, o[first, 0], lse[0, first])
+    dq, dk, dv = (f64(g) for g in c.backward())
+    assert np.isfinite(dq[first]).all() and np.isnan(dq[n - 50:]).all() and np.isnan(dk).all() and np.isnan(dv).all()
+
+
 def test_rows_behind_the_last_sequence(A):
     """Left as they were in what the caller gives, zeros in what the call makes or where the descriptor says so."""
     torch = torch_mod()

@@ -304,6 +304,24 @@ def test_scores_of_minus_infinity(A, name, head, new):
         check_forward(name, c.xq[2 * new:3 * new, h], k[600:, 0], v[600:, 0], seen, c.scale, o[2 * new:3 * new, h])
 
 
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_scores_that_are_not_finite(A, name, new, bad):
+    """A context's key whose score is NaN or plus infinity, in one of many parts and in the only one; the third sequence has none."""
+    c = Cache(A, 22, name, [900, 20, 300], [new] * 3, 2, 1, 64, 16)
+    c.q[:, :, 0], c.xq[:, :, 0] = 1.0, 1.0
+    for s, j in ((0, 400), (1, 3)):
+        p, at = orc.place(c.table[s], 16, j)
+        c.k_cache[p, :, at, 0] = bad
+    c.append()
+    o = f64(c.attend())
+    assert np.isnan(o[:2 * new]).all() and np.isfinite(o[2 * new:]).all()
+    k, v, _ = c.held(2)
+    for h in range(2):
+        check_forward(name, c.xq[2 * new:, h], k[:, 0], v[:, 0], orc.causal(new, 300 + new), c.scale, o[2 * new:, h])
+
+
 def test_steps_of_a_server(A):
     """A prompt, then token after token: the same attention as over the whole sequence at once, to the bounds of both (the cache holds the
     same bfloat16 keys, so the scores agree; weights and results are rounded in two orders)."""
