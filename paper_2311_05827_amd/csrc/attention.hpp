@@ -77,6 +77,12 @@ __device__ __forceinline__ A fresh_arguments() {
   __builtin_memcpy(&a, (const void*)at, sizeof(A));
   return a;
 }
+template <typename A, typename F>
+__device__ __forceinline__ F fresh_argument(F A::*field) {  // one of its members
+  auto at = __builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(at));
+  return ((const A*)(const void*)at)->*field;
+}
 
 // ---- sequences ---------------------------------------------------------------------------------
 // First token and end of a sequence; whatever the offsets hold, inside 0 .. tokens.

@@ -118,9 +118,10 @@ __device__ __forceinline__ bool next_stretch(const CacheArgs& g, Walk& w, Stretc
     if (in >= all) {
       w.before += all;
       ++w.seq;
-      if (g.unit_sums && w.seq < g.sequences && uniform(g.unit_sums[w.seq + 1]) <= w.at) {  // (not one by one over those without work)
-        w.seq = last_up_to(g.sequences - 1, w.at, [&](int i) { return g.unit_sums[i]; });
-        w.before = uniform(g.unit_sums[w.seq]);
+      const int64_t* const sums = fresh_argument(&CacheArgs::unit_sums);
+      if (sums && w.seq < g.sequences && uniform(sums[w.seq + 1]) <= w.at) {  // (not one by one over those without work)
+        w.seq = last_up_to(g.sequences - 1, w.at, [&](int i) { return sums[i]; });
+        w.before = uniform(sums[w.seq]);
       }
       continue;
     }
